@@ -51,7 +51,8 @@ enum {
   ZC_ERR_ALIGN = -6,    /* a device pointer is not 16-byte aligned */
   ZC_ERR_LAUNCH = -7,   /* the HIP runtime refused the launch */
   ZC_ERR_DTYPE = -8,    /* dtype is not ZC_BF16 or ZC_F16 */
-  ZC_ERR_STREAM = -9    /* zl_stream_bytes: the buffer does not start with a complete lossless stream */
+  ZC_ERR_STREAM = -9,   /* zl_stream_bytes: the buffer does not start with a complete lossless stream */
+  ZC_ERR_ARG = -10      /* zt_*: a number, a kind or a combination that the call does not take */
 };
 
 /* Element types of a message buffer.  The fp32 calls take no dtype argument. */

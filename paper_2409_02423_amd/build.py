@@ -1,19 +1,20 @@
-"""Compile the HIP library (csrc/zc_kernels.hip, csrc/zc2d_kernels.hip, csrc/zl_kernels.hip) for gfx950 into
+"""Compile the HIP library (csrc/zc_kernels.hip, csrc/zc2d_kernels.hip, csrc/zl_kernels.hip, csrc/zt_step.hip, csrc/zt_norm.hip,
+csrc/zt_norm_backward.hip) for gfx950 into
 libzc.so next to this file, and the lossless kernels once more, with their tuning knobs, into
 libzl_knobs.so for the tests.  hipcc cross-compiles without a GPU."""
 import os
 import subprocess
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SOURCES = [os.path.join(HERE, "csrc", f) for f in ("zc_kernels.hip", "zc2d_kernels.hip", "zl_kernels.hip")]
-DEPS = SOURCES + [os.path.join(HERE, "csrc", f) for f in ("zc_codec.h", "zc_half.h", "zc2d_codec.h", "zc2d_grid.h", "zl_codec.h")] + [
-                  os.path.join(HERE, "..", "include", "zc.h")]
+SOURCES = [os.path.join(HERE, "csrc", f) for f in ("zc_kernels.hip", "zc2d_kernels.hip", "zl_kernels.hip", "zt_step.hip", "zt_norm.hip", "zt_norm_backward.hip")]
+DEPS = SOURCES + [os.path.join(HERE, "csrc", f) for f in ("zc_codec.h", "zc_half.h", "zc2d_codec.h", "zc2d_grid.h", "zl_codec.h", "zt_device.h", "zt_norm.h")] + [
+                  os.path.join(HERE, "..", "include", h) for h in ("zc.h", "zt.h")]
 LIB = os.path.join(HERE, "libzc.so")
 STAMP = LIB + ".stamp"   # digest of what the library was built from (file times do not survive every copy)
 # The lossless calls alone, reading ZL_PATIENCE and ZL_WORKGROUPS_PER_CU from the environment: for tests
 # of what the shipped library does in rare conditions only.
 KNOBS_LIB = os.path.join(HERE, "libzl_knobs.so")
-KNOBS_SOURCES = SOURCES[2:]
+KNOBS_SOURCES = SOURCES[2:3]
 KNOBS_FLAGS = ("-DZC_TUNING_KNOBS",)
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -967,12 +967,13 @@ const char* zc_strerror(int code) {
     case ZC_ERR_NULL: return "null pointer";
     case ZC_ERR_RATE: return "unsupported rate (a multiple of 4 between 4 and 32; 2, 4, 8 or 16 for the 4 x 4 block codec)";
     case ZC_ERR_SIZE: return "buffer too large";
-    case ZC_ERR_CAPACITY: return "output capacity smaller than zc_compressed_size(n, rate)";
-    case ZC_ERR_K: return "number of chunks outside [1, 16]";
-    case ZC_ERR_ALIGN: return "device pointer not 16-byte aligned";
+    case ZC_ERR_CAPACITY: return "output capacity smaller than zc_compressed_size(n, rate) (zt_*: workspace too small)";
+    case ZC_ERR_K: return "number of chunks outside [1, 16] (zt_*: negative number of tensors)";
+    case ZC_ERR_ALIGN: return "device pointer not 16-byte aligned (zt_*: not aligned to its elements)";
     case ZC_ERR_LAUNCH: return "kernel launch failed";
-    case ZC_ERR_DTYPE: return "dtype must be ZC_BF16 or ZC_F16";
+    case ZC_ERR_DTYPE: return "dtype must be ZC_BF16 or ZC_F16 (zt_*: or ZC_F32)";
     case ZC_ERR_STREAM: return "not a complete lossless stream";
+    case ZC_ERR_ARG: return "a number, a kind or a combination that the call does not take";
     default: return "unknown error code";
   }
 }

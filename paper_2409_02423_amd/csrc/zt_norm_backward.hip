@@ -1,0 +1,377 @@
+// zt_norm_backward.hip -- gfx950 kernels and C ABI of the residual join with the norms around a block, backward (include/zt.h).
+//
+// As forward, a row stays in registers.  The sums over the rows, for weights, biases and a gate per channel, stay there too: a
+// workgroup takes many rows, adds their terms up lane by lane and leaves one partial sum for each column; a second kernel adds the
+// partial sums up in their order, so the result does not depend on which workgroup was first.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "zt_norm.h"
+
+namespace {
+
+struct BackwardArgs {
+  const char *dy, *dh, *y, *b, *gate, *pre_w, *post_w, *post_c;
+  const float4* stats;
+  char *dx, *db, *dgate;
+  float* partial;                // [workgroup or wavefront][sum][padded columns]
+  size_t sdy, sdh, sy, sb, sg, sdx, sdb, sdg;
+  uint32_t rows;
+  int cols, padded;
+  float scale, inv_cols;
+};
+
+// The sums over rows, in their order in the workspace.
+template <bool LAYER, bool POST, bool CHANNEL>
+struct SumIndex {
+  static constexpr int pre_w = 0, pre_c = 1, post_w = 1 + LAYER, post_c = 2 + LAYER, gate = 1 + LAYER + (POST ? 1 + LAYER : 0), count = gate + CHANNEL;
+};
+
+// A lane's sums over rows: in registers, or for wide rows (NV = 0) in the workspace, of which a workgroup has a part to itself.
+template <int COUNT, int DT, int NV, bool WAVE>
+struct Columns {
+  static constexpr int V = kVec<DT>;
+  float held[COUNT][NV > 0 ? NV : 1][V];
+  char* partial;
+  size_t one;          // bytes of one sum's columns
+  bool fresh = true;   // nothing in the workspace yet
+  __device__ __forceinline__ Columns(char* p, size_t bytes) : partial(p), one(bytes) {
+    if constexpr (NV > 0) {
+#pragma unroll
+      for (int k = 0; k < COUNT; ++k)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int j = 0; j < V; ++j) held[k][i][j] = 0.0f;
+    }
+  }
+  // Sum k of vector i: += a * b
+  __device__ __forceinline__ void add(const Lanes<DT, NV, WAVE>& at, int k, int i, const float (&a)[V], const float (&b)[V]) {
+    if constexpr (NV > 0) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) held[k][i][j] = fmaf(a[j], b[j], held[k][i][j]);
+    } else if (at.valid(i) > 0) {
+      Raw<kF32, V> r = {};
+      if (!fresh) r.load(partial + k * one, (uint32_t)at.col(i) * 4);
+      float s[V];
+      r.unpack(s);
+#pragma unroll
+      for (int j = 0; j < V; ++j) s[j] = fmaf(a[j], b[j], s[j]);
+      r.pack(s);
+      r.store(partial + k * one, (uint32_t)at.col(i) * 4);
+    }
+  }
+  __device__ __forceinline__ void add(const Lanes<DT, NV, WAVE>& at, int k, int i, const float (&a)[V]) {
+    float ones[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) ones[j] = 1.0f;
+    add(at, k, i, a, ones);
+  }
+  __device__ __forceinline__ void leave(const Lanes<DT, NV, WAVE>& at) const {
+    if constexpr (NV > 0) {
+#pragma unroll
+      for (int k = 0; k < COUNT; ++k)
+        at.each([&](int i) {
+          if (at.valid(i) > 0) {
+            Raw<kF32, V> r;
+            r.pack(held[k][i]);
+            r.store(partial + k * one, (uint32_t)at.col(i) * 4);
+          }
+        });
+    }
+  }
+};
+
+template <int DT, bool LAYER, bool POST, bool CHANNEL, int NV, int MOST>
+__global__ void __launch_bounds__(MOST == 64 ? 256 : MOST) norm_backward_kernel(BackwardArgs a) {
+  constexpr bool WAVE = MOST == 64;
+  constexpr int V = kVec<DT>, K = LAYER ? 2 : 1;
+  typedef SumIndex<LAYER, POST, CHANNEL> Index;
+  __shared__ float buffers[2][K][kMostWaves];
+  Sums<K, WAVE> sums{buffers};
+  const Lanes<DT, NV, WAVE> at(a.cols);
+  Values<DT, NV, WAVE> values;   // the gradient of y, then of z
+  Operand<DT, NV, WAVE> pre_w, post_w, post_c, gate, dy, dh, y, b;
+  const size_t one = (size_t)a.padded * sizeof(float);
+  Columns<Index::count, DT, NV, WAVE> columns(reinterpret_cast<char*>(a.partial) + at.first * Index::count * one, one);
+  for (uint32_t row = at.first; row < a.rows; row += at.step) {
+    const float4 stats = a.stats[row];
+    dh.open(at, a.dh + row * a.sdh);
+    y.open(at, a.y + row * a.sy);
+    pre_w.open(at, a.pre_w, 1.0f);
+    dy.open(at, a.dy ? a.dy + row * a.sdy : nullptr);
+    b.open(at, a.b ? a.b + row * a.sb : nullptr);
+    gate.open(at, a.gate ? a.gate + row * a.sg : nullptr, 1.0f);
+    if constexpr (POST) post_w.open(at, a.post_w, 1.0f);
+    if constexpr (POST && LAYER) post_c.open(at, a.post_c);
+    // a norm's input as it was normed, before weight and bias
+    const auto unit = [&](const Operand<DT, NV, WAVE>& from, int i, float mean, float r, float (&u)[V]) {
+      from.get(at, i, u);
+#pragma unroll
+      for (int j = 0; j < V; ++j) u[j] = LAYER ? (u[j] - mean) * r : u[j] * r;
+    };
+    // what a norm's gradient is made of: the sums of t = g w along u, and with LAYER of t
+    const auto add_sums = [&](float (&s)[K], const float (&g)[V], const float (&w)[V], const float (&u)[V]) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float t = g[j] * w[j];
+        s[0] = fmaf(t, u[j], s[0]);
+        if constexpr (LAYER) s[K - 1] += t;
+      }
+    };
+    // through the pre norm; behind the row's end dh is zero
+    float s[K] = {};
+    at.each([&](int i) {
+      float g[V], u[V], w[V];
+      dh.get(at, i, g);
+      unit(y, i, stats.z, stats.w, u);
+      pre_w.get(at, i, w);
+      columns.add(at, Index::pre_w, i, g, u);
+      if constexpr (LAYER) columns.add(at, Index::pre_c, i, g);
+      add_sums(s, g, w, u);
+    });
+    sums(s);
+    const float along = s[0] * a.inv_cols, mean = s[K - 1] * a.inv_cols;
+    float s2[K] = {};
+    at.each([&](int i) {
+      float g[V], u[V], w[V], d[V], v[V];
+      dh.get(at, i, g);
+      unit(y, i, stats.z, stats.w, u);
+      pre_w.get(at, i, w);
+      dy.get(at, i, d);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        float t = fmaf(-u[j], along, g[j] * w[j]);
+        if constexpr (LAYER) t -= mean;
+        d[j] = fmaf(stats.w, t, d[j]);
+        v[j] = a.scale * d[j];
+      }
+      if (a.dx) at.store(a.dx + row * a.sdx, i, v);
+      // through the gate
+      if constexpr (POST) {
+        unit(b, i, stats.x, stats.y, u);
+        post_w.get(at, i, w);
+      } else {
+        b.get(at, i, u);
+      }
+      if (CHANNEL || a.dgate) {
+        float z[V], c[V];
+        if constexpr (POST && LAYER) post_c.get(at, i, c);
+#pragma unroll
+        for (int j = 0; j < V; ++j) z[j] = !POST ? u[j] : LAYER ? fmaf(u[j], w[j], c[j]) : u[j] * w[j];
+        if constexpr (CHANNEL) {
+          columns.add(at, Index::gate, i, d, z);
+        } else {
+#pragma unroll
+          for (int j = 0; j < V; ++j) z[j] *= d[j];
+          at.store(a.dgate + row * a.sdg, i, z);
+        }
+      }
+      gate.get(at, i, g);
+#pragma unroll
+      for (int j = 0; j < V; ++j) d[j] *= g[j];
+      if constexpr (POST) {
+        at.clear_rest(d, i);
+        columns.add(at, Index::post_w, i, d, u);
+        if constexpr (LAYER) columns.add(at, Index::post_c, i, d);
+        add_sums(s2, d, w, u);
+        values.set(at, i, d);
+      } else if (a.db) {
+        at.store(a.db + row * a.sdb, i, d);
+      }
+    });
+    // through the post norm
+    if constexpr (POST) {
+      sums(s2);
+      const float along2 = s2[0] * a.inv_cols, mean2 = s2[K - 1] * a.inv_cols;
+      if (a.db) {
+        at.each([&](int i) {
+          float d[V], u[V], w[V];
+          values.get(at, i, d);
+          unit(b, i, stats.x, stats.y, u);
+          post_w.get(at, i, w);
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            float t = fmaf(-u[j], along2, d[j] * w[j]);
+            if constexpr (LAYER) t -= mean2;
+            d[j] = stats.y * t;
+          }
+          at.store(a.db + row * a.sdb, i, d);
+        });
+      }
+    }
+    columns.fresh = false;
+  }
+  columns.leave(at);
+}
+
+// Adds the partial sums up, in their order: a workgroup takes 64 columns of one sum, 16 lanes with four columns each and 16 slices of the
+// partial sums.
+struct ColumnArgs {
+  const float* partial;
+  float* out[5];
+  int partials, count, cols, padded;
+};
+__global__ void __launch_bounds__(256) column_sums_kernel(ColumnArgs a) {
+  __shared__ float4 slices[16][16];
+  const int lane = threadIdx.x & 15, slice = threadIdx.x / 16, k = blockIdx.y;
+  const int col = (blockIdx.x * 16 + lane) * 4;
+  float4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (col < a.padded) {
+    const float* p = a.partial + (size_t)k * a.padded + col;
+    const size_t step = (size_t)a.count * a.padded;
+#pragma unroll 4
+    for (int i = slice; i < a.partials; i += 16) {
+      const float4 v = *reinterpret_cast<const float4*>(p + i * step);
+      s.x += v.x;
+      s.y += v.y;
+      s.z += v.z;
+      s.w += v.w;
+    }
+  }
+  slices[slice][lane] = s;
+  __syncthreads();
+  float* out = a.out[k];
+  if (threadIdx.x < 64 && out) {
+    const int c = blockIdx.x * 64 + threadIdx.x;
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) t += reinterpret_cast<const float*>(slices[i])[threadIdx.x];
+    if (c < a.cols) out[c] = t;
+  }
+}
+
+// ---- host ------------------------------------------------------------------------------
+
+Layout backward_layout(size_t cols, int dtype) {
+  const size_t vectors = row_vectors(cols, dtype);
+  if (vectors <= 64) return {1, 64, 64};
+  if (vectors <= 256) return {1, lanes_for(vectors, 1), 256};
+  if (vectors <= 1024) return {1, lanes_for(vectors, 1), 1024};
+  return {0, 1024, 1024};
+}
+
+// Workgroups, and the partial sums that they leave, one for each workgroup or, in the layout for short rows, wavefront.
+constexpr size_t kMostPartials = 1024;
+struct BackwardGrid {
+  unsigned groups;
+  size_t partials;
+};
+BackwardGrid backward_grid(size_t rows, const Layout& l) {
+  const size_t waves = l.most == 64 ? 4 : 1;
+  size_t groups = (rows + waves - 1) / waves;
+  if (groups > kMostPartials / waves) groups = kMostPartials / waves;
+  return {(unsigned)groups, groups * waves};
+}
+
+int sums_of(const zt_residual& f) {
+  const int layer = f.kind == ZT_LAYER;
+  return 1 + layer + (f.post ? 1 + layer : 0) + (f.gate == ZT_GATE_CHANNEL);
+}
+size_t padded_cols(size_t cols) { return (cols + 7) / 8 * 8; }
+
+template <int DT, bool LAYER, bool POST, bool CHANNEL>
+void launch(const BackwardArgs& a, const Layout& l, unsigned groups, hipStream_t s) {
+  const unsigned threads = l.most == 64 ? 256 : l.lanes;
+#define CALL(NV, MOST) hipLaunchKernelGGL((norm_backward_kernel<DT, LAYER, POST, CHANNEL, NV, MOST>), dim3(groups), dim3(threads), 0, s, a)
+  if (l.most == 64) CALL(1, 64);
+  else if (l.most == 256) CALL(1, 256);
+  else if (l.vectors == 1) CALL(1, 1024);
+  else CALL(0, 1024);
+#undef CALL
+}
+template <int DT, bool LAYER, bool POST>
+void launch(const zt_residual& f, const BackwardArgs& a, const Layout& l, unsigned groups, hipStream_t s) {
+  f.gate == ZT_GATE_CHANNEL ? launch<DT, LAYER, POST, true>(a, l, groups, s) : launch<DT, LAYER, POST, false>(a, l, groups, s);
+}
+template <int DT>
+void launch(const zt_residual& f, const BackwardArgs& a, const Layout& l, unsigned groups, hipStream_t s) {
+  if (f.kind == ZT_LAYER) f.post ? launch<DT, true, true>(f, a, l, groups, s) : launch<DT, true, false>(f, a, l, groups, s);
+  else f.post ? launch<DT, false, true>(f, a, l, groups, s) : launch<DT, false, false>(f, a, l, groups, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t zt_residual_work_bytes(const struct zt_residual* form) {
+  if (check_form(form) != ZC_OK || form->rows == 0 || form->cols == 0) return 0;
+  const Layout l = backward_layout(form->cols, form->dtype);
+  return backward_grid(form->rows, l).partials * (size_t)sums_of(*form) * padded_cols(form->cols) * sizeof(float);
+}
+
+int zt_residual_norm_backward(const struct zt_residual* form, const void* d_dy, const void* d_dh, const void* d_y, const void* d_b,
+                              const void* d_gate, const void* d_pre_weight, const void* d_post_weight, const void* d_post_bias,
+                              const float* d_stats, void* d_dx, void* d_db, void* d_dgate, float* d_dpre_weight, float* d_dpre_bias,
+                              float* d_dpost_weight, float* d_dpost_bias, void* d_work, size_t work_bytes, void* stream) {
+  const int rc = check_form(form);
+  if (rc != ZC_OK) return rc;
+  const zt_residual& f = *form;
+  if (f.kind == ZT_RMS && (d_dpre_bias || d_dpost_bias || d_post_bias)) return ZC_ERR_ARG;
+  if ((!f.post && (d_dpost_weight || d_dpost_bias)) || (f.gate == ZT_GATE_NONE && d_dgate)) return ZC_ERR_ARG;
+  if (!good_strides({f.stride_dy, f.stride_dh, f.stride_y, f.stride_b, f.stride_gate}, {f.stride_dx, f.stride_db, f.stride_dgate}, f.cols)) return ZC_ERR_ARG;
+  if (!d_b && (f.post || f.gate != ZT_GATE_NONE || d_db)) return ZC_ERR_NULL;
+  if (f.cols == 0) return ZC_OK;
+  const size_t e = dtype_bytes(f.dtype);
+  const bool channel = f.gate == ZT_GATE_CHANNEL;
+  if (f.rows != 0 && (!d_dh || !d_y || !d_stats || !d_work || (f.gate != ZT_GATE_NONE && !d_gate))) return ZC_ERR_NULL;
+  if (!all_aligned({d_dy, d_dh, d_y, d_b, d_gate, d_pre_weight, d_post_weight, d_post_bias, d_dx, d_db}, e) || !aligned(d_dgate, channel ? 4 : e) ||
+      !all_aligned({d_dpre_weight, d_dpre_bias, d_dpost_weight, d_dpost_bias}, 4) || !aligned(d_stats, 16) || !aligned(d_work, 16))
+    return ZC_ERR_ALIGN;
+  if (work_bytes < zt_residual_work_bytes(form)) return ZC_ERR_CAPACITY;
+  BackwardArgs a;
+  a.dy = bytes_of(d_dy);
+  a.dh = bytes_of(d_dh);
+  a.y = bytes_of(d_y);
+  a.b = bytes_of(d_b);
+  a.gate = f.gate == ZT_GATE_NONE ? nullptr : bytes_of(d_gate);
+  a.pre_w = bytes_of(d_pre_weight);
+  a.post_w = bytes_of(d_post_weight);
+  a.post_c = bytes_of(d_post_bias);
+  a.stats = reinterpret_cast<const float4*>(d_stats);
+  a.dx = static_cast<char*>(d_dx);
+  a.db = static_cast<char*>(d_db);
+  a.dgate = channel ? nullptr : static_cast<char*>(d_dgate);
+  a.partial = static_cast<float*>(d_work);
+  a.sdy = stride_of(f.stride_dy, f.cols) * e;
+  a.sdh = stride_of(f.stride_dh, f.cols) * e;
+  a.sy = stride_of(f.stride_y, f.cols) * e;
+  a.sb = stride_of(f.stride_b, f.cols) * e;
+  a.sg = f.gate == ZT_GATE_FULL ? stride_of(f.stride_gate, f.cols) * e : 0;   // a gate per channel is the same for every row
+  a.sdx = stride_of(f.stride_dx, f.cols) * e;
+  a.sdb = stride_of(f.stride_db, f.cols) * e;
+  a.sdg = stride_of(f.stride_dgate, f.cols) * e;
+  a.rows = (uint32_t)f.rows;
+  a.cols = (int)f.cols;
+  a.padded = (int)padded_cols(f.cols);
+  a.scale = f.residual_scale;
+  a.inv_cols = (float)(1.0 / (double)f.cols);
+  const Layout l = backward_layout(f.cols, f.dtype);
+  const BackwardGrid grid = backward_grid(f.rows, l);
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (f.rows != 0) {
+    if (f.dtype == ZC_F32) launch<kF32>(f, a, l, grid.groups, s);
+    else if (f.dtype == ZC_BF16) launch<kBF16>(f, a, l, grid.groups, s);
+    else launch<kF16>(f, a, l, grid.groups, s);
+  }
+  ColumnArgs c;      // with no rows the sums are zero
+  int k = 0;
+  c.out[k++] = d_dpre_weight;
+  if (f.kind == ZT_LAYER) c.out[k++] = d_dpre_bias;
+  if (f.post) c.out[k++] = d_dpost_weight;
+  if (f.post && f.kind == ZT_LAYER) c.out[k++] = d_dpost_bias;
+  if (channel) c.out[k++] = static_cast<float*>(d_dgate);
+  bool wanted = false;
+  for (int i = 0; i < k; ++i) wanted = wanted || c.out[i];
+  if (wanted) {
+    c.partial = a.partial;
+    c.partials = (int)grid.partials;
+    c.count = k;
+    c.cols = a.cols;
+    c.padded = a.padded;
+    hipLaunchKernelGGL(column_sums_kernel, dim3((unsigned)((f.cols + 63) / 64), (unsigned)k), dim3(256), 0, s, c);
+  }
+  return finish_launch();
+}
+
+}  // extern "C"

@@ -1,0 +1,382 @@
+// zt_step.hip -- gfx950 kernels and C ABI of the optimizer's side of include/zt.h: the global gradient norm over many tensors,
+// clipping, the clipped AdamW step on a shard.
+//
+// All of them are bound by memory.  A list of tensors is cut into chunks of kChunk values of one tensor; the list travels in the
+// kernel's arguments, so nothing is copied to the GPU ahead of a launch, and lists longer than kMostTensors take several
+// launches.  The sum of squares is left as one double per workgroup of the first pass (ZT_SLOTS of them), which every workgroup of the
+// second pass adds up for itself, in the same order: no launch in between, and no atomics.
+#include <hip/hip_runtime.h>
+#include <float.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/zt.h"
+#include "zt_device.h"
+
+namespace {
+
+constexpr int kMostTensors = 112;      // of one launch: 3.4 KB of its arguments
+constexpr int kChunk = 8192;           // values
+constexpr size_t kMostChunks = (size_t)1 << 31;   // of one launch
+constexpr size_t kMaxValues = (size_t)1 << 40;    // of a tensor
+
+struct TensorList {
+  const char* in[kMostTensors];
+  char* out[kMostTensors];
+  unsigned long long n[kMostTensors];
+  uint32_t first[kMostTensors + 1];    // chunks of the tensors before this one
+  uint8_t in_type[kMostTensors], out_type[kMostTensors];
+  int count;
+};
+static_assert(sizeof(TensorList) + 64 <= 4096, "a launch's arguments");
+
+// The tensor that a chunk is of.
+__device__ __forceinline__ int tensor_of(const TensorList& list, uint32_t chunk) {
+  int low = 0, high = list.count - 1;
+  while (low < high) {
+    const int mid = (low + high + 1) / 2;
+    if (list.first[mid] <= chunk) low = mid;
+    else high = mid - 1;
+  }
+  return low;
+}
+
+// ---- sum of squares --------------------------------------------------------------------
+
+constexpr int kSumThreads = 1024;
+
+template <int DT>
+__device__ __forceinline__ void add_squares(const char* p, size_t left, double (&sum)[2]) {
+  constexpr int kSteps = kChunk / kSumThreads / kVec<DT>;
+  Raw<DT> raw[kSteps];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int at = (threadIdx.x + i * kSumThreads) * kVec<DT>;
+    const int valid = left >= (size_t)kChunk ? kVec<DT> : (int)left - at;
+    raw[i].load(p, at * kBytes<DT>, valid);
+  }
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+    for (int j = 0; j < kVec<DT>; ++j) {
+      const double v = raw[i].get(j);      // 24 significant bits: the square is exact
+      sum[j & 1] = __builtin_fma(v, v, sum[j & 1]);
+    }
+}
+
+__global__ void __launch_bounds__(kSumThreads) sum_squares_kernel(TensorList list, int accumulate, double* slots) {
+  __shared__ double buffer[1][kMostWaves];
+  double sum[2] = {0.0, 0.0};
+  const uint32_t chunks = list.first[list.count];
+  for (uint32_t chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
+    const int t = tensor_of(list, chunk);
+    const size_t at = (size_t)(chunk - list.first[t]) * kChunk;
+    const size_t left = list.n[t] - at;
+    const char* p = list.in[t];
+    switch (list.in_type[t]) {
+      case kF32: add_squares<kF32>(p + at * 4, left, sum); break;
+      case kBF16: add_squares<kBF16>(p + at * 2, left, sum); break;
+      default: add_squares<kF16>(p + at * 2, left, sum); break;
+    }
+  }
+  double total[1] = {sum[0] + sum[1]};
+  group_sum(total, buffer);
+  if (threadIdx.x == 0) slots[blockIdx.x] = accumulate ? slots[blockIdx.x] + total[0] : total[0];
+}
+
+// ---- the norm and the factor -----------------------------------------------------------
+
+constexpr int kThreads = 256;
+static_assert(ZT_SLOTS % kThreads == 0, "slots per lane");
+
+// Total of the slots, the same in every lane of every workgroup.
+__device__ __forceinline__ double slots_total(const double* slots, double (&buffer)[1][kMostWaves]) {
+  double v[1] = {0.0};
+#pragma unroll
+  for (int i = 0; i < ZT_SLOTS / kThreads; ++i) v[0] += slots[threadIdx.x + i * kThreads];
+  group_sum(v, buffer);
+  return v[0];
+}
+
+__device__ __forceinline__ float clip_factor(double norm, float scale, float max_norm) {
+  return norm <= (double)max_norm ? scale : (float)((double)scale * ((double)max_norm / norm));
+}
+
+__global__ void __launch_bounds__(kThreads) norm_kernel(const double* slots, float scale, float* norm) {
+  __shared__ double buffer[1][kMostWaves];
+  const double total = slots_total(slots, buffer);
+  if (threadIdx.x == 0) norm[0] = (float)((double)scale * sqrt(total));
+}
+
+// ---- clipping --------------------------------------------------------------------------
+
+template <int DI, int DO>
+__device__ __forceinline__ void scale_chunk(const char* in, char* out, size_t left, float factor) {
+  constexpr int kN = DI == kF32 && DO == kF32 ? 4 : 8;   // values per lane and step
+  constexpr int kSteps = kChunk / kThreads / kN;
+  Raw<DI, kN> raw[kSteps];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int at = (threadIdx.x + i * kThreads) * kN;
+    const int valid = left >= (size_t)kChunk ? kN : (int)left - at;
+    raw[i].load(in, at * kBytes<DI>, valid);
+  }
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int at = (threadIdx.x + i * kThreads) * kN;
+    const int valid = left >= (size_t)kChunk ? kN : (int)left - at;
+    float v[kN];
+    raw[i].unpack(v);
+#pragma unroll
+    for (int j = 0; j < kN; ++j) v[j] *= factor;
+    Raw<DO, kN> result;
+    result.pack(v);
+    result.store(out, at * kBytes<DO>, valid);
+  }
+}
+
+__global__ void __launch_bounds__(kThreads) clip_kernel(TensorList list, const double* slots, float scale, float max_norm, float* norm_out) {
+  __shared__ double buffer[1][kMostWaves];
+  const double norm = (double)scale * sqrt(slots_total(slots, buffer));
+  if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) norm_out[0] = (float)norm;
+  const float factor = clip_factor(norm, scale, max_norm);
+  const uint32_t chunks = list.first[list.count];
+  for (uint32_t chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
+    const int t = tensor_of(list, chunk);
+    const size_t at = (size_t)(chunk - list.first[t]) * kChunk;
+    const size_t left = list.n[t] - at;
+    const int di = list.in_type[t], dt = list.out_type[t];
+    const char* in = list.in[t] + at * (di == kF32 ? 4 : 2);
+    char* out = list.out[t] + at * (dt == kF32 ? 4 : 2);
+    switch (di * 3 + dt) {
+      case kF32 * 3 + kF32: scale_chunk<kF32, kF32>(in, out, left, factor); break;
+      case kF32 * 3 + kBF16: scale_chunk<kF32, kBF16>(in, out, left, factor); break;
+      case kF32 * 3 + kF16: scale_chunk<kF32, kF16>(in, out, left, factor); break;
+      case kBF16 * 3 + kF32: scale_chunk<kBF16, kF32>(in, out, left, factor); break;
+      case kBF16 * 3 + kBF16: scale_chunk<kBF16, kBF16>(in, out, left, factor); break;
+      case kBF16 * 3 + kF16: scale_chunk<kBF16, kF16>(in, out, left, factor); break;
+      case kF16 * 3 + kF32: scale_chunk<kF16, kF32>(in, out, left, factor); break;
+      case kF16 * 3 + kBF16: scale_chunk<kF16, kBF16>(in, out, left, factor); break;
+      default: scale_chunk<kF16, kF16>(in, out, left, factor); break;
+    }
+  }
+}
+
+// ---- AdamW -----------------------------------------------------------------------------
+
+struct AdamwArgs {
+  const char* grad;
+  const double* slots;
+  float *param, *m, *v;
+  char* half;
+  float* norm_out;
+  size_t n;
+  float lr, beta1, rest1, beta2, rest2, eps, weight_decay, correct1, correct2;   // correct: 1 / (1 - beta^step)
+  float scale, max_norm;
+};
+
+// DG: the gradients' type; DH: that of the copy, kF32 for none.
+template <int DG, int DH>
+__global__ void __launch_bounds__(kThreads) adamw_kernel(AdamwArgs a) {
+  __shared__ double buffer[1][kMostWaves];
+  constexpr int kN = 4;
+  float factor = a.scale;
+  bool finite = true;
+  if (a.slots) {
+    const double norm = (double)a.scale * sqrt(slots_total(a.slots, buffer));
+    if (a.norm_out && blockIdx.x == 0 && threadIdx.x == 0) a.norm_out[0] = (float)norm;
+    factor = clip_factor(norm, a.scale, a.max_norm);
+    finite = norm < __builtin_inf();
+  }
+  constexpr int kTile = kThreads * kN;
+  const size_t tiles = (a.n + kTile - 1) / kTile;
+  for (size_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    const size_t start = tile * kTile, left = a.n - start;
+    const uint32_t at = threadIdx.x * kN;
+    const int valid = left >= (size_t)kTile ? kN : (int)left - (int)at;
+    char *param = reinterpret_cast<char*>(a.param + start), *first = reinterpret_cast<char*>(a.m + start), *second = reinterpret_cast<char*>(a.v + start);
+    Raw<DG, kN> rg;
+    Raw<kF32, kN> rp, rm, rv;
+    rg.load(a.grad + start * kBytes<DG>, at * kBytes<DG>, valid);
+    rp.load(param, at * 4, valid);
+    rm.load(first, at * 4, valid);
+    rv.load(second, at * 4, valid);
+    float g[kN], p[kN], m[kN], v[kN];
+    rg.unpack(g);
+    rp.unpack(p);
+    rm.unpack(m);
+    rv.unpack(v);
+    if (finite) {
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        const float gc = g[j] * factor;
+        m[j] = fmaf(a.beta1, m[j], a.rest1 * gc);
+        v[j] = fmaf(a.beta2, v[j], a.rest2 * (gc * gc));
+        const float update = (m[j] * a.correct1) / (sqrtf(v[j] * a.correct2) + a.eps);
+        p[j] = fmaf(-a.lr, fmaf(a.weight_decay, p[j], update), p[j]);
+      }
+      rp.pack(p);
+      rm.pack(m);
+      rv.pack(v);
+      rp.store(param, at * 4, valid);
+      rm.store(first, at * 4, valid);
+      rv.store(second, at * 4, valid);
+    }
+    if constexpr (DH != kF32) {
+      Raw<DH, kN> rh;
+      rh.pack(p);
+      rh.store(a.half + start * 2, at * 2, valid);
+    }
+  }
+}
+
+// ---- host ------------------------------------------------------------------------------
+
+constexpr unsigned kMostGroups = 2048;   // of the second pass: eight per CU
+
+// Checks a list of tensors; `out` NULL for the sum of squares.
+int check_list(const void* const* d_in, const size_t* n, const int* in_type, void* const* d_out, const int* out_type, int count, bool writes) {
+  if (count < 0) return ZC_ERR_K;
+  if (count == 0) return ZC_OK;
+  if (!d_in || !n || !in_type || (writes && (!d_out || !out_type))) return ZC_ERR_NULL;
+  for (int i = 0; i < count; ++i) {
+    if (!known_dtype(in_type[i]) || (writes && !known_dtype(out_type[i]))) return ZC_ERR_DTYPE;
+    if (n[i] == 0) continue;
+    if (n[i] > kMaxValues) return ZC_ERR_SIZE;
+    if (!d_in[i] || (writes && !d_out[i])) return ZC_ERR_NULL;
+    if (writes && d_in[i] == d_out[i] && in_type[i] != out_type[i]) return ZC_ERR_ARG;
+    if (!aligned(d_in[i], dtype_bytes(in_type[i])) || (writes && !aligned(d_out[i], dtype_bytes(out_type[i])))) return ZC_ERR_ALIGN;
+  }
+  return ZC_OK;
+}
+
+// Fills `list` with the tensors from `from` on that one launch takes; returns the first that it does not.
+int fill_list(TensorList& list, const void* const* d_in, const size_t* n, const int* in_type, void* const* d_out, const int* out_type, int count, int from) {
+  list.count = 0;
+  list.first[0] = 0;
+  size_t chunks = 0;
+  int i = from;
+  for (; i < count && list.count < kMostTensors; ++i) {
+    if (n[i] == 0) continue;
+    const size_t more = (n[i] + kChunk - 1) / kChunk;
+    if (chunks + more > kMostChunks && list.count > 0) break;
+    const int t = list.count++;
+    list.in[t] = static_cast<const char*>(d_in[i]);
+    list.out[t] = d_out ? static_cast<char*>(d_out[i]) : nullptr;
+    list.n[t] = n[i];
+    list.in_type[t] = (uint8_t)in_type[i];
+    list.out_type[t] = out_type ? (uint8_t)out_type[i] : 0;
+    chunks += more;
+    list.first[t + 1] = (uint32_t)chunks;
+  }
+  return i;
+}
+
+bool good_scale(float scale) { return scale > 0.0f && scale < INFINITY; }
+bool good_max_norm(float max_norm) { return max_norm > 0.0f; }
+
+}  // namespace
+
+extern "C" {
+
+int zt_sum_squares(const void* const* d_in, const size_t* n, const int* dtype, int count, int accumulate, double* d_slots, void* stream) {
+  const int rc = check_list(d_in, n, dtype, nullptr, nullptr, count, false);
+  if (rc != ZC_OK) return rc;
+  if (!d_slots) return ZC_ERR_NULL;
+  if (!aligned(d_slots, 16)) return ZC_ERR_ALIGN;
+  TensorList list;
+  int next = 0;
+  bool launched = false;
+  do {
+    next = fill_list(list, d_in, n, dtype, nullptr, nullptr, count, next);
+    if (list.count == 0 && accumulate) break;      // nothing (more) to add
+    hipLaunchKernelGGL(sum_squares_kernel, dim3(ZT_SLOTS), dim3(kSumThreads), 0, static_cast<hipStream_t>(stream), list, accumulate, d_slots);
+    accumulate = 1;
+    launched = true;
+  } while (next < count);
+  return launched ? finish_launch() : ZC_OK;
+}
+
+int zt_norm(const double* d_slots, float scale, float* d_norm, void* stream) {
+  if (!good_scale(scale)) return ZC_ERR_ARG;
+  if (!d_slots || !d_norm) return ZC_ERR_NULL;
+  if (!aligned(d_slots, 16) || !aligned(d_norm, 4)) return ZC_ERR_ALIGN;
+  hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(kThreads), 0, static_cast<hipStream_t>(stream), d_slots, scale, d_norm);
+  return finish_launch();
+}
+
+int zt_clip(const void* const* d_in, const size_t* n, const int* dtype_in, void* const* d_out, const int* dtype_out, int count,
+            const double* d_slots, float scale, float max_norm, float* d_norm, void* stream) {
+  const int rc = check_list(d_in, n, dtype_in, d_out, dtype_out, count, true);
+  if (rc != ZC_OK) return rc;
+  if (!good_scale(scale) || !good_max_norm(max_norm)) return ZC_ERR_ARG;
+  if (!d_slots) return ZC_ERR_NULL;
+  if (!aligned(d_slots, 16) || !aligned(d_norm, 4)) return ZC_ERR_ALIGN;
+  TensorList list;
+  int next = 0;
+  bool launched = false;
+  do {
+    next = fill_list(list, d_in, n, dtype_in, d_out, dtype_out, count, next);
+    const uint32_t chunks = list.first[list.count];
+    if (chunks == 0 && !d_norm) break;
+    const unsigned groups = chunks == 0 ? 1 : chunks < kMostGroups ? chunks : kMostGroups;
+    hipLaunchKernelGGL(clip_kernel, dim3(groups), dim3(kThreads), 0, static_cast<hipStream_t>(stream), list, d_slots, scale, max_norm, d_norm);
+    d_norm = nullptr;
+    launched = true;
+  } while (next < count);
+  return launched ? finish_launch() : ZC_OK;
+}
+
+int zt_adamw(const struct zt_adamw_form* form, const void* d_grad, const double* d_slots, float* d_param, float* d_m, float* d_v, void* d_half,
+             float* d_norm, void* stream) {
+  if (!form) return ZC_ERR_NULL;
+  if (!known_dtype(form->grad_dtype) || (d_half && form->half_dtype != ZC_BF16 && form->half_dtype != ZC_F16)) return ZC_ERR_DTYPE;
+  const auto within = [](double v) { return v >= 0.0 && v <= (double)FLT_MAX; };
+  if (form->step < 1 || !within(form->lr) || !within(form->eps) || !within(form->weight_decay) || !(form->beta1 >= 0.0 && form->beta1 < 1.0) ||
+      !(form->beta2 >= 0.0 && form->beta2 < 1.0) || !good_scale(form->scale) || (d_slots && !good_max_norm(form->max_norm)))
+    return ZC_ERR_ARG;
+  if (form->n > kMaxValues) return ZC_ERR_SIZE;
+  if (form->n != 0 && (!d_grad || !d_param || !d_m || !d_v)) return ZC_ERR_NULL;
+  if (!d_slots && d_norm) return ZC_ERR_NULL;
+  if (!aligned(d_slots, 16) || !aligned(d_norm, 4) || !aligned(d_grad, dtype_bytes(form->grad_dtype)) || !aligned(d_param, 4) || !aligned(d_m, 4) ||
+      !aligned(d_v, 4) || !aligned(d_half, 2))
+    return ZC_ERR_ALIGN;
+  if (form->n == 0) return d_norm ? zt_norm(d_slots, form->scale, d_norm, stream) : ZC_OK;
+  AdamwArgs a;
+  a.grad = static_cast<const char*>(d_grad);
+  a.slots = d_slots;
+  a.param = d_param;
+  a.m = d_m;
+  a.v = d_v;
+  a.half = static_cast<char*>(d_half);
+  a.norm_out = d_norm;
+  a.n = form->n;
+  a.lr = (float)form->lr;
+  a.beta1 = (float)form->beta1;
+  a.rest1 = (float)(1.0 - form->beta1);
+  a.beta2 = (float)form->beta2;
+  a.rest2 = (float)(1.0 - form->beta2);
+  a.eps = (float)form->eps;
+  a.weight_decay = (float)form->weight_decay;
+  a.correct1 = (float)(1.0 / (1.0 - pow(form->beta1, (double)form->step)));
+  a.correct2 = (float)(1.0 / (1.0 - pow(form->beta2, (double)form->step)));
+  a.scale = form->scale;
+  a.max_norm = form->max_norm;
+  const size_t groups = (form->n + 4 * kThreads - 1) / (4 * kThreads);
+  const dim3 grid((unsigned)(groups < kMostGroups ? groups : kMostGroups));
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const int dh = d_half ? form->half_dtype : ZC_F32;
+#define LAUNCH(DG)                                                                                              \
+  do {                                                                                                          \
+    if (dh == ZC_F32) hipLaunchKernelGGL((adamw_kernel<DG, kF32>), grid, dim3(kThreads), 0, s, a);              \
+    else if (dh == ZC_BF16) hipLaunchKernelGGL((adamw_kernel<DG, kBF16>), grid, dim3(kThreads), 0, s, a);       \
+    else hipLaunchKernelGGL((adamw_kernel<DG, kF16>), grid, dim3(kThreads), 0, s, a);                           \
+  } while (0)
+  if (form->grad_dtype == ZC_F32) LAUNCH(kF32);
+  else if (form->grad_dtype == ZC_BF16) LAUNCH(kBF16);
+  else LAUNCH(kF16);
+#undef LAUNCH
+  return finish_launch();
+}
+
+}  // extern "C"
