@@ -29,10 +29,13 @@ struct Raw {
   uint32_t w[kWords];
 
   // All of them, `at` bytes behind `base`; base is the same in every lane, which leaves the addressing to the load itself.
+  // ONCE: what is not read or written again soon (nontemporal) leaves the caches to what is.
+  template <bool ONCE = false>
   __device__ __forceinline__ void load(const char* base, uint32_t at) {
 #pragma unroll
     for (int i = 0; i < kWords / kPart; ++i) {
-      const part_t v = reinterpret_cast<const ZT_GLOBAL part_at_t*>((const ZT_GLOBAL char*)base + at)[i];
+      const ZT_GLOBAL part_at_t* p = reinterpret_cast<const ZT_GLOBAL part_at_t*>((const ZT_GLOBAL char*)base + at) + i;
+      const part_t v = ONCE ? __builtin_nontemporal_load(p) : *p;
 #pragma unroll
       for (int j = 0; j < kPart; ++j) w[i * kPart + j] = v[j];
     }
@@ -55,13 +58,16 @@ struct Raw {
       }
     }
   }
+  template <bool ONCE = false>
   __device__ __forceinline__ void store(char* base, uint32_t at) const {
 #pragma unroll
     for (int i = 0; i < kWords / kPart; ++i) {
       part_t v;
 #pragma unroll
       for (int j = 0; j < kPart; ++j) v[j] = w[i * kPart + j];
-      reinterpret_cast<ZT_GLOBAL part_at_t*>((ZT_GLOBAL char*)base + at)[i] = v;
+      ZT_GLOBAL part_at_t* p = reinterpret_cast<ZT_GLOBAL part_at_t*>((ZT_GLOBAL char*)base + at) + i;
+      if constexpr (ONCE) __builtin_nontemporal_store(part_at_t(v), p);
+      else *p = v;
     }
   }
   __device__ __forceinline__ void store(char* base, uint32_t at, int valid) const {

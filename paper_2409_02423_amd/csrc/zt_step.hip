@@ -17,7 +17,8 @@ namespace {
 
 constexpr int kMostTensors = 112;      // of one launch: 3.4 KB of its arguments
 constexpr int kChunk = 8192;           // values
-constexpr size_t kMostChunks = (size_t)1 << 31;   // of one launch
+constexpr size_t kMostChunks = (size_t)1 << 31;   // of one list
+constexpr size_t kMostGroups = (size_t)1 << 23;   // of one launch: a grid has fewer than 2^32 lanes
 constexpr size_t kMaxValues = (size_t)1 << 40;    // of a tensor
 
 struct TensorList {
@@ -45,15 +46,16 @@ __device__ __forceinline__ int tensor_of(const TensorList& list, uint32_t chunk)
 
 constexpr int kSumThreads = 1024;
 
-template <int DT>
-__device__ __forceinline__ void add_squares(const char* p, size_t left, double (&sum)[2]) {
+// Squares of one chunk, of which `left` values are left in the tensor (FULL: all of them).
+template <int DT, bool FULL>
+__device__ __forceinline__ void add_chunk(const char* p, int left, double (&sum)[2]) {
   constexpr int kSteps = kChunk / kSumThreads / kVec<DT>;
   Raw<DT> raw[kSteps];
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     const int at = (threadIdx.x + i * kSumThreads) * kVec<DT>;
-    const int valid = left >= (size_t)kChunk ? kVec<DT> : (int)left - at;
-    raw[i].load(p, at * kBytes<DT>, valid);
+    if constexpr (FULL) raw[i].load(p, at * kBytes<DT>);
+    else raw[i].load(p, at * kBytes<DT>, left - at);
   }
 #pragma unroll
   for (int i = 0; i < kSteps; ++i)
@@ -64,19 +66,30 @@ __device__ __forceinline__ void add_squares(const char* p, size_t left, double (
     }
 }
 
+// Squares of this workgroup's chunks of one tensor: `chunk` and every gridDim.x-th after it, before `end`.
+template <int DT>
+__device__ __forceinline__ uint32_t add_tensor(const char* p, size_t n, uint32_t first, uint32_t end, uint32_t chunk, double (&sum)[2]) {
+  for (; chunk < end; chunk += gridDim.x) {
+    const size_t at = (size_t)(chunk - first) * kChunk;
+    if (n - at >= (size_t)kChunk) add_chunk<DT, true>(p + at * kBytes<DT>, 0, sum);
+    else add_chunk<DT, false>(p + at * kBytes<DT>, (int)(n - at), sum);
+  }
+  return chunk;
+}
+
 __global__ void __launch_bounds__(kSumThreads) sum_squares_kernel(TensorList list, int accumulate, double* slots) {
   __shared__ double buffer[1][kMostWaves];
   double sum[2] = {0.0, 0.0};
   const uint32_t chunks = list.first[list.count];
-  for (uint32_t chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
+  for (uint32_t chunk = blockIdx.x; chunk < chunks;) {
     const int t = tensor_of(list, chunk);
-    const size_t at = (size_t)(chunk - list.first[t]) * kChunk;
-    const size_t left = list.n[t] - at;
     const char* p = list.in[t];
+    const size_t n = list.n[t];
+    const uint32_t first = list.first[t], end = list.first[t + 1];
     switch (list.in_type[t]) {
-      case kF32: add_squares<kF32>(p + at * 4, left, sum); break;
-      case kBF16: add_squares<kBF16>(p + at * 2, left, sum); break;
-      default: add_squares<kF16>(p + at * 2, left, sum); break;
+      case kF32: chunk = add_tensor<kF32>(p, n, first, end, chunk, sum); break;
+      case kBF16: chunk = add_tensor<kBF16>(p, n, first, end, chunk, sum); break;
+      default: chunk = add_tensor<kF16>(p, n, first, end, chunk, sum); break;
     }
   }
   double total[1] = {sum[0] + sum[1]};
@@ -110,55 +123,66 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const double* slots, flo
 
 // ---- clipping --------------------------------------------------------------------------
 
-template <int DI, int DO>
-__device__ __forceinline__ void scale_chunk(const char* in, char* out, size_t left, float factor) {
-  constexpr int kN = DI == kF32 && DO == kF32 ? 4 : 8;   // values per lane and step
+// One chunk: its loads go out first, and the factor is made while they are under way.
+template <int DI, int DO, bool FULL, class F>
+__device__ __forceinline__ void scale_chunk(const char* in, char* out, int left, F&& make_factor) {
+  constexpr int kN = DI == kF32 || DO == kF32 ? 4 : 8;   // values per lane and step: 16 bytes of the wider type
   constexpr int kSteps = kChunk / kThreads / kN;
   Raw<DI, kN> raw[kSteps];
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     const int at = (threadIdx.x + i * kThreads) * kN;
-    const int valid = left >= (size_t)kChunk ? kN : (int)left - at;
-    raw[i].load(in, at * kBytes<DI>, valid);
+    if constexpr (FULL) raw[i].template load<true>(in, at * kBytes<DI>);
+    else raw[i].load(in, at * kBytes<DI>, left - at);
   }
+  const float factor = make_factor();
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     const int at = (threadIdx.x + i * kThreads) * kN;
-    const int valid = left >= (size_t)kChunk ? kN : (int)left - at;
     float v[kN];
     raw[i].unpack(v);
 #pragma unroll
     for (int j = 0; j < kN; ++j) v[j] *= factor;
     Raw<DO, kN> result;
     result.pack(v);
-    result.store(out, at * kBytes<DO>, valid);
+    if constexpr (FULL) result.template store<true>(out, at * kBytes<DO>);
+    else result.store(out, at * kBytes<DO>, left - at);
   }
 }
+template <int DI, int DO, class F>
+__device__ __forceinline__ void scale_chunk(const char* in, char* out, size_t at, size_t n, F&& make_factor) {
+  in += at * kBytes<DI>;
+  out += at * kBytes<DO>;
+  if (n - at >= (size_t)kChunk) scale_chunk<DI, DO, true>(in, out, 0, make_factor);
+  else scale_chunk<DI, DO, false>(in, out, (int)(n - at), make_factor);
+}
 
-__global__ void __launch_bounds__(kThreads) clip_kernel(TensorList list, const double* slots, float scale, float max_norm, float* norm_out) {
+__global__ void __launch_bounds__(kThreads) clip_kernel(TensorList list, uint32_t from, const double* slots, float scale, float max_norm, float* norm_out) {
   __shared__ double buffer[1][kMostWaves];
-  const double norm = (double)scale * sqrt(slots_total(slots, buffer));
-  if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) norm_out[0] = (float)norm;
-  const float factor = clip_factor(norm, scale, max_norm);
-  const uint32_t chunks = list.first[list.count];
-  for (uint32_t chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
-    const int t = tensor_of(list, chunk);
-    const size_t at = (size_t)(chunk - list.first[t]) * kChunk;
-    const size_t left = list.n[t] - at;
-    const int di = list.in_type[t], dt = list.out_type[t];
-    const char* in = list.in[t] + at * (di == kF32 ? 4 : 2);
-    char* out = list.out[t] + at * (dt == kF32 ? 4 : 2);
-    switch (di * 3 + dt) {
-      case kF32 * 3 + kF32: scale_chunk<kF32, kF32>(in, out, left, factor); break;
-      case kF32 * 3 + kBF16: scale_chunk<kF32, kBF16>(in, out, left, factor); break;
-      case kF32 * 3 + kF16: scale_chunk<kF32, kF16>(in, out, left, factor); break;
-      case kBF16 * 3 + kF32: scale_chunk<kBF16, kF32>(in, out, left, factor); break;
-      case kBF16 * 3 + kBF16: scale_chunk<kBF16, kBF16>(in, out, left, factor); break;
-      case kBF16 * 3 + kF16: scale_chunk<kBF16, kF16>(in, out, left, factor); break;
-      case kF16 * 3 + kF32: scale_chunk<kF16, kF32>(in, out, left, factor); break;
-      case kF16 * 3 + kBF16: scale_chunk<kF16, kBF16>(in, out, left, factor); break;
-      default: scale_chunk<kF16, kF16>(in, out, left, factor); break;
-    }
+  const auto make_factor = [&] {
+    const double norm = (double)scale * sqrt(slots_total(slots, buffer));
+    if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) norm_out[0] = (float)norm;
+    return clip_factor(norm, scale, max_norm);
+  };
+  const uint32_t chunk = from + blockIdx.x;
+  if (chunk >= list.first[list.count]) {   // an empty list: the norm alone
+    make_factor();
+    return;
+  }
+  const int t = tensor_of(list, chunk);
+  const size_t at = (size_t)(chunk - list.first[t]) * kChunk, n = list.n[t];
+  const char* in = list.in[t];
+  char* out = list.out[t];
+  switch (list.in_type[t] * 3 + list.out_type[t]) {
+    case kF32 * 3 + kF32: scale_chunk<kF32, kF32>(in, out, at, n, make_factor); break;
+    case kF32 * 3 + kBF16: scale_chunk<kF32, kBF16>(in, out, at, n, make_factor); break;
+    case kF32 * 3 + kF16: scale_chunk<kF32, kF16>(in, out, at, n, make_factor); break;
+    case kBF16 * 3 + kF32: scale_chunk<kBF16, kF32>(in, out, at, n, make_factor); break;
+    case kBF16 * 3 + kBF16: scale_chunk<kBF16, kBF16>(in, out, at, n, make_factor); break;
+    case kBF16 * 3 + kF16: scale_chunk<kBF16, kF16>(in, out, at, n, make_factor); break;
+    case kF16 * 3 + kF32: scale_chunk<kF16, kF32>(in, out, at, n, make_factor); break;
+    case kF16 * 3 + kBF16: scale_chunk<kF16, kBF16>(in, out, at, n, make_factor); break;
+    default: scale_chunk<kF16, kF16>(in, out, at, n, make_factor); break;
   }
 }
 
@@ -175,11 +199,28 @@ struct AdamwArgs {
   float scale, max_norm;
 };
 
-// DG: the gradients' type; DH: that of the copy, kF32 for none.
-template <int DG, int DH>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(AdamwArgs a) {
-  __shared__ double buffer[1][kMostWaves];
+constexpr int kAdamwTile = kThreads * 4;   // four values per lane
+
+template <int DG, int DH, bool FULL>
+__device__ __forceinline__ void adamw_tile(const AdamwArgs& a, size_t start, int left, double (&buffer)[1][kMostWaves]) {
   constexpr int kN = 4;
+  const char* grad = a.grad + start * kBytes<DG>;
+  char *param = reinterpret_cast<char*>(a.param + start), *first = reinterpret_cast<char*>(a.m + start), *second = reinterpret_cast<char*>(a.v + start);
+  const int at = threadIdx.x * kN;
+  Raw<DG, kN> rg;
+  Raw<kF32, kN> rp, rm, rv;
+  if constexpr (FULL) {
+    rg.template load<true>(grad, at * kBytes<DG>);
+    rp.template load<true>(param, at * 4);
+    rm.template load<true>(first, at * 4);
+    rv.template load<true>(second, at * 4);
+  } else {
+    rg.load(grad, at * kBytes<DG>, left - at);
+    rp.load(param, at * 4, left - at);
+    rm.load(first, at * 4, left - at);
+    rv.load(second, at * 4, left - at);
+  }
+  // the factor, while the loads are under way
   float factor = a.scale;
   bool finite = true;
   if (a.slots) {
@@ -188,51 +229,51 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(AdamwArgs a) {
     factor = clip_factor(norm, a.scale, a.max_norm);
     finite = norm < __builtin_inf();
   }
-  constexpr int kTile = kThreads * kN;
-  const size_t tiles = (a.n + kTile - 1) / kTile;
-  for (size_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-    const size_t start = tile * kTile, left = a.n - start;
-    const uint32_t at = threadIdx.x * kN;
-    const int valid = left >= (size_t)kTile ? kN : (int)left - (int)at;
-    char *param = reinterpret_cast<char*>(a.param + start), *first = reinterpret_cast<char*>(a.m + start), *second = reinterpret_cast<char*>(a.v + start);
-    Raw<DG, kN> rg;
-    Raw<kF32, kN> rp, rm, rv;
-    rg.load(a.grad + start * kBytes<DG>, at * kBytes<DG>, valid);
-    rp.load(param, at * 4, valid);
-    rm.load(first, at * 4, valid);
-    rv.load(second, at * 4, valid);
-    float g[kN], p[kN], m[kN], v[kN];
-    rg.unpack(g);
-    rp.unpack(p);
-    rm.unpack(m);
-    rv.unpack(v);
-    if (finite) {
+  float g[kN], p[kN], m[kN], v[kN];
+  rg.unpack(g);
+  rp.unpack(p);
+  rm.unpack(m);
+  rv.unpack(v);
+  if (finite) {
 #pragma unroll
-      for (int j = 0; j < kN; ++j) {
-        const float gc = g[j] * factor;
-        m[j] = fmaf(a.beta1, m[j], a.rest1 * gc);
-        v[j] = fmaf(a.beta2, v[j], a.rest2 * (gc * gc));
-        const float update = (m[j] * a.correct1) / (sqrtf(v[j] * a.correct2) + a.eps);
-        p[j] = fmaf(-a.lr, fmaf(a.weight_decay, p[j], update), p[j]);
-      }
-      rp.pack(p);
-      rm.pack(m);
-      rv.pack(v);
-      rp.store(param, at * 4, valid);
-      rm.store(first, at * 4, valid);
-      rv.store(second, at * 4, valid);
+    for (int j = 0; j < kN; ++j) {
+      const float gc = g[j] * factor;
+      m[j] = fmaf(a.beta1, m[j], a.rest1 * gc);
+      v[j] = fmaf(a.beta2, v[j], a.rest2 * (gc * gc));
+      const float update = (m[j] * a.correct1) / (sqrtf(v[j] * a.correct2) + a.eps);
+      p[j] = fmaf(-a.lr, fmaf(a.weight_decay, p[j], update), p[j]);
     }
-    if constexpr (DH != kF32) {
-      Raw<DH, kN> rh;
-      rh.pack(p);
-      rh.store(a.half + start * 2, at * 2, valid);
+    rp.pack(p);
+    rm.pack(m);
+    rv.pack(v);
+    if constexpr (FULL) {
+      rp.template store<true>(param, at * 4);
+      rm.template store<true>(first, at * 4);
+      rv.template store<true>(second, at * 4);
+    } else {
+      rp.store(param, at * 4, left - at);
+      rm.store(first, at * 4, left - at);
+      rv.store(second, at * 4, left - at);
     }
+  }
+  if constexpr (DH != kF32) {
+    Raw<DH, kN> rh;
+    rh.pack(p);
+    if constexpr (FULL) rh.template store<true>(a.half + start * 2, at * 2);
+    else rh.store(a.half + start * 2, at * 2, left - at);
   }
 }
 
-// ---- host ------------------------------------------------------------------------------
+// One tile for each workgroup.  DG: the gradients' type; DH: that of the copy, kF32 for none.
+template <int DG, int DH>
+__global__ void __launch_bounds__(kThreads) adamw_kernel(AdamwArgs a) {
+  __shared__ double buffer[1][kMostWaves];
+  const size_t start = (size_t)blockIdx.x * kAdamwTile, left = a.n - start;
+  if (left >= (size_t)kAdamwTile) adamw_tile<DG, DH, true>(a, start, 0, buffer);
+  else adamw_tile<DG, DH, false>(a, start, (int)left, buffer);
+}
 
-constexpr unsigned kMostGroups = 2048;   // of the second pass: eight per CU
+// ---- host ------------------------------------------------------------------------------
 
 // Checks a list of tensors; `out` NULL for the sum of squares.
 int check_list(const void* const* d_in, const size_t* n, const int* in_type, void* const* d_out, const int* out_type, int count, bool writes) {
@@ -317,11 +358,13 @@ int zt_clip(const void* const* d_in, const size_t* n, const int* dtype_in, void*
   bool launched = false;
   do {
     next = fill_list(list, d_in, n, dtype_in, d_out, dtype_out, count, next);
-    const uint32_t chunks = list.first[list.count];
+    const size_t chunks = list.first[list.count];
     if (chunks == 0 && !d_norm) break;
-    const unsigned groups = chunks == 0 ? 1 : chunks < kMostGroups ? chunks : kMostGroups;
-    hipLaunchKernelGGL(clip_kernel, dim3(groups), dim3(kThreads), 0, static_cast<hipStream_t>(stream), list, d_slots, scale, max_norm, d_norm);
-    d_norm = nullptr;
+    for (size_t from = 0; from < chunks || from == 0; from += kMostGroups) {
+      const size_t groups = chunks == 0 ? 1 : chunks - from < kMostGroups ? chunks - from : kMostGroups;
+      hipLaunchKernelGGL(clip_kernel, dim3((unsigned)groups), dim3(kThreads), 0, static_cast<hipStream_t>(stream), list, (uint32_t)from, d_slots, scale, max_norm, d_norm);
+      d_norm = nullptr;
+    }
     launched = true;
   } while (next < count);
   return launched ? finish_launch() : ZC_OK;
@@ -350,7 +393,6 @@ int zt_adamw(const struct zt_adamw_form* form, const void* d_grad, const double*
   a.v = d_v;
   a.half = static_cast<char*>(d_half);
   a.norm_out = d_norm;
-  a.n = form->n;
   a.lr = (float)form->lr;
   a.beta1 = (float)form->beta1;
   a.rest1 = (float)(1.0 - form->beta1);
@@ -362,20 +404,28 @@ int zt_adamw(const struct zt_adamw_form* form, const void* d_grad, const double*
   a.correct2 = (float)(1.0 / (1.0 - pow(form->beta2, (double)form->step)));
   a.scale = form->scale;
   a.max_norm = form->max_norm;
-  const size_t groups = (form->n + 4 * kThreads - 1) / (4 * kThreads);
-  const dim3 grid((unsigned)(groups < kMostGroups ? groups : kMostGroups));
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const int dh = d_half ? form->half_dtype : ZC_F32;
-#define LAUNCH(DG)                                                                                              \
-  do {                                                                                                          \
-    if (dh == ZC_F32) hipLaunchKernelGGL((adamw_kernel<DG, kF32>), grid, dim3(kThreads), 0, s, a);              \
-    else if (dh == ZC_BF16) hipLaunchKernelGGL((adamw_kernel<DG, kBF16>), grid, dim3(kThreads), 0, s, a);       \
-    else hipLaunchKernelGGL((adamw_kernel<DG, kF16>), grid, dim3(kThreads), 0, s, a);                           \
+  for (size_t left = form->n; left != 0; left -= a.n) {
+    a.n = left < kMostGroups * kAdamwTile ? left : kMostGroups * kAdamwTile;
+    const dim3 grid((unsigned)((a.n + kAdamwTile - 1) / kAdamwTile));
+#define LAUNCH(DG)                                                                                         \
+  do {                                                                                                     \
+    if (dh == ZC_F32) hipLaunchKernelGGL((adamw_kernel<DG, kF32>), grid, dim3(kThreads), 0, s, a);         \
+    else if (dh == ZC_BF16) hipLaunchKernelGGL((adamw_kernel<DG, kBF16>), grid, dim3(kThreads), 0, s, a);  \
+    else hipLaunchKernelGGL((adamw_kernel<DG, kF16>), grid, dim3(kThreads), 0, s, a);                      \
   } while (0)
-  if (form->grad_dtype == ZC_F32) LAUNCH(kF32);
-  else if (form->grad_dtype == ZC_BF16) LAUNCH(kBF16);
-  else LAUNCH(kF16);
+    if (form->grad_dtype == ZC_F32) LAUNCH(kF32);
+    else if (form->grad_dtype == ZC_BF16) LAUNCH(kBF16);
+    else LAUNCH(kF16);
 #undef LAUNCH
+    a.grad += a.n * dtype_bytes(form->grad_dtype);
+    a.param += a.n;
+    a.m += a.n;
+    a.v += a.n;
+    if (a.half) a.half += a.n * 2;
+    a.norm_out = nullptr;
+  }
   return finish_launch();
 }
 
