@@ -6,6 +6,7 @@ call allocates (outputs that are not passed, workspaces) belongs to the stream i
 library cannot be loaded, every call raises.
 """
 import ctypes
+from array import array
 
 import torch
 
@@ -71,76 +72,92 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _on_device(t, what, device=None):
+# A call's checks take as long as a small kernel does, so what is right is seen with few questions (each some 0.1 us), and what
+# is wrong is asked again for its name.
+
+
+def _current(t, what):
+    """The device of a tensor, by number, which is the current one's."""
     if not (isinstance(t, torch.Tensor) and t.is_cuda):
         raise TypeError("%s must be a CUDA tensor" % what)
-    if t.device.index != torch.cuda.current_device() if device is None else t.device != device:
-        raise ValueError("%s must be on %s" % (what, "the current device" if device is None else device))
+    device = t.get_device()
+    if device != torch.cuda.current_device():
+        raise ValueError("%s must be on the current device" % what)
+    return device
 
 
-def _flat(t, what, dtype=None, device=None):
-    """A contiguous tensor's pointer."""
-    _on_device(t, what, device)
-    if not t.is_contiguous() or (t.dtype not in _DTYPES if dtype is None else t.dtype != dtype):
-        raise TypeError("%s must be contiguous, of dtype %s" % (what, dtype or "float32, bfloat16 or float16"))
+def _refuse(t, what, dtype, device):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+        raise TypeError("%s must be a CUDA tensor" % what)
+    if t.get_device() != device:
+        raise ValueError("%s must be on device %d" % (what, device))
+    if t.dtype != dtype:
+        raise TypeError("%s must be of dtype %s" % (what, dtype))
+
+
+def _flat(t, what, dtype, device, count):
+    """Pointer of a contiguous tensor of `count` values."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device and t.is_contiguous() and t.numel() == count):
+        _refuse(t, what, dtype, device)
+        if not t.is_contiguous():
+            raise TypeError("%s must be contiguous" % what)
+        raise ValueError("%s must hold %d values" % (what, count))
     return t.data_ptr()
 
 
 # ---- residual join and norms ---------------------------------------------------------
 
 
-def _rows_of(t, like, what):
-    """Pointer of a tensor of like's shape and type whose rows are apart by one stride, and that stride."""
-    _on_device(t, what, like.device)
-    if t.dtype != like.dtype:
-        raise TypeError("%s must be of dtype %s" % (what, like.dtype))
-    if t.shape != like.shape:
-        raise ValueError("%s must have shape %s" % (what, tuple(like.shape)))
-    if t.is_contiguous():
-        return t.data_ptr(), like.shape[-1]
-    if t.dim() != 2:
-        try:
-            t = t.view(-1, t.shape[-1])
-        except RuntimeError:
-            raise TypeError("%s: the distance from row to row must be the same everywhere" % what) from None
-    if t.shape[1] > 1 and t.stride(1) != 1:
-        raise TypeError("%s: a row's values must lie next to one another" % what)
-    if t.shape[0] > 1 and t.stride(0) == 0:
-        raise TypeError("%s: rows that are all the same one (an expanded tensor) are not taken; make it contiguous" % what)
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else like.shape[-1]
+class _Rows:
+    """What the activations of a call have in common: shape, type, device, and the form that the library is given."""
 
+    def __init__(self, like, kind, post, d_gate, residual_scale, eps):
+        self.device = _current(like, "activations")
+        self.dtype, self.shape = like.dtype, like.shape
+        code = _DTYPES.get(self.dtype)
+        if code is None or not self.shape:
+            raise TypeError("activations must be float32, bfloat16 or float16 tensors of [..., cols]")
+        self.cols = cols = self.shape[-1]
+        self.form = Residual(like.numel() // cols if cols else 0, cols, code, kind, 1 if post else 0, ZT_GATE_NONE, residual_scale, eps)
+        self.gate = None
+        if d_gate is not None:
+            if isinstance(d_gate, torch.Tensor) and d_gate.dim() == 1:
+                self.form.gate, self.gate = ZT_GATE_CHANNEL, self.channels(d_gate, "d_gate")
+            else:
+                self.form.gate, self.gate = ZT_GATE_FULL, self.rows(d_gate, "gate")
 
-def _channels(t, like, what):
-    if t is None:
-        return None
-    pointer = _flat(t, what, like.dtype, like.device)
-    if t.numel() != like.shape[-1]:
-        raise ValueError("%s must hold %d values" % (what, like.shape[-1]))
-    return pointer
+    def rows(self, t, name):
+        """Pointer of a tensor of the common shape and type whose rows are apart by one stride, which the form is told."""
+        if isinstance(t, torch.Tensor) and t.is_contiguous() and t.dtype is self.dtype and t.get_device() == self.device and t.shape == self.shape:
+            return t.data_ptr()      # stride 0 in the form: cols
+        what = "d_" + name
+        _refuse(t, what, self.dtype, self.device)
+        if t.shape != self.shape:
+            raise ValueError("%s must have shape %s" % (what, tuple(self.shape)))
+        if t.dim() != 2:
+            try:
+                t = t.view(-1, self.cols)
+            except RuntimeError:
+                raise TypeError("%s: the distance from row to row must be the same everywhere" % what) from None
+        if t.shape[1] > 1 and t.stride(1) != 1:
+            raise TypeError("%s: a row's values must lie next to one another" % what)
+        if t.shape[0] > 1:
+            if t.stride(0) == 0:
+                raise TypeError("%s: rows that are all the same one (an expanded tensor) are not taken; make it contiguous" % what)
+            setattr(self.form, "stride_" + name, t.stride(0))
+        return t.data_ptr()
 
+    def channels(self, t, what):
+        return None if t is None else _flat(t, what, self.dtype, self.device, self.cols)
 
-def _form(like, kind, post, d_gate, residual_scale, eps):
-    if not (isinstance(like, torch.Tensor) and like.is_cuda):
-        raise TypeError("activations must be CUDA tensors")
-    _on_device(like, "activations")
-    if like.dtype not in _DTYPES or like.dim() == 0:
-        raise TypeError("activations must be float32, bfloat16 or float16 tensors of [..., cols]")
-    cols = like.shape[-1]
-    f = Residual(rows=like.numel() // cols if cols else 0, cols=cols, dtype=_DTYPES[like.dtype], kind=kind, post=1 if post else 0,
-                 residual_scale=residual_scale, eps=eps)
-    gate = None
-    if d_gate is not None:
-        if d_gate.dim() == 1:
-            f.gate, gate = ZT_GATE_CHANNEL, _channels(d_gate, like, "d_gate")
-        else:
-            f.gate = ZT_GATE_FULL
-            gate, f.stride_gate = _rows_of(d_gate, like, "d_gate")
-    return f, gate
+    def weights(self, post, pre_weight, pre_bias, post_weight, post_bias):
+        if not post and (post_weight is not None or post_bias is not None):
+            raise ValueError("post_weight and post_bias belong to a norm after the block: post=True")
+        return (self.channels(pre_weight, "pre_weight"), self.channels(pre_bias, "pre_bias"), self.channels(post_weight, "post_weight"),
+                self.channels(post_bias, "post_bias"))
 
-
-def _without_post(post, post_weight, post_bias):
-    if not post and (post_weight is not None or post_bias is not None):
-        raise ValueError("post_weight and post_bias belong to a norm after the block: post=True")
+    def empty(self, stream):
+        return _empty(self.shape, self.dtype, self.device, stream)
 
 
 def zt_residual_norm(d_x, d_b=None, kind=ZT_RMS, pre_weight=None, pre_bias=None, post=False, post_weight=None, post_bias=None, d_gate=None,
@@ -149,27 +166,16 @@ def zt_residual_norm(d_x, d_b=None, kind=ZT_RMS, pre_weight=None, pre_bias=None,
 
     d_x and d_b are [..., cols]; d_gate is None, [cols] or of their shape.  d_stats, an fp32 tensor of rows x 4, gets what
     zt_residual_norm_backward needs.  want_y=False: y is not stored (and returned as None)."""
-    f, gate = _form(d_x, kind, post, d_gate, residual_scale, eps)
-    _without_post(post, post_weight, post_bias)
-    x, f.stride_x = _rows_of(d_x, d_x, "d_x")
-    b = y = None
-    if d_b is not None:
-        b, f.stride_b = _rows_of(d_b, d_x, "d_b")
+    r = _Rows(d_x, kind, post, d_gate, residual_scale, eps)
+    weights = r.weights(post, pre_weight, pre_bias, post_weight, post_bias)
     if d_y is None and want_y:
-        d_y = _empty(d_x.shape, d_x.dtype, d_x.device, stream)
-    if d_y is not None:
-        y, f.stride_y = _rows_of(d_y, d_x, "d_y")
+        d_y = r.empty(stream)
     if d_h is None:
-        d_h = _empty(d_x.shape, d_x.dtype, d_x.device, stream)
-    h, f.stride_h = _rows_of(d_h, d_x, "d_h")
-    stats = None
-    if d_stats is not None:
-        stats = _flat(d_stats, "d_stats", torch.float32, d_x.device)
-        if d_stats.numel() != 4 * f.rows:
-            raise ValueError("d_stats must hold four floats for each of the %d rows" % f.rows)
-    _check(lib().zt_residual_norm(f, x, b, gate, _channels(pre_weight, d_x, "pre_weight"), _channels(pre_bias, d_x, "pre_bias"),
-                                  _channels(post_weight, d_x, "post_weight"), _channels(post_bias, d_x, "post_bias"), y, h, stats,
-                                  zc._stream_handle(stream)), "zt_residual_norm")
+        d_h = r.empty(stream)
+    x, b = r.rows(d_x, "x"), None if d_b is None else r.rows(d_b, "b")
+    y, h = None if d_y is None else r.rows(d_y, "y"), r.rows(d_h, "h")
+    stats = None if d_stats is None else _flat(d_stats, "d_stats", torch.float32, r.device, 4 * r.form.rows)
+    _check(lib().zt_residual_norm(r.form, x, b, r.gate, *weights, y, h, stats, zc._stream_handle(stream)), "zt_residual_norm")
     return d_y, d_h
 
 
@@ -178,83 +184,76 @@ def zt_residual_norm_backward(d_dy, d_dh, d_y, d_b, d_stats, kind=ZT_RMS, pre_we
     """The gradients of zt_residual_norm from those of y (None for zero) and h, as a dict: "x", "b" and a full "gate" in the
     activations' type; "pre_weight", "pre_bias", "post_weight", "post_bias" and a channel "gate" in fp32; None for what the
     forward call did not have.  d_y is y as it was stored; the other arguments are the forward call's."""
-    f, gate = _form(d_dh, kind, post, d_gate, residual_scale, 0.0)
-    _without_post(post, post_weight, post_bias)
-    device, cols = d_dh.device, d_dh.shape[-1]
-    dh, f.stride_dh = _rows_of(d_dh, d_dh, "d_dh")
-    y, f.stride_y = _rows_of(d_y, d_dh, "d_y")
-    dy = b = db = None
-    if d_dy is not None:
-        dy, f.stride_dy = _rows_of(d_dy, d_dh, "d_dy")
-    if d_dx is None:
-        d_dx = _empty(d_dh.shape, d_dh.dtype, device, stream)
-    dx, f.stride_dx = _rows_of(d_dx, d_dh, "d_dx")
-    if d_b is not None:
-        b, f.stride_b = _rows_of(d_b, d_dh, "d_b")
-        if d_db is None:
-            d_db = _empty(d_dh.shape, d_dh.dtype, device, stream)
-        db, f.stride_db = _rows_of(d_db, d_dh, "d_db")
-    elif d_db is not None:
+    r = _Rows(d_dh, kind, post, d_gate, residual_scale, 0.0)
+    pre_w, _, post_w, post_c = r.weights(post, pre_weight, pre_bias, post_weight, post_bias)
+    if d_b is None and d_db is not None:
         raise ValueError("d_db without d_b")
-    stats = _flat(d_stats, "d_stats", torch.float32, device)
-    if d_stats.numel() != 4 * f.rows:
-        raise ValueError("d_stats must hold four floats for each of the %d rows" % f.rows)
-    pre_w, post_w, post_c = _channels(pre_weight, d_dh, "pre_weight"), _channels(post_weight, d_dh, "post_weight"), _channels(post_bias, d_dh, "post_bias")
-    _channels(pre_bias, d_dh, "pre_bias")
-    out = {"x": d_dx, "b": d_db, "gate": None}
-    if f.gate == ZT_GATE_FULL:
-        out["gate"] = _empty(d_dh.shape, d_dh.dtype, device, stream)
-    # the sums over the rows, one allocation for all: it is a bucket of fp32 gradients
-    names = [n for n, t in (("pre_weight", pre_weight), ("pre_bias", pre_bias), ("post_weight", post_weight), ("post_bias", post_bias)) if t is not None]
-    if f.gate == ZT_GATE_CHANNEL:
-        names.append("gate")
-    sums = _empty((len(names), cols), torch.float32, device, stream)
-    for n in ("pre_weight", "pre_bias", "post_weight", "post_bias"):
-        out[n] = None
-    for i, n in enumerate(names):
-        out[n] = sums[i]
-    work = _empty(int(lib().zt_residual_work_bytes(f)), torch.uint8, device, stream)
-
-    def pointer(name):
-        return None if out[name] is None else out[name].data_ptr()
-
-    _check(lib().zt_residual_norm_backward(f, dy, dh, y, b, gate, pre_w, post_w, post_c, stats, dx, db, pointer("gate"), pointer("pre_weight"),
-                                           pointer("pre_bias"), pointer("post_weight"), pointer("post_bias"), work.data_ptr(), work.numel(),
-                                           zc._stream_handle(stream)), "zt_residual_norm_backward")
+    if d_dx is None:
+        d_dx = r.empty(stream)
+    if d_db is None and d_b is not None:
+        d_db = r.empty(stream)
+    full, channel = r.form.gate == ZT_GATE_FULL, r.form.gate == ZT_GATE_CHANNEL
+    dgate = r.empty(stream) if full else None
+    # the sums over the rows lie behind one another: a bucket of fp32 gradients
+    wanted = (pre_weight is not None, pre_bias is not None, post_weight is not None, post_bias is not None, channel)
+    sums = _empty((sum(wanted), r.cols), torch.float32, r.device, stream)
+    at, pointers = sums.data_ptr(), []
+    for w in wanted:
+        pointers.append(at if w else None)
+        at += 4 * r.cols if w else 0
+    dh, y, dx = r.rows(d_dh, "dh"), r.rows(d_y, "y"), r.rows(d_dx, "dx")
+    dy = None if d_dy is None else r.rows(d_dy, "dy")
+    b, db = (None, None) if d_b is None else (r.rows(d_b, "b"), r.rows(d_db, "db"))
+    stats = _flat(d_stats, "d_stats", torch.float32, r.device, 4 * r.form.rows)
+    L = lib()
+    size = L.zt_residual_work_bytes(r.form)
+    work = _empty(size, torch.uint8, r.device, stream)
+    _check(L.zt_residual_norm_backward(r.form, dy, dh, y, b, r.gate, pre_w, post_w, post_c, stats, dx, db, dgate.data_ptr() if full else pointers[4],
+                                       *pointers[:4], work.data_ptr(), size, zc._stream_handle(stream)), "zt_residual_norm_backward")
+    of = iter(sums.unbind(0))
+    out = {"x": d_dx, "b": d_db}
+    for name, w in zip(("pre_weight", "pre_bias", "post_weight", "post_bias", "gate"), wanted):
+        out[name] = next(of) if w else None
+    if full:
+        out["gate"] = dgate
     return out
 
 
 # ---- gradients -----------------------------------------------------------------------
 
 
-def _list(tensors, what):
+_data_ptr, _numel, _get_device, _is_contiguous = torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.get_device, torch.Tensor.is_contiguous
+
+
+class _List:
     """Pointers, lengths and types of a list of tensors as C arrays."""
-    count = len(tensors)
-    pointers, lengths, types = (ctypes.c_void_p * max(count, 1))(), (ctypes.c_size_t * max(count, 1))(), (ctypes.c_int * max(count, 1))()
-    device = None
-    for i, t in enumerate(tensors):
-        if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in _DTYPES and t.is_contiguous()):
+
+    def __init__(self, tensors, what):
+        self.count = len(tensors)
+        types = [_DTYPES.get(getattr(t, "dtype", None)) for t in tensors]
+        self.device = torch.cuda.current_device() if tensors and None not in types and tensors[0].is_cuda else None
+        if None in types or not all(map(_is_contiguous, tensors)) or (tensors and self.device is None):
             raise TypeError("%s must be contiguous CUDA tensors of dtype float32, bfloat16 or float16" % what)
-        if device is None:
-            device = torch.cuda.current_device()
-        if t.get_device() != device:
+        if tensors and set(map(_get_device, tensors)) != {self.device}:
             raise ValueError("%s must be on the current device" % what)
-        pointers[i], lengths[i], types[i] = t.data_ptr(), t.numel(), _DTYPES[t.dtype]
-    return pointers, lengths, types, count
+        self.pointers, self.lengths, self.types = array("Q", map(_data_ptr, tensors)), array("Q", map(_numel, tensors)), array("i", types)
+
+    def arguments(self):
+        return self.pointers.buffer_info()[0], self.lengths.buffer_info()[0], self.types.buffer_info()[0]
 
 
-def _check_slots(d_slots):
-    pointer = _flat(d_slots, "d_slots", torch.float64)
-    if d_slots.numel() != ZT_SLOTS:
-        raise ValueError("d_slots must hold %d values" % ZT_SLOTS)
-    return pointer
+def _slots(d_slots):
+    """Pointer and device of the partial sums of squares."""
+    device = _current(d_slots, "d_slots")
+    return _flat(d_slots, "d_slots", torch.float64, device, ZT_SLOTS), device
 
 
-def _check_norm(d_norm):
-    pointer = _flat(d_norm, "d_norm", torch.float32)
-    if d_norm.numel() < 1:
-        raise ValueError("d_norm must hold a value")
-    return pointer
+def _norm(d_norm, device, stream):
+    """The tensor that gets the norm, and its pointer."""
+    if d_norm is None:
+        d_norm = _empty(1, torch.float32, device, stream)
+        return d_norm, d_norm.data_ptr()
+    return d_norm, _flat(d_norm, "d_norm", torch.float32, device, 1)
 
 
 def zt_sum_squares(tensors, d_slots=None, accumulate=False, stream=None):
@@ -262,19 +261,21 @@ def zt_sum_squares(tensors, d_slots=None, accumulate=False, stream=None):
     add theirs up (an all-reduce of d_slots) before the norm is taken."""
     if accumulate and d_slots is None:
         raise ValueError("accumulate needs d_slots")
-    pointers, lengths, types, count = _list(list(tensors), "tensors")
+    tensors = _List(list(tensors), "tensors")
     if d_slots is None:
-        d_slots = _empty(ZT_SLOTS, torch.float64, "cuda", stream)
-    _check(lib().zt_sum_squares(pointers, lengths, types, count, 1 if accumulate else 0, _check_slots(d_slots), zc._stream_handle(stream)), "zt_sum_squares")
+        d_slots = _empty(ZT_SLOTS, torch.float64, "cuda" if tensors.device is None else tensors.device, stream)
+        slots = d_slots.data_ptr()
+    else:
+        slots, _ = _slots(d_slots)
+    _check(lib().zt_sum_squares(*tensors.arguments(), tensors.count, 1 if accumulate else 0, slots, zc._stream_handle(stream)), "zt_sum_squares")
     return d_slots
 
 
 def zt_norm(d_slots, scale=1.0, d_norm=None, stream=None):
     """scale * sqrt(the sum of squares): a tensor of one fp32 value."""
-    slots = _check_slots(d_slots)
-    if d_norm is None:
-        d_norm = _empty(1, torch.float32, d_slots.device, stream)
-    _check(lib().zt_norm(slots, scale, _check_norm(d_norm), zc._stream_handle(stream)), "zt_norm")
+    slots, device = _slots(d_slots)
+    d_norm, norm = _norm(d_norm, device, stream)
+    _check(lib().zt_norm(slots, scale, norm, zc._stream_handle(stream)), "zt_norm")
     return d_norm
 
 
@@ -283,25 +284,22 @@ def zt_clip(tensors, max_norm, scale=1.0, d_out=None, d_slots=None, d_norm=None,
 
     d_out is a list of as many tensors of the same lengths, of any of the types; None: in place.  d_slots is what
     zt_sum_squares gave for them, summed over the ranks that share them out; None: it is taken here."""
-    tensors = list(tensors)
-    pointers, lengths, types, count = _list(tensors, "tensors")
-    if d_out is None:
-        outs, out_types = pointers, types
-    else:
-        d_out = list(d_out)
-        outs, out_lengths, out_types, out_count = _list(d_out, "d_out")
-        if out_count != count or list(out_lengths) != list(lengths):
+    tensors = _List(list(tensors), "tensors")
+    outs = tensors
+    if d_out is not None:
+        outs = _List(list(d_out), "d_out")
+        if outs.lengths != tensors.lengths:
             raise ValueError("d_out must be as many tensors of the same lengths")
-    handle = zc._stream_handle(stream)
+    handle, device = zc._stream_handle(stream), "cuda" if tensors.device is None else tensors.device
+    arguments = tensors.arguments()
     if d_slots is None:
-        d_slots = _empty(ZT_SLOTS, torch.float64, "cuda", stream)
+        d_slots = _empty(ZT_SLOTS, torch.float64, device, stream)
         slots = d_slots.data_ptr()
-        _check(lib().zt_sum_squares(pointers, lengths, types, count, 0, slots, handle), "zt_sum_squares")
+        _check(lib().zt_sum_squares(*arguments, tensors.count, 0, slots, handle), "zt_sum_squares")
     else:
-        slots = _check_slots(d_slots)
-    if d_norm is None:
-        d_norm = _empty(1, torch.float32, "cuda", stream)
-    _check(lib().zt_clip(pointers, lengths, types, outs, out_types, count, slots, scale, max_norm, _check_norm(d_norm), handle), "zt_clip")
+        slots, device = _slots(d_slots)
+    d_norm, norm = _norm(d_norm, device, stream)
+    _check(lib().zt_clip(*arguments, outs.pointers.buffer_info()[0], outs.types.buffer_info()[0], tensors.count, slots, scale, max_norm, norm, handle), "zt_clip")
     return d_norm
 
 
@@ -309,27 +307,24 @@ def zt_adamw(d_grad, d_param, d_m, d_v, lr, beta1, beta2, eps, weight_decay, ste
              d_norm=None, stream=None):
     """One AdamW step on a shard, in place: d_param, d_m and d_v are fp32, d_grad any type, d_half (bfloat16 or float16) gets
     the new parameters.  With d_slots (zt_sum_squares) the gradients are clipped to max_norm and the norm is returned."""
-    grad = _flat(d_grad, "d_grad")
-    form = AdamwForm(n=d_grad.numel(), grad_dtype=_DTYPES[d_grad.dtype], step=step, lr=lr, beta1=beta1, beta2=beta2, eps=eps,
-                     weight_decay=weight_decay, scale=scale, max_norm=max_norm)
-    pointers = []
-    for t, what in ((d_param, "d_param"), (d_m, "d_m"), (d_v, "d_v")):
-        pointers.append(_flat(t, what, torch.float32))
-        if t.numel() != form.n:
-            raise ValueError("%s must hold %d values" % (what, form.n))
-    half = slots = norm = None
+    device = _current(d_grad, "d_grad")
+    n, code = d_grad.numel(), _DTYPES.get(d_grad.dtype)
+    if code is None:
+        raise TypeError("d_grad must be of dtype float32, bfloat16 or float16")
+    grad = _flat(d_grad, "d_grad", d_grad.dtype, device, n)
+    param = _flat(d_param, "d_param", torch.float32, device, n)
+    m, v = _flat(d_m, "d_m", torch.float32, device, n), _flat(d_v, "d_v", torch.float32, device, n)
+    half, half_code, slots, norm = None, 0, None, None
     if d_half is not None:
-        half = _flat(d_half, "d_half")
-        if d_half.numel() != form.n:
-            raise ValueError("d_half must hold %d values" % form.n)
-        form.half_dtype = _DTYPES[d_half.dtype]
+        half_code = _DTYPES.get(d_half.dtype, zc.ZC_F32) if isinstance(d_half, torch.Tensor) else zc.ZC_F32
+        if half_code == zc.ZC_F32:
+            raise TypeError("d_half must be of dtype bfloat16 or float16")
+        half = _flat(d_half, "d_half", d_half.dtype, device, n)
     if d_slots is not None:
-        slots = _check_slots(d_slots)
-        if d_norm is None:
-            d_norm = _empty(1, torch.float32, d_grad.device, stream)
+        slots = _flat(d_slots, "d_slots", torch.float64, device, ZT_SLOTS)
+        d_norm, norm = _norm(d_norm, device, stream)
     elif d_norm is not None:
         raise ValueError("d_norm needs d_slots")
-    if d_norm is not None:
-        norm = _check_norm(d_norm)
-    _check(lib().zt_adamw(form, grad, slots, *pointers, half, norm, zc._stream_handle(stream)), "zt_adamw")
+    form = AdamwForm(n, code, half_code, step, lr, beta1, beta2, eps, weight_decay, scale, max_norm)
+    _check(lib().zt_adamw(form, grad, slots, param, m, v, half, norm, zc._stream_handle(stream)), "zt_adamw")
     return d_norm
