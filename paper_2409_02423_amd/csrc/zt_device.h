@@ -40,7 +40,8 @@ struct Raw {
       for (int j = 0; j < kPart; ++j) w[i * kPart + j] = v[j];
     }
   }
-  // The first `valid`, the rest zero; nothing is read behind them.
+  // The first `valid`, the rest zero; nothing is read behind them.  What is missing is read as the last one there, so that the loads
+  // do not wait for one another.
   __device__ __forceinline__ void load(const char* base, uint32_t at, int valid) {
     if (valid >= N) {
       load(base, at);
@@ -48,14 +49,20 @@ struct Raw {
     }
 #pragma unroll
     for (int i = 0; i < kWords; ++i) w[i] = 0;
+    if (valid <= 0) return;
     const ZT_GLOBAL char* p = (const ZT_GLOBAL char*)base + at;
+    uint32_t one[N - 1];
 #pragma unroll
     for (int i = 0; i < N - 1; ++i) {
-      if constexpr (DT == kF32) {
-        if (i < valid) w[i] = reinterpret_cast<const ZT_GLOBAL uint32_t*>(p)[i];
-      } else {
-        if (i < valid) w[i / 2] |= (uint32_t) reinterpret_cast<const ZT_GLOBAL uint16_t*>(p)[i] << (i % 2 * 16);
-      }
+      const int j = i < valid ? i : valid - 1;
+      if constexpr (DT == kF32) one[i] = reinterpret_cast<const ZT_GLOBAL uint32_t*>(p)[j];
+      else one[i] = reinterpret_cast<const ZT_GLOBAL uint16_t*>(p)[j];
+    }
+#pragma unroll
+    for (int i = 0; i < N - 1; ++i) {
+      const uint32_t v = i < valid ? one[i] : 0;
+      if constexpr (DT == kF32) w[i] = v;
+      else w[i / 2] |= v << (i % 2 * 16);
     }
   }
   template <bool ONCE = false>
@@ -70,20 +77,22 @@ struct Raw {
       else *p = v;
     }
   }
-  __device__ __forceinline__ void store(char* base, uint32_t at, int valid) const {
-    if (valid >= N) {
-      store(base, at);
-      return;
-    }
+  // Those from `from` to `to`.
+  __device__ __forceinline__ void store(char* base, uint32_t at, int from, int to) const {
     ZT_GLOBAL char* p = (ZT_GLOBAL char*)base + at;
 #pragma unroll
-    for (int i = 0; i < N - 1; ++i) {
+    for (int i = 0; i < N; ++i) {
       if constexpr (DT == kF32) {
-        if (i < valid) reinterpret_cast<ZT_GLOBAL uint32_t*>(p)[i] = w[i];
+        if (i >= from && i < to) reinterpret_cast<ZT_GLOBAL uint32_t*>(p)[i] = w[i];
       } else {
-        if (i < valid) reinterpret_cast<ZT_GLOBAL uint16_t*>(p)[i] = (uint16_t)(w[i / 2] >> (i % 2 * 16));
+        if (i >= from && i < to) reinterpret_cast<ZT_GLOBAL uint16_t*>(p)[i] = (uint16_t)(w[i / 2] >> (i % 2 * 16));
       }
     }
+  }
+  // The first `valid`.
+  __device__ __forceinline__ void store(char* base, uint32_t at, int valid) const {
+    if (valid >= N) store(base, at);
+    else store(base, at, 0, valid);
   }
   // Exact.
   __device__ __forceinline__ float get(int i) const {

@@ -14,14 +14,13 @@ struct NormArgs {
   char *y, *h;
   float4* stats;
   size_t sx, sb, sg, sy, sh;     // bytes from row to row
-  uint32_t rows;
   int cols;
   float scale, eps, inv_cols;
 };
 
 // Takes the mean from a row's values (with LAYER); its 1 / deviation.
-template <int DT, bool LAYER, int NV, bool WAVE>
-__device__ __forceinline__ void centre(Values<DT, NV, WAVE>& values, const Lanes<DT, NV, WAVE>& at, Sums<1, WAVE>& sums, float inv_cols, float eps, float& mean, float& r) {
+template <int DT, bool LAYER, int NV>
+__device__ __forceinline__ void centre(Values<DT, NV>& values, const Lanes<DT, NV>& at, Sums<1>& sums, float inv_cols, float eps, float& mean, float& r) {
   constexpr int V = kVec<DT>;
   float s[1] = {0.0f};
   mean = 0.0f;
@@ -53,8 +52,8 @@ __device__ __forceinline__ void centre(Values<DT, NV, WAVE>& values, const Lanes
 }
 
 // v r w (+ c) of one vector.
-template <int DT, bool LAYER, int NV, bool WAVE>
-__device__ __forceinline__ void weigh(float (&v)[kVec<DT>], float r, const Operand<DT, NV, WAVE>& w, const Operand<DT, NV, WAVE>& c, const Lanes<DT, NV, WAVE>& at, int i) {
+template <int DT, bool LAYER, int NV>
+__device__ __forceinline__ void weigh(float (&v)[kVec<DT>], float r, const Operand<DT, NV>& w, const Operand<DT, NV>& c, const Lanes<DT, NV>& at, int i) {
   float wv[kVec<DT>], cv[kVec<DT>];
   w.get(at, i, wv);
   if constexpr (LAYER) c.get(at, i, cv);
@@ -63,87 +62,95 @@ __device__ __forceinline__ void weigh(float (&v)[kVec<DT>], float r, const Opera
 }
 
 template <int DT, bool LAYER, bool POST, int NV, int MOST>
-__global__ void __launch_bounds__(MOST == 64 ? 256 : MOST) norm_kernel(NormArgs a) {
-  constexpr bool WAVE = MOST == 64;
+__global__ void __launch_bounds__(MOST) norm_kernel(NormArgs a) {
   constexpr int V = kVec<DT>;
   __shared__ float buffers[2][1][kMostWaves];
-  Sums<1, WAVE> sums{buffers};
-  const Lanes<DT, NV, WAVE> at(a.cols);
-  Values<DT, NV, WAVE> values;
-  Operand<DT, NV, WAVE> pre_w, pre_c, post_w, post_c, gate, x, b;
-  for (uint32_t row = at.first; row < a.rows; row += at.step) {
-    x.open(at, a.x + row * a.sx);
-    b.open(at, a.b ? a.b + row * a.sb : nullptr);
-    gate.open(at, a.gate ? a.gate + row * a.sg : nullptr, 1.0f);
-    pre_w.open(at, a.pre_w, 1.0f);
-    if constexpr (LAYER) pre_c.open(at, a.pre_c);
-    if constexpr (POST) post_w.open(at, a.post_w, 1.0f);
-    if constexpr (POST && LAYER) post_c.open(at, a.post_c);
-    float4 stats = {0.0f, 0.0f, 0.0f, 0.0f};
-    if constexpr (POST) {
-      at.each([&](int i) {
-        float v[V];
-        b.get(at, i, v);
-        values.set(at, i, v);
-      });
-      centre<DT, LAYER>(values, at, sums, a.inv_cols, a.eps, stats.x, stats.y);
-    }
-    at.each([&](int i) {
-      float v[V], g[V], xv[V];
-      if constexpr (POST) {
-        values.get(at, i, v);
-        weigh<DT, LAYER>(v, stats.y, post_w, post_c, at, i);
-      } else {
-        b.get(at, i, v);
-      }
-      gate.get(at, i, g);
-      x.get(at, i, xv);
-#pragma unroll
-      for (int j = 0; j < V; ++j) v[j] = fmaf(g[j], v[j], a.scale * xv[j]);
-      at.clear_rest(v, i);
-      values.set(at, i, v);
-      if (a.y) at.store(a.y + row * a.sy, i, v);
-    });
-    centre<DT, LAYER>(values, at, sums, a.inv_cols, a.eps, stats.z, stats.w);
+  Sums<1> sums{buffers};
+  const Lanes<DT, NV> at(a.cols);
+  const size_t row = blockIdx.x;
+  Values<DT, NV> values;
+  Operand<DT, NV> pre_w, pre_c, post_w, post_c, gate, x, b;
+  x.open(at, a.x + row * a.sx);
+  b.open(at, a.b ? a.b + row * a.sb : nullptr);
+  gate.open(at, a.gate ? a.gate + row * a.sg : nullptr, 1.0f);
+  pre_w.open(at, a.pre_w, 1.0f);
+  if constexpr (LAYER) pre_c.open(at, a.pre_c);
+  if constexpr (POST) post_w.open(at, a.post_w, 1.0f);
+  if constexpr (POST && LAYER) post_c.open(at, a.post_c);
+  float4 stats = {0.0f, 0.0f, 0.0f, 0.0f};
+  if constexpr (POST) {
     at.each([&](int i) {
       float v[V];
-      values.get(at, i, v);
-      weigh<DT, LAYER>(v, stats.w, pre_w, pre_c, at, i);
-      at.store(a.h + row * a.sh, i, v);
+      b.get(at, i, v);
+      at.clear_rest(v, i);
+      values.set(at, i, v);
     });
-    if (a.stats && at.leads()) a.stats[row] = stats;
+    centre<DT, LAYER>(values, at, sums, a.inv_cols, a.eps, stats.x, stats.y);
   }
+  at.each([&](int i) {
+    float v[V], g[V], xv[V];
+    if constexpr (POST) {
+      values.get(at, i, v);
+      weigh<DT, LAYER>(v, stats.y, post_w, post_c, at, i);
+    } else {
+      b.get(at, i, v);
+    }
+    gate.get(at, i, g);
+    x.get(at, i, xv);
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = fmaf(g[j], v[j], a.scale * xv[j]);
+    at.clear_rest(v, i);
+    values.set(at, i, v);
+    if (a.y) at.store(a.y + row * a.sy, i, v);
+  });
+  centre<DT, LAYER>(values, at, sums, a.inv_cols, a.eps, stats.z, stats.w);
+  at.each([&](int i) {
+    float v[V];
+    values.get(at, i, v);
+    weigh<DT, LAYER>(v, stats.w, pre_w, pre_c, at, i);
+    at.store(a.h + row * a.sh, i, v);
+  });
+  if (a.stats && threadIdx.x == 0) a.stats[row] = stats;
 }
 
 // ---- host ------------------------------------------------------------------------------
 
+// As few vectors a lane as leave a row to one wavefront, or to at most four, one for each SIMD of a CU: more vectors a lane take
+// registers and with them rows that are under way, more wavefronts wait for one another at each sum.  us forward, with 1, 2, 3, 4 and 5
+// vectors a lane: 8192 x 1500 in bf16 18.4, 22.8, 22.0, 29.2 and 33.1 (3, 2, 1, 1 and 1 wavefronts); x 2561 44.4, 36.8, 37.5, 43.7, 58.7 (6, 3, 2, 2, 2);
+// x 4099 84.7, 68.7, 61.8, 74.4, 74.0 (9, 5, 3, 3, 2); x 6144 74.1, 72.9, 69.8, 74.6, 93.2 (12, 6, 4, 3, 3); 4000 x 4099 in fp32, a gate for each
+// value, 2 to 5 vectors 78.1, 82.9, 90.1, 64.2 (9, 6, 5, 4).
 Layout forward_layout(size_t cols, int dtype) {
   const size_t vectors = row_vectors(cols, dtype);
-  if (vectors <= 64) return {1, 64, 64};
-  if (vectors <= 128) return {2, 64, 64};
-  if (vectors <= 1024) return {2, lanes_for(vectors, 2), 512};
-  if (vectors <= 2048) return {2, lanes_for(vectors, 2), 1024};
+  if (cols < (size_t)vector_values(dtype)) return {0, 64, 1024};
+  const int each = (int)((vectors + 255) / 256);
+  if (each <= 5) return {each, lanes_for(vectors, each), 256};
+  if (vectors <= 2048) return {vectors <= 1536 ? 3 : 4, lanes_for(vectors, vectors <= 1536 ? 3 : 4), 512};
   return {0, 1024, 1024};
 }
 
 template <int DT, bool LAYER, bool POST>
-void launch(const NormArgs& a, const Layout& l, hipStream_t s) {
-  const unsigned threads = l.most == 64 ? 256 : l.lanes, rows_each = l.most == 64 ? 4 : 1;
-  const unsigned groups = (a.rows + rows_each - 1) / rows_each;
-  const dim3 grid(groups < kCUs * 8 ? groups : kCUs * 8);
-#define CALL(NV, MOST) hipLaunchKernelGGL((norm_kernel<DT, LAYER, POST, NV, MOST>), grid, dim3(threads), 0, s, a)
-  if (l.vectors == 1) CALL(1, 64);
-  else if (l.vectors == 2 && l.most == 64) CALL(2, 64);
-  else if (l.vectors == 2 && l.most == 512) CALL(2, 512);
-  else if (l.vectors == 2) CALL(2, 1024);
-  else CALL(0, 1024);
+void launch(const NormArgs& a, const Layout& l, unsigned rows, hipStream_t s) {
+#define CALL(NV, MOST) hipLaunchKernelGGL((norm_kernel<DT, LAYER, POST, NV, MOST>), dim3(rows), dim3(l.lanes), 0, s, a)
+  switch (l.most * 8 + l.vectors) {
+    case 256 * 8 + 1: CALL(1, 256); break;
+    case 256 * 8 + 2: CALL(2, 256); break;
+    case 256 * 8 + 3: CALL(3, 256); break;
+    case 256 * 8 + 4: CALL(4, 256); break;
+    case 256 * 8 + 5: CALL(5, 256); break;
+    case 512 * 8 + 3: CALL(3, 512); break;
+    case 512 * 8 + 4: CALL(4, 512); break;
+    default: CALL(0, 1024); break;
+  }
 #undef CALL
 }
 template <int DT>
-void launch(const zt_residual& f, const NormArgs& a, const Layout& l, hipStream_t s) {
-  if (f.kind == ZT_LAYER) f.post ? launch<DT, true, true>(a, l, s) : launch<DT, true, false>(a, l, s);
-  else f.post ? launch<DT, false, true>(a, l, s) : launch<DT, false, false>(a, l, s);
+void launch(const zt_residual& f, const NormArgs& a, const Layout& l, unsigned rows, hipStream_t s) {
+  if (f.kind == ZT_LAYER) f.post ? launch<DT, true, true>(a, l, rows, s) : launch<DT, true, false>(a, l, rows, s);
+  else f.post ? launch<DT, false, true>(a, l, rows, s) : launch<DT, false, false>(a, l, rows, s);
 }
+
+constexpr size_t kMostRows = (size_t)1 << 21;   // of one launch: a grid has fewer than 2^32 lanes
 
 }  // namespace
 
@@ -177,16 +184,24 @@ int zt_residual_norm(const struct zt_residual* form, const void* d_x, const void
   a.sg = f.gate == ZT_GATE_FULL ? stride_of(f.stride_gate, f.cols) * e : 0;   // a gate per channel is the same for every row
   a.sy = stride_of(f.stride_y, f.cols) * e;
   a.sh = stride_of(f.stride_h, f.cols) * e;
-  a.rows = (uint32_t)f.rows;
   a.cols = (int)f.cols;
   a.scale = f.residual_scale;
   a.eps = f.eps;
   a.inv_cols = (float)(1.0 / (double)f.cols);
   const Layout l = forward_layout(f.cols, f.dtype);
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (f.dtype == ZC_F32) launch<kF32>(f, a, l, s);
-  else if (f.dtype == ZC_BF16) launch<kBF16>(f, a, l, s);
-  else launch<kF16>(f, a, l, s);
+  for (size_t done = 0; done < f.rows; done += kMostRows) {
+    const unsigned rows = (unsigned)(f.rows - done < kMostRows ? f.rows - done : kMostRows);
+    if (f.dtype == ZC_F32) launch<kF32>(f, a, l, rows, s);
+    else if (f.dtype == ZC_BF16) launch<kBF16>(f, a, l, rows, s);
+    else launch<kF16>(f, a, l, rows, s);
+    a.x += rows * a.sx;
+    if (a.b) a.b += rows * a.sb;
+    if (a.gate) a.gate += rows * a.sg;
+    if (a.y) a.y += rows * a.sy;
+    a.h += rows * a.sh;
+    if (a.stats) a.stats += rows;
+  }
   return finish_launch();
 }
 

@@ -14,7 +14,7 @@ struct BackwardArgs {
   const char *dy, *dh, *y, *b, *gate, *pre_w, *post_w, *post_c;
   const float4* stats;
   char *dx, *db, *dgate;
-  float* partial;                // [workgroup or wavefront][sum][padded columns]
+  float* partial;                // [workgroup or wavefront][sum][columns, padded]
   size_t sdy, sdh, sy, sb, sg, sdx, sdb, sdg;
   uint32_t rows;
   int cols, padded;
@@ -28,14 +28,14 @@ struct SumIndex {
 };
 
 // A lane's sums over rows: in registers, or for wide rows (NV = 0) in the workspace, of which a workgroup has a part to itself.
-template <int COUNT, int DT, int NV, bool WAVE>
+template <int COUNT, int DT, int NV>
 struct Columns {
   static constexpr int V = kVec<DT>;
   float held[COUNT][NV > 0 ? NV : 1][V];
-  char* partial;
-  size_t one;          // bytes of one sum's columns
+  float* partial;
+  size_t padded;       // columns
   bool fresh = true;   // nothing in the workspace yet
-  __device__ __forceinline__ Columns(char* p, size_t bytes) : partial(p), one(bytes) {
+  __device__ __forceinline__ Columns(float* p, size_t columns) : partial(p), padded(columns) {
     if constexpr (NV > 0) {
 #pragma unroll
       for (int k = 0; k < COUNT; ++k)
@@ -46,66 +46,98 @@ struct Columns {
     }
   }
   // Sum k of vector i: += a * b
-  __device__ __forceinline__ void add(const Lanes<DT, NV, WAVE>& at, int k, int i, const float (&a)[V], const float (&b)[V]) {
+  __device__ __forceinline__ void add(const Lanes<DT, NV>& at, int k, int i, const float (&a)[V], const float (&b)[V]) {
     if constexpr (NV > 0) {
 #pragma unroll
       for (int j = 0; j < V; ++j) held[k][i][j] = fmaf(a[j], b[j], held[k][i][j]);
-    } else if (at.valid(i) > 0) {
-      Raw<kF32, V> r = {};
-      if (!fresh) r.load(partial + k * one, (uint32_t)at.col(i) * 4);
-      float s[V];
-      r.unpack(s);
+    } else {
+      float* sums = partial + k * padded + at.col(i);
+      if (at.whole(i)) {
+        Raw<kF32, V> r = {};
+        if (!fresh) r.load(reinterpret_cast<char*>(sums - at.col(i)), (uint32_t)at.col(i) * 4);
+        float s[V];
+        r.unpack(s);
 #pragma unroll
-      for (int j = 0; j < V; ++j) s[j] = fmaf(a[j], b[j], s[j]);
-      r.pack(s);
-      r.store(partial + k * one, (uint32_t)at.col(i) * 4);
+        for (int j = 0; j < V; ++j) s[j] = fmaf(a[j], b[j], s[j]);
+        r.pack(s);
+        r.store(reinterpret_cast<char*>(sums - at.col(i)), (uint32_t)at.col(i) * 4);
+      } else if (at.any(i)) {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+          if (j >= at.from(i) && j < at.to()) sums[j] = fmaf(a[j], b[j], fresh ? 0.0f : sums[j]);
+      }
     }
   }
-  __device__ __forceinline__ void add(const Lanes<DT, NV, WAVE>& at, int k, int i, const float (&a)[V]) {
+  __device__ __forceinline__ void add(const Lanes<DT, NV>& at, int k, int i, const float (&a)[V]) {
     float ones[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) ones[j] = 1.0f;
     add(at, k, i, a, ones);
   }
-  __device__ __forceinline__ void leave(const Lanes<DT, NV, WAVE>& at) const {
+  __device__ __forceinline__ void leave(const Lanes<DT, NV>& at) const {
     if constexpr (NV > 0) {
 #pragma unroll
       for (int k = 0; k < COUNT; ++k)
         at.each([&](int i) {
-          if (at.valid(i) > 0) {
-            Raw<kF32, V> r;
-            r.pack(held[k][i]);
-            r.store(partial + k * one, (uint32_t)at.col(i) * 4);
-          }
+          Raw<kF32, V> r;
+          r.pack(held[k][i]);
+          char* sums = reinterpret_cast<char*>(partial + k * padded);
+          if (at.whole(i)) r.store(sums, (uint32_t)at.col(i) * 4);
+          else if (at.any(i)) r.store(sums, (uint32_t)at.col(i) * 4, at.from(i), at.to());
         });
     }
   }
 };
 
-template <int DT, bool LAYER, bool POST, bool CHANNEL, int NV, int MOST>
-__global__ void __launch_bounds__(MOST == 64 ? 256 : MOST) norm_backward_kernel(BackwardArgs a) {
-  constexpr bool WAVE = MOST == 64;
-  constexpr int V = kVec<DT>, K = LAYER ? 2 : 1;
-  typedef SumIndex<LAYER, POST, CHANNEL> Index;
-  __shared__ float buffers[2][K][kMostWaves];
-  Sums<K, WAVE> sums{buffers};
-  const Lanes<DT, NV, WAVE> at(a.cols);
-  Values<DT, NV, WAVE> values;   // the gradient of y, then of z
-  Operand<DT, NV, WAVE> pre_w, post_w, post_c, gate, dy, dh, y, b;
-  const size_t one = (size_t)a.padded * sizeof(float);
-  Columns<Index::count, DT, NV, WAVE> columns(reinterpret_cast<char*>(a.partial) + at.first * Index::count * one, one);
-  for (uint32_t row = at.first; row < a.rows; row += at.step) {
-    const float4 stats = a.stats[row];
+// What a row is made of, apart from the weights.
+template <int DT, int NV>
+struct BackwardRow {
+  Operand<DT, NV> dh, y, dy, b, gate;
+  float4 stats;
+  __device__ __forceinline__ void open(const Lanes<DT, NV>& at, const BackwardArgs& a, uint32_t row) {
+    stats = a.stats[row];
     dh.open(at, a.dh + row * a.sdh);
     y.open(at, a.y + row * a.sy);
-    pre_w.open(at, a.pre_w, 1.0f);
     dy.open(at, a.dy ? a.dy + row * a.sdy : nullptr);
     b.open(at, a.b ? a.b + row * a.sb : nullptr);
     gate.open(at, a.gate ? a.gate + row * a.sg : nullptr, 1.0f);
+  }
+};
+
+template <int DT, bool LAYER, bool POST, bool CHANNEL, int NV, int MOST>
+__global__ void __launch_bounds__(MOST) norm_backward_kernel(BackwardArgs a) {
+  constexpr int V = kVec<DT>, K = LAYER ? 2 : 1;
+  typedef SumIndex<LAYER, POST, CHANNEL> Index;
+  __shared__ float buffers[2][K][kMostWaves];
+  Sums<K> sums{buffers};
+  const Lanes<DT, NV> at(a.cols);
+  Values<DT, NV> values;   // the gradient of y, then of z
+  Operand<DT, NV> pre_w, post_w, post_c;
+  const auto open_weights = [&] {
+    pre_w.open(at, a.pre_w, 1.0f);
     if constexpr (POST) post_w.open(at, a.post_w, 1.0f);
     if constexpr (POST && LAYER) post_c.open(at, a.post_c);
+  };
+  Columns<Index::count, DT, NV> columns(a.partial + (size_t)blockIdx.x * Index::count * a.padded, a.padded);
+  // The weights stay, and the next row is under way while this one is worked on, where registers hold all that.
+  constexpr bool kAhead = NV < 2 || DT == kF32 || !(LAYER && POST);
+  BackwardRow<DT, NV> now, next;
+  if constexpr (kAhead) {
+    open_weights();
+    if (blockIdx.x < a.rows) next.open(at, a, blockIdx.x);
+  }
+  for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    if constexpr (kAhead) {
+      now = next;
+      if (row + gridDim.x < a.rows) next.open(at, a, row + gridDim.x);
+    } else {
+      open_weights();
+      now.open(at, a, row);
+    }
+    const float4 stats = now.stats;
+    const auto &dh = now.dh, &y = now.y, &dy = now.dy, &b = now.b, &gate = now.gate;
     // a norm's input as it was normed, before weight and bias
-    const auto unit = [&](const Operand<DT, NV, WAVE>& from, int i, float mean, float r, float (&u)[V]) {
+    const auto unit = [&](const Operand<DT, NV>& from, int i, float mean, float r, float (&u)[V]) {
       from.get(at, i, u);
 #pragma unroll
       for (int j = 0; j < V; ++j) u[j] = LAYER ? (u[j] - mean) * r : u[j] * r;
@@ -119,11 +151,12 @@ __global__ void __launch_bounds__(MOST == 64 ? 256 : MOST) norm_backward_kernel(
         if constexpr (LAYER) s[K - 1] += t;
       }
     };
-    // through the pre norm; behind the row's end dh is zero
+    // through the pre norm
     float s[K] = {};
     at.each([&](int i) {
       float g[V], u[V], w[V];
       dh.get(at, i, g);
+      at.clear_rest(g, i);
       unit(y, i, stats.z, stats.w, u);
       pre_w.get(at, i, w);
       columns.add(at, Index::pre_w, i, g, u);
@@ -205,15 +238,16 @@ __global__ void __launch_bounds__(MOST == 64 ? 256 : MOST) norm_backward_kernel(
   columns.leave(at);
 }
 
-// Adds the partial sums up, in their order: a workgroup takes 64 columns of one sum, 16 lanes with four columns each and 16 slices of the
+// Adds the partial sums up, in their order: a workgroup takes 64 columns of one sum, 16 lanes with four columns each and 64 slices of the
 // partial sums.
 struct ColumnArgs {
   const float* partial;
   float* out[5];
   int partials, count, cols, padded;
 };
-__global__ void __launch_bounds__(256) column_sums_kernel(ColumnArgs a) {
-  __shared__ float4 slices[16][16];
+constexpr int kSlices = 64;
+__global__ void __launch_bounds__(16 * kSlices) column_sums_kernel(ColumnArgs a) {
+  __shared__ float4 slices[kSlices][16];
   const int lane = threadIdx.x & 15, slice = threadIdx.x / 16, k = blockIdx.y;
   const int col = (blockIdx.x * 16 + lane) * 4;
   float4 s = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -221,7 +255,7 @@ __global__ void __launch_bounds__(256) column_sums_kernel(ColumnArgs a) {
     const float* p = a.partial + (size_t)k * a.padded + col;
     const size_t step = (size_t)a.count * a.padded;
 #pragma unroll 4
-    for (int i = slice; i < a.partials; i += 16) {
+    for (int i = slice; i < a.partials; i += kSlices) {
       const float4 v = *reinterpret_cast<const float4*>(p + i * step);
       s.x += v.x;
       s.y += v.y;
@@ -235,33 +269,33 @@ __global__ void __launch_bounds__(256) column_sums_kernel(ColumnArgs a) {
   if (threadIdx.x < 64 && out) {
     const int c = blockIdx.x * 64 + threadIdx.x;
     float t = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) t += reinterpret_cast<const float*>(slices[i])[threadIdx.x];
+#pragma unroll 16
+    for (int i = 0; i < kSlices; ++i) t += reinterpret_cast<const float*>(slices[i])[threadIdx.x];
     if (c < a.cols) out[c] = t;
   }
 }
 
 // ---- host ------------------------------------------------------------------------------
 
+// One vector a lane where a workgroup can have as many lanes: more of them take registers and no more bytes are under way.  us
+// with 1, 2, 3 and 4 vectors a lane, each at its best number of workgroups: 8192 x 6144 values in bf16 with both norms and a gate per channel 115.7, 116.2,
+// 124.4 and 149.1; x 4096 78.2, 79.1, 104.1 and 88.5; x 2048 45.3, 47.4, 58.9 and 73.0.  Beyond 768 lanes, whose registers still hold two rows, two
+// vectors.
 Layout backward_layout(size_t cols, int dtype) {
   const size_t vectors = row_vectors(cols, dtype);
-  if (vectors <= 64) return {1, 64, 64};
+  if (cols < (size_t)vector_values(dtype)) return {0, 64, 1024};
   if (vectors <= 256) return {1, lanes_for(vectors, 1), 256};
-  if (vectors <= 1024) return {1, lanes_for(vectors, 1), 1024};
+  if (vectors <= 768) return {1, lanes_for(vectors, 1), 768};
+  if (vectors <= 1024) return {2, lanes_for(vectors, 2), 512};
   return {0, 1024, 1024};
 }
 
-// Workgroups, and the partial sums that they leave, one for each workgroup or, in the layout for short rows, wavefront.
-constexpr size_t kMostPartials = 1024;
-struct BackwardGrid {
-  unsigned groups;
-  size_t partials;
-};
-BackwardGrid backward_grid(size_t rows, const Layout& l) {
-  const size_t waves = l.most == 64 ? 4 : 1;
-  size_t groups = (rows + waves - 1) / waves;
-  if (groups > kMostPartials / waves) groups = kMostPartials / waves;
-  return {(unsigned)groups, groups * waves};
+// Workgroups, each of which leaves one partial sum for each column: as few as keep memory busy.  us with 1, 2, 3, 4, 6, 8 and 12
+// a CU: 256 lanes (8192 x 2048 as above) 49.2, 45.3, 46.8, 52.8, 54.5, 57.0, 63.4; 128 lanes (16384 x 1024) 81.9, 56.1, 45.2, 48.5, 49.9, 57.4, 61.8; 64 lanes
+// (32768 x 512) 137, 87.0, 58.7, 50.3, 49.7, 50.7, 54.5; 512 and 768 lanes with 1 and 2 78.2 and 83.2, 115.7 and 123.5.
+size_t backward_groups(size_t rows, const Layout& l) {
+  const size_t per_cu = l.vectors == 0 || l.lanes > 256 ? 1 : l.lanes > 128 ? 2 : l.lanes > 64 ? 3 : 6;
+  return rows < kCUs * per_cu ? rows : kCUs * per_cu;
 }
 
 int sums_of(const zt_residual& f) {
@@ -272,11 +306,10 @@ size_t padded_cols(size_t cols) { return (cols + 7) / 8 * 8; }
 
 template <int DT, bool LAYER, bool POST, bool CHANNEL>
 void launch(const BackwardArgs& a, const Layout& l, unsigned groups, hipStream_t s) {
-  const unsigned threads = l.most == 64 ? 256 : l.lanes;
-#define CALL(NV, MOST) hipLaunchKernelGGL((norm_backward_kernel<DT, LAYER, POST, CHANNEL, NV, MOST>), dim3(groups), dim3(threads), 0, s, a)
-  if (l.most == 64) CALL(1, 64);
-  else if (l.most == 256) CALL(1, 256);
-  else if (l.vectors == 1) CALL(1, 1024);
+#define CALL(NV, MOST) hipLaunchKernelGGL((norm_backward_kernel<DT, LAYER, POST, CHANNEL, NV, MOST>), dim3(groups), dim3(l.lanes), 0, s, a)
+  if (l.most == 256) CALL(1, 256);
+  else if (l.most == 768) CALL(1, 768);
+  else if (l.most == 512) CALL(2, 512);
   else CALL(0, 1024);
 #undef CALL
 }
@@ -297,7 +330,7 @@ extern "C" {
 size_t zt_residual_work_bytes(const struct zt_residual* form) {
   if (check_form(form) != ZC_OK || form->rows == 0 || form->cols == 0) return 0;
   const Layout l = backward_layout(form->cols, form->dtype);
-  return backward_grid(form->rows, l).partials * (size_t)sums_of(*form) * padded_cols(form->cols) * sizeof(float);
+  return backward_groups(form->rows, l) * (size_t)sums_of(*form) * padded_cols(form->cols) * sizeof(float);
 }
 
 int zt_residual_norm_backward(const struct zt_residual* form, const void* d_dy, const void* d_dh, const void* d_y, const void* d_b,
@@ -347,12 +380,12 @@ int zt_residual_norm_backward(const struct zt_residual* form, const void* d_dy, 
   a.scale = f.residual_scale;
   a.inv_cols = (float)(1.0 / (double)f.cols);
   const Layout l = backward_layout(f.cols, f.dtype);
-  const BackwardGrid grid = backward_grid(f.rows, l);
+  const size_t groups = backward_groups(f.rows, l);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (f.rows != 0) {
-    if (f.dtype == ZC_F32) launch<kF32>(f, a, l, grid.groups, s);
-    else if (f.dtype == ZC_BF16) launch<kBF16>(f, a, l, grid.groups, s);
-    else launch<kF16>(f, a, l, grid.groups, s);
+    if (f.dtype == ZC_F32) launch<kF32>(f, a, l, (unsigned)groups, s);
+    else if (f.dtype == ZC_BF16) launch<kBF16>(f, a, l, (unsigned)groups, s);
+    else launch<kF16>(f, a, l, (unsigned)groups, s);
   }
   ColumnArgs c;      // with no rows the sums are zero
   int k = 0;
@@ -365,11 +398,11 @@ int zt_residual_norm_backward(const struct zt_residual* form, const void* d_dy, 
   for (int i = 0; i < k; ++i) wanted = wanted || c.out[i];
   if (wanted) {
     c.partial = a.partial;
-    c.partials = (int)grid.partials;
+    c.partials = (int)groups;
     c.count = k;
     c.cols = a.cols;
     c.padded = a.padded;
-    hipLaunchKernelGGL(column_sums_kernel, dim3((unsigned)((f.cols + 63) / 64), (unsigned)k), dim3(256), 0, s, c);
+    hipLaunchKernelGGL(column_sums_kernel, dim3((unsigned)((a.padded + 63) / 64), (unsigned)k), dim3(16 * kSlices), 0, s, c);
   }
   return finish_launch();
 }
