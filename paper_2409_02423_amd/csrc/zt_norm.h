@@ -50,35 +50,58 @@ struct Lanes {
     else r.load(row, 0, cols);
     return r;
   }
-  // Nontemporal: rows together are far more than the caches next to the lanes hold.
+  // Nontemporal: rows together are far more than the caches next to the lanes hold.  What is not a lane's own is dropped by the
+  // store's bounds and not branched around: behind a branch it is not known how many stores there were, and the next wait for a load,
+  // which counts them, is for all of them (backward, 8192 x 4100 values in bf16, 110 us; now 80).
   __device__ __forceinline__ void store(char* row, int i, const float (&v)[V]) const {
     Raw<DT> r;
     r.pack(v);
-    if (whole(i)) r.template store<true>(row, (uint32_t)col(i) * kBytes<DT>);
-    else if (any(i)) r.store(row, (uint32_t)col(i) * kBytes<DT>, from(i), to());
+    if constexpr (NV > 0) {
+      typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+      typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+      constexpr int kNontemporal = 2, kNowhere = -16;
+      const auto to_row = __builtin_amdgcn_make_buffer_rsrc(row, 0, cols * kBytes<DT>, 0x00027000);
+      const int at = place(i) * kBytes<DT>;
+      __builtin_amdgcn_raw_buffer_store_b128(u32x4{r.w[0], r.w[1], r.w[2], r.w[3]}, to_row, whole(i) ? at : kNowhere, 0, kNontemporal);
+      const int own = cols % V;
+      if (own != 0) {      // the last vector's, which are the last of its values: in parts of 8, 4 and 2 bytes
+        const bool mine = !whole(i) && any(i);
+        if constexpr (DT == kF32) {
+          if (own & 2) __builtin_amdgcn_raw_buffer_store_b64(u32x2{r.w[2], r.w[3]}, to_row, mine ? at + (own & 1) * 4 : kNowhere, 0, 0);
+          if (own & 1) __builtin_amdgcn_raw_buffer_store_b32(own & 2 ? r.w[1] : r.w[3], to_row, mine ? at : kNowhere, 0, 0);
+        } else {
+          if (own & 4) __builtin_amdgcn_raw_buffer_store_b64(u32x2{r.w[2], r.w[3]}, to_row, mine ? at + (own & 3) * 2 : kNowhere, 0, 0);
+          if (own & 2) __builtin_amdgcn_raw_buffer_store_b32(own & 4 ? r.w[1] : r.w[3], to_row, mine ? at + (own & 1) * 2 : kNowhere, 0, 0);
+          const uint32_t last = own & 4 ? (own & 2 ? r.w[0] : r.w[1]) : (own & 2 ? r.w[2] : r.w[3]);
+          if (own & 1) __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(last >> 16), to_row, mine ? at : kNowhere, 0, 0);
+        }
+      }
+    } else {
+      if (whole(i)) r.template store<true>(row, (uint32_t)col(i) * kBytes<DT>);
+      else if (any(i)) r.store(row, (uint32_t)col(i) * kBytes<DT>, from(i), to());
+    }
   }
   // What is not its own counts as zero.
   __device__ __forceinline__ void clear_rest(float (&v)[V], int i) const {
-    if (!whole(i)) {
+    if (NV > 0 ? cols < NV * lanes * V : !whole(i)) {
       const int begin = from(i), end = to();
 #pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (j < begin || j >= end) v[j] = 0.0f;
+      for (int j = 0; j < V; ++j) v[j] = j < begin || j >= end ? 0.0f : v[j];
     }
   }
 };
 
-// A row of one operand, or of weights: a lane's vectors, loaded at once and held, or each loaded where it is used (NV = 0).  An
-// operand that is absent is the same value everywhere.
-template <int DT, int NV>
+// A row of one operand, or of weights: a lane's vectors, loaded at once and held, or each loaded where it is used.  An operand that is
+// absent is the same value everywhere.
+template <int DT, int NV, bool HOLD = (NV > 0)>
 struct Operand {
-  Raw<DT> held[NV > 0 ? NV : 1];
+  Raw<DT> held[HOLD ? NV : 1];
   const char* row;
   float otherwise;
   __device__ __forceinline__ void open(const Lanes<DT, NV>& at, const char* p, float absent = 0.0f) {
     row = p;
     otherwise = absent;
-    if constexpr (NV > 0) at.each([&](int i) { held[i] = fetch(at, i); });
+    if constexpr (HOLD) at.each([&](int i) { held[i] = fetch(at, i); });
   }
   __device__ __forceinline__ Raw<DT> fetch(const Lanes<DT, NV>& at, int i) const {
     Raw<DT> r;
@@ -93,27 +116,27 @@ struct Operand {
     return r;
   }
   __device__ __forceinline__ void get(const Lanes<DT, NV>& at, int i, float (&v)[kVec<DT>]) const {
-    if constexpr (NV > 0) held[i].unpack(v);
+    if constexpr (HOLD) held[i].unpack(v);
     else fetch(at, i).unpack(v);
   }
 };
 
-// A row's fp32 values: in registers, or in LDS (NV = 0), where a lane reads only what it has written.
-template <int DT, int NV>
+// A row's fp32 values: in registers, or in LDS, where a lane reads only what it has written.
+template <int DT, int NV, bool HOLD = (NV > 0)>
 struct Values {
   static constexpr int V = kVec<DT>;
-  float held[NV > 0 ? NV : 1][V];
+  float held[HOLD ? NV : 1][V];
   float4* lds;
   __device__ __forceinline__ Values() {
-    if constexpr (NV == 0) {
-      __shared__ float4 row[ZT_MAX_COLS / 4];
+    if constexpr (!HOLD) {
+      __shared__ float4 row[NV > 0 ? 1024 * NV * V / 4 : ZT_MAX_COLS / 4];
       lds = row;
     }
   }
   __device__ __forceinline__ void get(const Lanes<DT, NV>& at, int i, float (&v)[V]) const {
 #pragma unroll
     for (int j = 0; j < V; j += 4) {
-      if constexpr (NV > 0) {
+      if constexpr (HOLD) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[j + q] = held[i][j + q];
       } else {
@@ -128,7 +151,7 @@ struct Values {
   __device__ __forceinline__ void set(const Lanes<DT, NV>& at, int i, const float (&v)[V]) {
 #pragma unroll
     for (int j = 0; j < V; j += 4) {
-      if constexpr (NV > 0) {
+      if constexpr (HOLD) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) held[i][j + q] = v[j + q];
       } else {

@@ -90,9 +90,9 @@ struct Columns {
 };
 
 // What a row is made of, apart from the weights.
-template <int DT, int NV>
+template <int DT, int NV, bool HOLD>
 struct BackwardRow {
-  Operand<DT, NV> dh, y, dy, b, gate;
+  Operand<DT, NV, HOLD> dh, y, dy, b, gate;
   float4 stats;
   __device__ __forceinline__ void open(const Lanes<DT, NV>& at, const BackwardArgs& a, uint32_t row) {
     stats = a.stats[row];
@@ -104,15 +104,15 @@ struct BackwardRow {
   }
 };
 
-template <int DT, bool LAYER, bool POST, bool CHANNEL, int NV, int MOST>
+template <int DT, bool LAYER, bool POST, bool CHANNEL, int NV, int MOST, bool HOLD>
 __global__ void __launch_bounds__(MOST) norm_backward_kernel(BackwardArgs a) {
   constexpr int V = kVec<DT>, K = LAYER ? 2 : 1;
   typedef SumIndex<LAYER, POST, CHANNEL> Index;
   __shared__ float buffers[2][K][kMostWaves];
   Sums<K> sums{buffers};
   const Lanes<DT, NV> at(a.cols);
-  Values<DT, NV> values;   // the gradient of y, then of z
-  Operand<DT, NV> pre_w, post_w, post_c;
+  Values<DT, NV, HOLD> values;   // the gradient of y, then of z
+  Operand<DT, NV, HOLD> pre_w, post_w, post_c;
   const auto open_weights = [&] {
     pre_w.open(at, a.pre_w, 1.0f);
     if constexpr (POST) post_w.open(at, a.post_w, 1.0f);
@@ -120,8 +120,8 @@ __global__ void __launch_bounds__(MOST) norm_backward_kernel(BackwardArgs a) {
   };
   Columns<Index::count, DT, NV> columns(a.partial + (size_t)blockIdx.x * Index::count * a.padded, a.padded);
   // The weights stay, and the next row is under way while this one is worked on, where registers hold all that.
-  constexpr bool kAhead = NV < 2 || DT == kF32 || !(LAYER && POST);
-  BackwardRow<DT, NV> now, next;
+  constexpr bool kAhead = HOLD && (NV < 2 || DT == kF32 || !(LAYER && POST));
+  BackwardRow<DT, NV, HOLD> now, next;
   if constexpr (kAhead) {
     open_weights();
     if (blockIdx.x < a.rows) next.open(at, a, blockIdx.x);
@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(MOST) norm_backward_kernel(BackwardArgs a) {
     const float4 stats = now.stats;
     const auto &dh = now.dh, &y = now.y, &dy = now.dy, &b = now.b, &gate = now.gate;
     // a norm's input as it was normed, before weight and bias
-    const auto unit = [&](const Operand<DT, NV>& from, int i, float mean, float r, float (&u)[V]) {
+    const auto unit = [&](const Operand<DT, NV, HOLD>& from, int i, float mean, float r, float (&u)[V]) {
       from.get(at, i, u);
 #pragma unroll
       for (int j = 0; j < V; ++j) u[j] = LAYER ? (u[j] - mean) * r : u[j] * r;
@@ -280,13 +280,15 @@ __global__ void __launch_bounds__(16 * kSlices) column_sums_kernel(ColumnArgs a)
 // One vector a lane where a workgroup can have as many lanes: more of them take registers and no more bytes are under way.  us
 // with 1, 2, 3 and 4 vectors a lane, each at its best number of workgroups: 8192 x 6144 values in bf16 with both norms and a gate per channel 115.7, 116.2,
 // 124.4 and 149.1; x 4096 78.2, 79.1, 104.1 and 88.5; x 2048 45.3, 47.4, 58.9 and 73.0.  Beyond 768 lanes, whose registers still hold two rows, two
-// vectors.
-Layout backward_layout(size_t cols, int dtype) {
-  const size_t vectors = row_vectors(cols, dtype);
-  if (cols < (size_t)vector_values(dtype)) return {0, 64, 1024};
+// vectors.  Wide rows in fp32 keep their sums over rows and load the rest where it is used (2048 x 8192 values 146 us in the form for
+// any width, whose sums are in the workspace, 98 like this); the sums of all five kinds, and those of half-precision rows, are too many registers.
+Layout backward_layout(const zt_residual& f) {
+  const size_t vectors = row_vectors(f.cols, f.dtype);
+  if (f.cols < (size_t)vector_values(f.dtype)) return {0, 64, 1024};
   if (vectors <= 256) return {1, lanes_for(vectors, 1), 256};
   if (vectors <= 768) return {1, lanes_for(vectors, 1), 768};
   if (vectors <= 1024) return {2, lanes_for(vectors, 2), 512};
+  if (vectors <= 2048 && f.dtype == ZC_F32 && !(f.kind == ZT_LAYER && f.post && f.gate == ZT_GATE_CHANNEL)) return {2, lanes_for(vectors, 2), 1024};
   return {0, 1024, 1024};
 }
 
@@ -306,11 +308,12 @@ size_t padded_cols(size_t cols) { return (cols + 7) / 8 * 8; }
 
 template <int DT, bool LAYER, bool POST, bool CHANNEL>
 void launch(const BackwardArgs& a, const Layout& l, unsigned groups, hipStream_t s) {
-#define CALL(NV, MOST) hipLaunchKernelGGL((norm_backward_kernel<DT, LAYER, POST, CHANNEL, NV, MOST>), dim3(groups), dim3(l.lanes), 0, s, a)
-  if (l.most == 256) CALL(1, 256);
-  else if (l.most == 768) CALL(1, 768);
-  else if (l.most == 512) CALL(2, 512);
-  else CALL(0, 1024);
+#define CALL(NV, MOST, HOLD) hipLaunchKernelGGL((norm_backward_kernel<DT, LAYER, POST, CHANNEL, NV, MOST, HOLD>), dim3(groups), dim3(l.lanes), 0, s, a)
+  if (l.most == 256) CALL(1, 256, true);
+  else if (l.most == 768) CALL(1, 768, true);
+  else if (l.most == 512) CALL(2, 512, true);
+  else if (l.vectors == 0) CALL(0, 1024, false);
+  else if constexpr (DT == kF32 && !(LAYER && POST && CHANNEL)) CALL(2, 1024, false);
 #undef CALL
 }
 template <int DT, bool LAYER, bool POST>
@@ -329,7 +332,7 @@ extern "C" {
 
 size_t zt_residual_work_bytes(const struct zt_residual* form) {
   if (check_form(form) != ZC_OK || form->rows == 0 || form->cols == 0) return 0;
-  const Layout l = backward_layout(form->cols, form->dtype);
+  const Layout l = backward_layout(*form);
   return backward_groups(form->rows, l) * (size_t)sums_of(*form) * padded_cols(form->cols) * sizeof(float);
 }
 
@@ -379,7 +382,7 @@ int zt_residual_norm_backward(const struct zt_residual* form, const void* d_dy, 
   a.padded = (int)padded_cols(f.cols);
   a.scale = f.residual_scale;
   a.inv_cols = (float)(1.0 / (double)f.cols);
-  const Layout l = backward_layout(f.cols, f.dtype);
+  const Layout l = backward_layout(f);
   const size_t groups = backward_groups(f.rows, l);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (f.rows != 0) {
