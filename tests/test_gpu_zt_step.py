@@ -57,6 +57,25 @@ def test_sum_of_squares(zt, sizes, types):
     assert twice is slots and abs(float(slots.sum()) - 2 * want) <= 2 * EXACT * want
 
 
+@pytest.mark.parametrize("types", ("f32", "bf16", ("bf16", "f32", "f16")), ids=str)
+def test_lists_of_more_chunks_than_workgroups(zt, types):
+    """Each workgroup goes from tensor to tensor several times, long ones and short ones by turns."""
+    import torch
+    print("lists of more chunks than workgroups", types, flush=True)
+    sizes = [3 * 1025 * 1025, 3 * 1025, 1025 * 1025, 1025, 4 * 1025 * 1025, 4 * 1025, 1025, 8192, 16384 * 40 + 5] * 3
+    g = torch.Generator(device="cuda").manual_seed(12)
+    names = [types] if isinstance(types, str) else list(types)
+    tensors = [torch.randn(n, generator=g, device="cuda").to(_dtypes()[names[i % len(names)]]) for i, n in enumerate(sizes)]
+    want = sum(float((t.double() ** 2).sum()) for t in tensors)
+    assert abs(float(zt.zt_sum_squares(tensors).sum()) - want) <= EXACT * want
+    out = [torch.full((n,), 7.0, device="cuda") for n in sizes]
+    norm = zt.zt_clip(tensors, 2.0, d_out=out)
+    assert abs(float(norm) - math.sqrt(want)) <= 2.0 ** -23 * math.sqrt(want)
+    for t, o in zip(tensors, out):
+        exact = t.double() * (2.0 / math.sqrt(want))
+        assert bool(((o.double() - exact).abs() <= 2.0 ** -21 * exact.abs()).all())
+
+
 def test_squares_neither_overflow_nor_vanish(zt):
     import torch
     for value in (3e38, 1e-30, 1.4e-45):
