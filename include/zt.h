@@ -115,7 +115,7 @@ int zt_norm(const double* d_slots, float scale, float* d_norm, void* stream);
 /* Clipping: d_out[i] = c * d_in[i] for every tensor, with norm as zt_norm gives it and
  *     c = scale                      if norm <= max_norm
  *     c = scale * max_norm / norm    otherwise (NaN if the norm is NaN).
- * max_norm > 0; infinity asks for no clipping.  Tensor i is read as dtype_in[i] and written as
+ * max_norm > 0; infinity asks for no clipping.  In place with c = 1 nothing is written.  Tensor i is read as dtype_in[i] and written as
  * dtype_out[i]; d_out[i] may be d_in[i] if the types are the same, no other overlap.  d_norm
  * may be NULL. */
 int zt_clip(const void* const* d_in, const size_t* n, const int* dtype_in, void* const* d_out, const int* dtype_out,

@@ -152,6 +152,7 @@ __device__ __forceinline__ void scale_chunk(const char* in, char* out, int left,
     else raw[i].load(in, at * kBytes<DI>, left - at);
   }
   const float factor = make_factor();
+  if (DI == DO && in == out && factor == 1.0f) return;   // in place, and nothing to change
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     const int at = (threadIdx.x + i * kThreads) * kN;

@@ -223,6 +223,7 @@ def zt_residual_norm_backward(d_dy, d_dh, d_y, d_b, d_stats, kind=ZT_RMS, pre_we
 
 
 _data_ptr, _numel, _get_device, _is_contiguous = torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.get_device, torch.Tensor.is_contiguous
+_dtype = torch.Tensor.dtype.__get__     # as these, refuses what is no tensor with a TypeError
 
 
 class _List:
@@ -230,7 +231,7 @@ class _List:
 
     def __init__(self, tensors, what):
         self.count = len(tensors)
-        types = [_DTYPES.get(getattr(t, "dtype", None)) for t in tensors]
+        types = list(map(_DTYPES.get, map(_dtype, tensors)))
         self.device = torch.cuda.current_device() if tensors and None not in types and tensors[0].is_cuda else None
         if None in types or not all(map(_is_contiguous, tensors)) or (tensors and self.device is None):
             raise TypeError("%s must be contiguous CUDA tensors of dtype float32, bfloat16 or float16" % what)

@@ -317,6 +317,29 @@ def test_offsets_beyond_32_bits(zt):
     assert torch.equal(far, y) and torch.equal(h2, h)
 
 
+def test_more_rows_than_a_grid_has(zt):
+    """2^21 workgroups are launched at most: rows beyond them are a launch of their own."""
+    import torch
+    rows, cols = (1 << 21) + 77, 16
+    print("rows", rows, flush=True)
+    g = torch.Generator(device="cuda").manual_seed(13)
+    x, b, gate = (torch.randn((rows, cols), generator=g, device="cuda").bfloat16() for _ in range(3))
+    stats = torch.empty((rows, 4), device="cuda")
+    form = dict(post=True, residual_scale=0.5, d_gate=gate)
+    y, h = zt.zt_residual_norm(x, b, d_stats=stats, **form)
+    some = torch.cat([torch.arange(4), torch.arange((1 << 21) - 4, rows)]).cuda()
+    stats2 = torch.empty((some.numel(), 4), device="cuda")
+    y2, h2 = zt.zt_residual_norm(x[some], b[some], d_stats=stats2, **dict(form, d_gate=gate[some]))
+    assert torch.equal(y[some], y2) and torch.equal(h[some], h2) and torch.equal(stats[some], stats2)
+    weight = torch.ones(cols, device="cuda").bfloat16()
+    got = zt.zt_residual_norm_backward(None, h, y, b, stats, pre_weight=weight, **form)
+    want = zt.zt_residual_norm_backward(None, h2, y2, b[some], stats2, pre_weight=weight, **dict(form, d_gate=gate[some]))
+    assert all(torch.equal(got[k][some], want[k]) for k in ("x", "b", "gate"))
+    unit = y.double() * stats[:, 3:].double()
+    # 2^21 terms, of which 1365 are added up one after the other
+    assert bool(((got["pre_weight"].double() - (h.double() * unit).sum(0)).abs() <= 1365 * 2.0 ** -24 * (h.double() * unit).abs().sum(0)).all())
+
+
 def test_another_stream_and_a_graph(zt):
     import torch
     d, _ = _inputs(606, 64, 700, "bf16", True, True, "channel")
