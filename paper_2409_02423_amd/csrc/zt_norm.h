@@ -105,8 +105,10 @@ struct Operand {
   }
   __device__ __forceinline__ Raw<DT> fetch(const Lanes<DT, NV>& at, int i) const {
     Raw<DT> r;
-    if (row) {
-      r = at.load(row, i);
+    const char* p = row;
+    if constexpr (!HOLD) asm volatile("" : "+s"(p));   // loaded anew each time: the compiler would keep what registers have no room for
+    if (p) {
+      r = at.load(p, i);
     } else {
       float v[kVec<DT>];
 #pragma unroll

@@ -280,15 +280,19 @@ __global__ void __launch_bounds__(16 * kSlices) column_sums_kernel(ColumnArgs a)
 // One vector a lane where a workgroup can have as many lanes: more of them take registers and no more bytes are under way.  us
 // with 1, 2, 3 and 4 vectors a lane, each at its best number of workgroups: 8192 x 6144 values in bf16 with both norms and a gate per channel 115.7, 116.2,
 // 124.4 and 149.1; x 4096 78.2, 79.1, 104.1 and 88.5; x 2048 45.3, 47.4, 58.9 and 73.0.  Beyond 768 lanes, whose registers still hold two rows, two
-// vectors.  Wide rows in fp32 keep their sums over rows and load the rest where it is used (2048 x 8192 values 146 us in the form for
-// any width, whose sums are in the workspace, 98 like this); the sums of all five kinds, and those of half-precision rows, are too many registers.
+// vectors.  Wide rows in fp32 keep their sums over rows and load the rest where it is used: 2048 x 8192 values as above 146 us in the form for
+// any width, whose sums are in the workspace, 93 with two vectors and 108 with four; with sums of all five kinds two take more registers than there are, and
+// it is 181 and, with four, 116.  In half precision, whose vectors have twice the values, neither fits.
 Layout backward_layout(const zt_residual& f) {
   const size_t vectors = row_vectors(f.cols, f.dtype);
   if (f.cols < (size_t)vector_values(f.dtype)) return {0, 64, 1024};
   if (vectors <= 256) return {1, lanes_for(vectors, 1), 256};
   if (vectors <= 768) return {1, lanes_for(vectors, 1), 768};
   if (vectors <= 1024) return {2, lanes_for(vectors, 2), 512};
-  if (vectors <= 2048 && f.dtype == ZC_F32 && !(f.kind == ZT_LAYER && f.post && f.gate == ZT_GATE_CHANNEL)) return {2, lanes_for(vectors, 2), 1024};
+  if (vectors <= 2048 && f.dtype == ZC_F32) {
+    if (f.kind == ZT_LAYER && f.post && f.gate == ZT_GATE_CHANNEL) return {4, lanes_for(vectors, 4), 512};
+    return {2, lanes_for(vectors, 2), 1024};
+  }
   return {0, 1024, 1024};
 }
 
@@ -311,9 +315,10 @@ void launch(const BackwardArgs& a, const Layout& l, unsigned groups, hipStream_t
 #define CALL(NV, MOST, HOLD) hipLaunchKernelGGL((norm_backward_kernel<DT, LAYER, POST, CHANNEL, NV, MOST, HOLD>), dim3(groups), dim3(l.lanes), 0, s, a)
   if (l.most == 256) CALL(1, 256, true);
   else if (l.most == 768) CALL(1, 768, true);
-  else if (l.most == 512) CALL(2, 512, true);
+  else if (l.most == 512 && l.vectors == 2) CALL(2, 512, true);
   else if (l.vectors == 0) CALL(0, 1024, false);
-  else if constexpr (DT == kF32 && !(LAYER && POST && CHANNEL)) CALL(2, 1024, false);
+  else if constexpr (DT == kF32 && LAYER && POST && CHANNEL) CALL(4, 512, false);
+  else if constexpr (DT == kF32) CALL(2, 1024, false);
 #undef CALL
 }
 template <int DT, bool LAYER, bool POST>
