@@ -13,31 +13,49 @@ namespace {
 
 // How a row lies over lanes.  A workgroup takes whole rows, one at a time; a lane has NV vectors of 16 bytes of a row, neighbouring
 // lanes neighbouring ones.  NV = 0 is the form for rows that registers do not hold: as many
-// vectors as it takes, operands loaded where they are used and the row's fp32 values in LDS; and for rows shorter than a vector.
+// vectors as it takes, operands loaded where they are used and the row's fp32 values in LDS.  NV = kShort16 and kShort32 are those for rows of
+// 16 and 32 vectors at most, which as many lanes take each, four or two rows to a wavefront; they may be shorter than a vector.
 //
 // So that every load is a whole one, a row's last vector is moved to end where the row does.  What it then shares with the one ahead of
 // it is not its own: it is loaded but counts for nothing and is not stored.  (Loading the last values one by one, in a branch of
-// their own, held up each row's first sum: 8192 x 4099 values in fp32 150 us forward, now 105.)  Which lane has which column does not depend on where
+// their own, held up each row's first sum: 8192 x 4099 values in fp32 150 us forward, now 111.)  Which lane has which column does not depend on where
 // tensors lie, nor do the results, bit for bit.  (Vectors that start where memory is aligned to them made 8192 x 4099 in bf16 12 % faster, at that price.)
+constexpr int kShort16 = -1, kShort32 = -2;
+template <int NV> constexpr int kShortLanes = NV == kShort16 ? 16 : NV == kShort32 ? 32 : 0;   // of a row, where a workgroup has several
+template <int NV> constexpr int kHeld = NV > 0 ? NV : 1;   // vectors that registers hold, if any
+
 template <int DT, int NV>
 struct Lanes {
   static constexpr int V = kVec<DT>;
   int lane, lanes, cols;
-  __device__ __forceinline__ explicit Lanes(int columns) : lane(threadIdx.x), lanes(blockDim.x), cols(columns) {}
+  uint32_t first, step;   // rows
+  __device__ __forceinline__ explicit Lanes(int columns) : cols(columns) {
+    if constexpr (NV < 0) {
+      lanes = kShortLanes<NV>;
+      lane = threadIdx.x % kShortLanes<NV>;
+      first = (blockIdx.x * blockDim.x + threadIdx.x) / kShortLanes<NV>;
+      step = gridDim.x * blockDim.x / kShortLanes<NV>;
+    } else {
+      lane = threadIdx.x;
+      lanes = blockDim.x;
+      first = blockIdx.x;
+      step = gridDim.x;
+    }
+  }
   // Place of a lane's vector i in the order of lanes, and the column that it is loaded from.
   __device__ __forceinline__ int place(int i) const { return (lane + i * lanes) * V; }
   __device__ __forceinline__ int col(int i) const { return max(0, min(place(i), cols - V)); }
   // Its own values are those from `from` to `to`.
   __device__ __forceinline__ int from(int i) const { return min(place(i) - col(i), V); }
-  __device__ __forceinline__ int to() const { return NV == 0 && cols < V ? cols : V; }
+  __device__ __forceinline__ int to() const { return NV < 0 && cols < V ? cols : V; }
   __device__ __forceinline__ bool whole(int i) const { return place(i) <= cols - V; }
   __device__ __forceinline__ bool any(int i) const { return place(i) < cols; }
   // f(i) for each of a lane's vectors.
   template <class F>
   __device__ __forceinline__ void each(F&& f) const {
-    if constexpr (NV > 0) {
+    if constexpr (NV != 0) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) f(i);
+      for (int i = 0; i < kHeld<NV>; ++i) f(i);
     } else {
       const int count = (cols + lanes * V - 1) / (lanes * V);
 #pragma unroll 1
@@ -46,7 +64,7 @@ struct Lanes {
   }
   __device__ __forceinline__ Raw<DT> load(const char* row, int i) const {
     Raw<DT> r;
-    if (NV > 0 || cols >= V) r.load(row, (uint32_t)col(i) * kBytes<DT>);
+    if (NV >= 0 || cols >= V) r.load(row, (uint32_t)col(i) * kBytes<DT>);
     else r.load(row, 0, cols);
     return r;
   }
@@ -93,9 +111,9 @@ struct Lanes {
 
 // A row of one operand, or of weights: a lane's vectors, loaded at once and held, or each loaded where it is used.  An operand that is
 // absent is the same value everywhere.
-template <int DT, int NV, bool HOLD = (NV > 0)>
+template <int DT, int NV, bool HOLD = (NV != 0)>
 struct Operand {
-  Raw<DT> held[HOLD ? NV : 1];
+  Raw<DT> held[kHeld<NV>];
   const char* row;
   float otherwise;
   __device__ __forceinline__ void open(const Lanes<DT, NV>& at, const char* p, float absent = 0.0f) {
@@ -124,10 +142,10 @@ struct Operand {
 };
 
 // A row's fp32 values: in registers, or in LDS, where a lane reads only what it has written.
-template <int DT, int NV, bool HOLD = (NV > 0)>
+template <int DT, int NV, bool HOLD = (NV != 0)>
 struct Values {
   static constexpr int V = kVec<DT>;
-  float held[HOLD ? NV : 1][V];
+  float held[kHeld<NV>][V];
   float4* lds;
   __device__ __forceinline__ Values() {
     if constexpr (!HOLD) {
@@ -165,13 +183,21 @@ struct Values {
 static_assert(ZT_MAX_COLS % (1024 * 8) == 0, "the last vectors of a workgroup's lanes in LDS");
 
 // Sums of K values over a row's lanes, the same in each of them.
-template <int K>
+template <int K, int NV>
 struct Sums {
   float (*buffers)[K][kMostWaves];
   int next = 0;
   __device__ __forceinline__ void operator()(float (&v)[K]) {
-    group_sum(v, buffers[next]);
-    next ^= 1;
+    if constexpr (NV < 0) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        v[k] = row_sum(v[k]);
+        if constexpr (NV == kShort32) v[k] += __shfl_xor(v[k], 16);
+      }
+    } else {
+      group_sum(v, buffers[next]);
+      next ^= 1;
+    }
   }
 };
 
@@ -180,12 +206,17 @@ struct Sums {
 constexpr unsigned kCUs = 256;
 constexpr size_t kMaxStride = (size_t)1 << 40;
 
-// NV vectors a lane (0: the form for wide rows); a workgroup of `lanes`, at most `most`, for a row.
+// NV vectors a lane (0: the form for wide rows, below: those for short ones); a workgroup of `lanes`, at most `most`, for a row, or `rows` short ones.
 struct Layout {
-  int vectors, lanes, most;
+  int vectors, lanes, most, rows = 1;
 };
 int vector_values(int dtype) { return dtype == ZC_F32 ? 4 : 8; }
 size_t row_vectors(size_t cols, int dtype) { return (cols + vector_values(dtype) - 1) / vector_values(dtype); }
+// Rows that leave most of a wavefront idle share one.  us in bf16 with a wavefront for each row and with this, forward and
+// backward: 262144 x 7 values 3066 and 38, 6226 and 80 (values of rows shorter than a vector were loaded one by one by the only lane that had any);
+// x 64 96 and 29, 252 and 53; 131072 x 129 65 and 37, 152 and 62; x 200 60 and 39, 148 and 65.
+bool short_rows(size_t vectors) { return vectors <= 32; }
+Layout short_layout(size_t vectors) { return vectors <= 16 ? Layout{kShort16, 256, 256, 16} : Layout{kShort32, 256, 256, 8}; }
 int lanes_for(size_t vectors, int each) { return (int)(((vectors + each - 1) / each + 63) / 64 * 64); }
 
 int check_form(const zt_residual* f) {

@@ -1,8 +1,11 @@
 // zt_norm_backward.hip -- gfx950 kernels and C ABI of the residual join with the norms around a block, backward (include/zt.h).
 //
-// As forward, a row stays in registers.  The sums over the rows, for weights, biases and a gate per channel, stay there too: a
-// workgroup takes many rows, adds their terms up lane by lane and leaves one partial sum for each column; a second kernel adds the
-// partial sums up in their order, so the result does not depend on which workgroup was first.
+// The gradient of unit = (v - mean) r is r (t - unit mean(t unit) - mean(t)) for that of the norm's output times its weights, t; through the
+// join it is followed from h to y, to x and the block's output, and through the gate and the other norm to b.  As forward, a row
+// stays in registers (12 bytes a value in half precision for some 30 operations: memory bounds it).  The sums over the rows, for weights, biases and a gate per
+// channel, stay there too: a workgroup takes many rows, adds their terms up lane by lane and leaves one partial sum for each column; a second kernel adds the
+// partial sums up in their order, so the result does not depend on which workgroup was first.  8192 x 6144 values in bf16 with both norms and a gate per
+// channel: 110 us, 5.5 TB/s, and 5.5 us for 256 partial sums of 18432 columns.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -14,7 +17,7 @@ struct BackwardArgs {
   const char *dy, *dh, *y, *b, *gate, *pre_w, *post_w, *post_c;
   const float4* stats;
   char *dx, *db, *dgate;
-  float* partial;                // [workgroup or wavefront][sum][columns, padded]
+  float* partial;                // [workgroup][sum][columns, padded]
   size_t sdy, sdh, sy, sb, sg, sdx, sdb, sdg;
   uint32_t rows;
   int cols, padded;
@@ -31,23 +34,23 @@ struct SumIndex {
 template <int COUNT, int DT, int NV>
 struct Columns {
   static constexpr int V = kVec<DT>;
-  float held[COUNT][NV > 0 ? NV : 1][V];
+  float held[COUNT][kHeld<NV>][V];
   float* partial;
   size_t padded;       // columns
   bool fresh = true;   // nothing in the workspace yet
   __device__ __forceinline__ Columns(float* p, size_t columns) : partial(p), padded(columns) {
-    if constexpr (NV > 0) {
+    if constexpr (NV != 0) {
 #pragma unroll
       for (int k = 0; k < COUNT; ++k)
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < kHeld<NV>; ++i)
 #pragma unroll
           for (int j = 0; j < V; ++j) held[k][i][j] = 0.0f;
     }
   }
   // Sum k of vector i: += a * b
   __device__ __forceinline__ void add(const Lanes<DT, NV>& at, int k, int i, const float (&a)[V], const float (&b)[V]) {
-    if constexpr (NV > 0) {
+    if constexpr (NV != 0) {
 #pragma unroll
       for (int j = 0; j < V; ++j) held[k][i][j] = fmaf(a[j], b[j], held[k][i][j]);
     } else {
@@ -74,8 +77,28 @@ struct Columns {
     for (int j = 0; j < V; ++j) ones[j] = 1.0f;
     add(at, k, i, a, ones);
   }
-  __device__ __forceinline__ void leave(const Lanes<DT, NV>& at) const {
-    if constexpr (NV > 0) {
+  __device__ __forceinline__ void leave(const Lanes<DT, NV>& at) {
+    if constexpr (NV < 0) {      // of the rows that a workgroup has at a time: over a wavefront's, then over the wavefronts
+      constexpr int kLanes = kShortLanes<NV>;
+      __shared__ float parts[COUNT][4][kLanes][V];
+      const int wave = threadIdx.x / 64;
+#pragma unroll
+      for (int k = 0; k < COUNT; ++k)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          float s = held[k][0][j];
+          if constexpr (kLanes == 16) s += __shfl_xor(s, 16);
+          s += __shfl_xor(s, 32);
+          if ((threadIdx.x & 63) < kLanes) parts[k][wave][at.lane][j] = s;
+        }
+      __syncthreads();
+      if (threadIdx.x >= kLanes) return;
+#pragma unroll
+      for (int k = 0; k < COUNT; ++k)
+#pragma unroll
+        for (int j = 0; j < V; ++j) held[k][0][j] = (parts[k][0][at.lane][j] + parts[k][1][at.lane][j]) + (parts[k][2][at.lane][j] + parts[k][3][at.lane][j]);
+    }
+    if constexpr (NV != 0) {
 #pragma unroll
       for (int k = 0; k < COUNT; ++k)
         at.each([&](int i) {
@@ -109,7 +132,7 @@ __global__ void __launch_bounds__(MOST) norm_backward_kernel(BackwardArgs a) {
   constexpr int V = kVec<DT>, K = LAYER ? 2 : 1;
   typedef SumIndex<LAYER, POST, CHANNEL> Index;
   __shared__ float buffers[2][K][kMostWaves];
-  Sums<K> sums{buffers};
+  Sums<K, NV> sums{buffers};
   const Lanes<DT, NV> at(a.cols);
   Values<DT, NV, HOLD> values;   // the gradient of y, then of z
   Operand<DT, NV, HOLD> pre_w, post_w, post_c;
@@ -124,12 +147,12 @@ __global__ void __launch_bounds__(MOST) norm_backward_kernel(BackwardArgs a) {
   BackwardRow<DT, NV, HOLD> now, next;
   if constexpr (kAhead) {
     open_weights();
-    if (blockIdx.x < a.rows) next.open(at, a, blockIdx.x);
+    if (at.first < a.rows) next.open(at, a, at.first);
   }
-  for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+  for (uint32_t row = at.first; row < a.rows; row += at.step) {
     if constexpr (kAhead) {
       now = next;
-      if (row + gridDim.x < a.rows) next.open(at, a, row + gridDim.x);
+      if (row + at.step < a.rows) next.open(at, a, row + at.step);
     } else {
       open_weights();
       now.open(at, a, row);
@@ -282,10 +305,10 @@ __global__ void __launch_bounds__(16 * kSlices) column_sums_kernel(ColumnArgs a)
 // 124.4 and 149.1; x 4096 78.2, 79.1, 104.1 and 88.5; x 2048 45.3, 47.4, 58.9 and 73.0.  Beyond 768 lanes, whose registers still hold two rows, two
 // vectors.  Wide rows in fp32 keep their sums over rows and load the rest where it is used: 2048 x 8192 values as above 146 us in the form for
 // any width, whose sums are in the workspace, 93 with two vectors and 108 with four; with sums of all five kinds two take more registers than there are, and
-// it is 181 and, with four, 116.  In half precision, whose vectors have twice the values, neither fits.
+// it is 181 and, with four, 116.  In half precision, whose vectors have twice the values, registers hold neither.
 Layout backward_layout(const zt_residual& f) {
   const size_t vectors = row_vectors(f.cols, f.dtype);
-  if (f.cols < (size_t)vector_values(f.dtype)) return {0, 64, 1024};
+  if (short_rows(vectors)) return short_layout(vectors);
   if (vectors <= 256) return {1, lanes_for(vectors, 1), 256};
   if (vectors <= 768) return {1, lanes_for(vectors, 1), 768};
   if (vectors <= 1024) return {2, lanes_for(vectors, 2), 512};
@@ -299,9 +322,11 @@ Layout backward_layout(const zt_residual& f) {
 // Workgroups, each of which leaves one partial sum for each column: as few as keep memory busy.  us with 1, 2, 3, 4, 6, 8 and 12
 // a CU: 256 lanes (8192 x 2048 as above) 49.2, 45.3, 46.8, 52.8, 54.5, 57.0, 63.4; 128 lanes (16384 x 1024) 81.9, 56.1, 45.2, 48.5, 49.9, 57.4, 61.8; 64 lanes
 // (32768 x 512) 137, 87.0, 58.7, 50.3, 49.7, 50.7, 54.5; 512 and 768 lanes with 1 and 2 78.2 and 83.2, 115.7 and 123.5.
+// Short rows with 2, 3, 4 and 6: 262144 x 64 in bf16 57.1, 53.4, 50.4, 54.6; 131072 x 128 45.1, 45.0, 47.3, 50.1; x 200 65.6, 65.2, 70.7, 74.4.
 size_t backward_groups(size_t rows, const Layout& l) {
-  const size_t per_cu = l.vectors == 0 || l.lanes > 256 ? 1 : l.lanes > 128 ? 2 : l.lanes > 64 ? 3 : 6;
-  return rows < kCUs * per_cu ? rows : kCUs * per_cu;
+  const size_t per_cu = l.vectors < 0 ? 3 : l.vectors == 0 || l.lanes > 256 ? 1 : l.lanes > 128 ? 2 : l.lanes > 64 ? 3 : 6;
+  const size_t groups = (rows + l.rows - 1) / l.rows;
+  return groups < kCUs * per_cu ? groups : kCUs * per_cu;
 }
 
 int sums_of(const zt_residual& f) {
@@ -313,7 +338,9 @@ size_t padded_cols(size_t cols) { return (cols + 7) / 8 * 8; }
 template <int DT, bool LAYER, bool POST, bool CHANNEL>
 void launch(const BackwardArgs& a, const Layout& l, unsigned groups, hipStream_t s) {
 #define CALL(NV, MOST, HOLD) hipLaunchKernelGGL((norm_backward_kernel<DT, LAYER, POST, CHANNEL, NV, MOST, HOLD>), dim3(groups), dim3(l.lanes), 0, s, a)
-  if (l.most == 256) CALL(1, 256, true);
+  if (l.vectors == kShort16) CALL(kShort16, 256, true);
+  else if (l.vectors == kShort32) CALL(kShort32, 256, true);
+  else if (l.most == 256) CALL(1, 256, true);
   else if (l.most == 768) CALL(1, 768, true);
   else if (l.most == 512 && l.vectors == 2) CALL(2, 512, true);
   else if (l.vectors == 0) CALL(0, 1024, false);
