@@ -27,7 +27,8 @@ template <int NV> constexpr int kHeld = NV > 0 ? NV : 1;   // vectors that regis
 template <int DT, int NV>
 struct Lanes {
   static constexpr int V = kVec<DT>;
-  int lane, lanes, cols;
+  mutable int lane;
+  int lanes, cols;
   uint32_t first, step;   // rows
   __device__ __forceinline__ explicit Lanes(int columns) : cols(columns) {
     if constexpr (NV < 0) {
@@ -50,6 +51,8 @@ struct Lanes {
   __device__ __forceinline__ int to() const { return NV < 0 && cols < V ? cols : V; }
   __device__ __forceinline__ bool whole(int i) const { return place(i) <= cols - V; }
   __device__ __forceinline__ bool any(int i) const { return place(i) < cols; }
+  // What follows works its places out anew: kept for all vectors and rows they take registers that wide rows need.
+  __device__ __forceinline__ void forget() const { asm volatile("" : "+v"(lane)); }
   // f(i) for each of a lane's vectors.
   template <class F>
   __device__ __forceinline__ void each(F&& f) const {

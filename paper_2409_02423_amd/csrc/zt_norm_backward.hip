@@ -30,6 +30,10 @@ struct SumIndex {
   static constexpr int pre_w = 0, pre_c = 1, post_w = 1 + LAYER, post_c = 2 + LAYER, gate = 1 + LAYER + (POST ? 1 + LAYER : 0), count = gate + CHANNEL;
 };
 
+// A sum is added up where that stands and not at the end of the row, where the compiler would move it: what is added takes more
+// registers till then than all the sums.
+__device__ __forceinline__ void now(float& sum) { asm volatile("" : "+v"(sum)); }
+
 // A lane's sums over rows: in registers, or for wide rows (NV = 0) in the workspace, of which a workgroup has a part to itself.
 template <int COUNT, int DT, int NV>
 struct Columns {
@@ -52,7 +56,10 @@ struct Columns {
   __device__ __forceinline__ void add(const Lanes<DT, NV>& at, int k, int i, const float (&a)[V], const float (&b)[V]) {
     if constexpr (NV != 0) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) held[k][i][j] = fmaf(a[j], b[j], held[k][i][j]);
+      for (int j = 0; j < V; ++j) {
+        held[k][i][j] = fmaf(a[j], b[j], held[k][i][j]);
+        if constexpr (NV > 1) now(held[k][i][j]);
+      }
     } else {
       float* sums = partial + k * padded + at.col(i);
       if (at.whole(i)) {
@@ -127,8 +134,12 @@ struct BackwardRow {
   }
 };
 
-template <int DT, bool LAYER, bool POST, bool CHANNEL, int NV, int MOST, bool HOLD>
+// What registers hold of a row and the weights besides the sums: all of it, the row, or what is worked on.
+enum Hold { kNothing, kRow, kAll };
+
+template <int DT, bool LAYER, bool POST, bool CHANNEL, int NV, int MOST, Hold HOW>
 __global__ void __launch_bounds__(MOST) norm_backward_kernel(BackwardArgs a) {
+  constexpr bool HOLD = HOW == kAll, ROW = HOW != kNothing;
   constexpr int V = kVec<DT>, K = LAYER ? 2 : 1;
   typedef SumIndex<LAYER, POST, CHANNEL> Index;
   __shared__ float buffers[2][K][kMostWaves];
@@ -143,24 +154,24 @@ __global__ void __launch_bounds__(MOST) norm_backward_kernel(BackwardArgs a) {
   };
   Columns<Index::count, DT, NV> columns(a.partial + (size_t)blockIdx.x * Index::count * a.padded, a.padded);
   // The weights stay, and the next row is under way while this one is worked on, where registers hold all that.
-  constexpr bool kAhead = HOLD && (NV < 2 || DT == kF32 || !(LAYER && POST));
-  BackwardRow<DT, NV, HOLD> now, next;
+  constexpr bool kAhead = HOLD && (NV < 2 || DT == kF32 || !(LAYER && POST && CHANNEL));
+  BackwardRow<DT, NV, ROW> current, next;
   if constexpr (kAhead) {
     open_weights();
     if (at.first < a.rows) next.open(at, a, at.first);
   }
   for (uint32_t row = at.first; row < a.rows; row += at.step) {
     if constexpr (kAhead) {
-      now = next;
+      current = next;
       if (row + at.step < a.rows) next.open(at, a, row + at.step);
     } else {
       open_weights();
-      now.open(at, a, row);
+      current.open(at, a, row);
     }
-    const float4 stats = now.stats;
-    const auto &dh = now.dh, &y = now.y, &dy = now.dy, &b = now.b, &gate = now.gate;
+    const float4 stats = current.stats;
+    const auto &dh = current.dh, &y = current.y, &dy = current.dy, &b = current.b, &gate = current.gate;
     // a norm's input as it was normed, before weight and bias
-    const auto unit = [&](const Operand<DT, NV, HOLD>& from, int i, float mean, float r, float (&u)[V]) {
+    const auto unit = [&](const Operand<DT, NV, ROW>& from, int i, float mean, float r, float (&u)[V]) {
       from.get(at, i, u);
 #pragma unroll
       for (int j = 0; j < V; ++j) u[j] = LAYER ? (u[j] - mean) * r : u[j] * r;
@@ -173,10 +184,15 @@ __global__ void __launch_bounds__(MOST) norm_backward_kernel(BackwardArgs a) {
         s[0] = fmaf(t, u[j], s[0]);
         if constexpr (LAYER) s[K - 1] += t;
       }
+      if constexpr (NV > 1) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) now(s[k]);
+      }
     };
     // through the pre norm
     float s[K] = {};
     at.each([&](int i) {
+      if constexpr (NV > 1 && !HOLD) at.forget();
       float g[V], u[V], w[V];
       dh.get(at, i, g);
       at.clear_rest(g, i);
@@ -190,6 +206,7 @@ __global__ void __launch_bounds__(MOST) norm_backward_kernel(BackwardArgs a) {
     const float along = s[0] * a.inv_cols, mean = s[K - 1] * a.inv_cols;
     float s2[K] = {};
     at.each([&](int i) {
+      if constexpr (NV > 1 && !HOLD) at.forget();
       float g[V], u[V], w[V], d[V], v[V];
       dh.get(at, i, g);
       unit(y, i, stats.z, stats.w, u);
@@ -242,6 +259,7 @@ __global__ void __launch_bounds__(MOST) norm_backward_kernel(BackwardArgs a) {
       const float along2 = s2[0] * a.inv_cols, mean2 = s2[K - 1] * a.inv_cols;
       if (a.db) {
         at.each([&](int i) {
+          if constexpr (NV > 1 && !HOLD) at.forget();
           float d[V], u[V], w[V];
           values.get(at, i, d);
           unit(b, i, stats.x, stats.y, u);
@@ -303,18 +321,23 @@ __global__ void __launch_bounds__(16 * kSlices) column_sums_kernel(ColumnArgs a)
 // One vector a lane where a workgroup can have as many lanes: more of them take registers and no more bytes are under way.  us
 // with 1, 2, 3 and 4 vectors a lane, each at its best number of workgroups: 8192 x 6144 values in bf16 with both norms and a gate per channel 115.7, 116.2,
 // 124.4 and 149.1; x 4096 78.2, 79.1, 104.1 and 88.5; x 2048 45.3, 47.4, 58.9 and 73.0.  Beyond 768 lanes, whose registers still hold two rows, two
-// vectors.  Wide rows in fp32 keep their sums over rows and load the rest where it is used: 2048 x 8192 values as above 146 us in the form for
-// any width, whose sums are in the workspace, 93 with two vectors and 108 with four; with sums of all five kinds two take more registers than there are, and
-// it is 181 and, with four, 116.  In half precision, whose vectors have twice the values, registers hold neither.
+// vectors.  Wider ones have fewer registers for a value: rows of more than 1024 vectors keep their sums there and, where
+// it fits, the row. us in the form for any width, whose sums are in the workspace, with the sums in registers and with the row as
+// well, with both norms and a gate per channel: 4096 x 12288 in bf16 312, 169 and, with at most 768 lanes, which have more registers each, 152; x 8200 225, 150
+// and 119; 2048 x 16384 212, 112, and it does not fit; 4096 x 8193 in fp32 302, 257, and it does not fit; x 8192 the latter two 175 and 171. With sums of
+// all five kinds in half precision it takes fewer lanes, without the row: 4096 x 12288 448 and 273.
 Layout backward_layout(const zt_residual& f) {
   const size_t vectors = row_vectors(f.cols, f.dtype);
   if (short_rows(vectors)) return short_layout(vectors);
   if (vectors <= 256) return {1, lanes_for(vectors, 1), 256};
   if (vectors <= 768) return {1, lanes_for(vectors, 1), 768};
   if (vectors <= 1024) return {2, lanes_for(vectors, 2), 512};
-  if (vectors <= 2048 && f.dtype == ZC_F32) {
+  if (f.dtype == ZC_F32) {
+    if (vectors <= 2048) return {2, lanes_for(vectors, 2), 1024};
+    if (vectors <= 4096) return {4, lanes_for(vectors, 4), 1024};
+  } else if (vectors <= 2048) {
     if (f.kind == ZT_LAYER && f.post && f.gate == ZT_GATE_CHANNEL) return {4, lanes_for(vectors, 4), 512};
-    return {2, lanes_for(vectors, 2), 1024};
+    return {2, lanes_for(vectors, 2), vectors <= 1536 ? 768 : 1024};
   }
   return {0, 1024, 1024};
 }
@@ -337,15 +360,22 @@ size_t padded_cols(size_t cols) { return (cols + 7) / 8 * 8; }
 
 template <int DT, bool LAYER, bool POST, bool CHANNEL>
 void launch(const BackwardArgs& a, const Layout& l, unsigned groups, hipStream_t s) {
-#define CALL(NV, MOST, HOLD) hipLaunchKernelGGL((norm_backward_kernel<DT, LAYER, POST, CHANNEL, NV, MOST, HOLD>), dim3(groups), dim3(l.lanes), 0, s, a)
-  if (l.vectors == kShort16) CALL(kShort16, 256, true);
-  else if (l.vectors == kShort32) CALL(kShort32, 256, true);
-  else if (l.most == 256) CALL(1, 256, true);
-  else if (l.most == 768) CALL(1, 768, true);
-  else if (l.most == 512 && l.vectors == 2) CALL(2, 512, true);
-  else if (l.vectors == 0) CALL(0, 1024, false);
-  else if constexpr (DT == kF32 && LAYER && POST && CHANNEL) CALL(4, 512, false);
-  else if constexpr (DT == kF32) CALL(2, 1024, false);
+#define CALL(NV, MOST, HOW) hipLaunchKernelGGL((norm_backward_kernel<DT, LAYER, POST, CHANNEL, NV, MOST, HOW>), dim3(groups), dim3(l.lanes), 0, s, a)
+  if (l.vectors == kShort16) CALL(kShort16, 256, kAll);
+  else if (l.vectors == kShort32) CALL(kShort32, 256, kAll);
+  else if (l.vectors == 1 && l.most == 256) CALL(1, 256, kAll);
+  else if (l.vectors == 1) CALL(1, 768, kAll);
+  else if (l.vectors == 2 && l.most == 512) CALL(2, 512, kAll);
+  else if (l.vectors == 0) CALL(0, 1024, kNothing);
+  else if constexpr (DT == kF32) {
+    if (l.vectors == 2) CALL(2, 1024, kRow);
+    else CALL(4, 1024, kNothing);
+  } else if constexpr (LAYER && POST && CHANNEL) {
+    CALL(4, 512, kNothing);
+  } else {
+    if (l.most == 768) CALL(2, 768, kRow);
+    else CALL(2, 1024, (CHANNEL || (LAYER && POST)) ? kNothing : kRow);
+  }
 #undef CALL
 }
 template <int DT, bool LAYER, bool POST>

@@ -140,6 +140,29 @@ def test_rows(zt, rows, cols):
     _check_backward(zt, 403, rows, cols, "f32", True, True, "channel")
 
 
+# both sides of the lines where rows begin to share a wavefront, and where wide ones have other lanes or hold less
+LINES = [("f32", cols) for cols in (3, 63, 65, 127, 129, 4097, 8189, 8193, 12291, 16381, 16385)]
+LINES += [(dtype, cols) for dtype in ("bf16", "f16") for cols in (5, 127, 129, 255, 257, 8195, 12287, 12289, 16383, 16385)]
+
+
+@pytest.mark.parametrize("layer, post, gate", FORMS)
+@pytest.mark.parametrize("dtype, cols", LINES)
+def test_every_form_at_the_lines_between_layouts(zt, dtype, cols, layer, post, gate):
+    print("line", dtype, cols, layer, post, gate, flush=True)
+    _check_forward(zt, 420, 3, cols, dtype, layer, post, gate)
+    _check_backward(zt, 421, 3, cols, dtype, layer, post, gate)
+
+
+# more rows than workgroups, so that each adds up several
+@pytest.mark.parametrize("dtype, rows, cols", (("bf16", 13001, 100), ("f32", 12999, 50), ("f16", 6500, 200), ("f32", 6300, 101), ("bf16", 300, 5001), ("f32", 300, 5001),
+                                               ("f32", 270, 9000), ("f16", 300, 8200), ("bf16", 300, 12289), ("bf16", 270, 16400)))
+def test_workgroups_with_several_rows(zt, dtype, rows, cols):
+    print("several rows", dtype, rows, cols, flush=True)
+    _check_backward(zt, 422, rows, cols, dtype, False, True, "channel")
+    _check_backward(zt, 423, rows, cols, dtype, True, True, "channel")
+    _check_backward(zt, 424, rows, cols, dtype, True, False, "none")
+
+
 def test_rows_far_from_zero(zt):
     """A mean a hundred times the deviation: the deviation comes of what is left when the mean is taken away."""
     _check_forward(zt, 410, 6, 1537, "f32", True, True, "none", mean=200.0)
