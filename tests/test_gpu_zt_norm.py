@@ -255,6 +255,38 @@ def test_outputs_in_place_of_inputs(zt):
     assert torch.equal(dy2, want["x"]) and torch.equal(dh2, want["b"])
 
 
+@pytest.mark.parametrize("dtype, cols", (("f32", 3), ("bf16", 101), ("f32", 99), ("f16", 203), ("f32", 4999), ("bf16", 8203), ("f32", 9001), ("f16", 12299), ("bf16", 16397)))
+def test_strides_and_places_of_short_and_wide_rows(zt, dtype, cols):
+    print("places", dtype, cols, flush=True)
+    test_strides_and_places(zt, dtype, cols)
+
+
+@pytest.mark.parametrize("layer, post, gate", ((False, True, "channel"), (True, True, "channel"), (True, True, "full"), (True, False, "none"), (False, False, "channel")))
+@pytest.mark.parametrize("dtype, cols", (("bf16", 5), ("f32", 99), ("bf16", 203), ("f32", 1001), ("f16", 6147), ("f32", 4999), ("bf16", 8203), ("f32", 9001), ("f16", 12299),
+                                         ("f32", 16389), ("bf16", 16397)))
+def test_outputs_in_place_at_odd_widths(zt, dtype, cols, layer, post, gate):
+    """Where a row's last vector overlaps its neighbour, what it shares with it may have been overwritten by then."""
+    import torch
+    print("in place", dtype, cols, layer, post, gate, flush=True)
+    rows = 300 if cols < 1000 else 5
+    d, _ = _inputs(620, rows, cols, dtype, layer, post, gate)
+    form = _form(zt, d, layer, post, 0.7)
+    stats = torch.empty((rows, 4), device="cuda")
+    y, h = zt.zt_residual_norm(d["x"], d["b"], d_stats=stats, **form)
+    x2, b2 = d["x"].clone(), d["b"].clone()
+    zt.zt_residual_norm(x2, b2, d_y=x2, d_h=b2, **form)
+    assert torch.equal(x2, y) and torch.equal(b2, h)
+    x2 = d["x"].clone()
+    zt.zt_residual_norm(x2, d["b"], d_h=x2, want_y=False, **form)
+    assert torch.equal(x2, h)
+    want = zt.zt_residual_norm_backward(d["dy"], d["dh"], y, d["b"], stats, **form)
+    for dx_is, db_is in (("dy", "dh"), ("dh", None)):
+        t = {"dy": d["dy"].clone(), "dh": d["dh"].clone(), None: None}
+        got = zt.zt_residual_norm_backward(t["dy"], t["dh"], y, d["b"], stats, d_dx=t[dx_is], d_db=t[db_is], **form)
+        for k, v in want.items():
+            assert v is None or torch.equal(got[k], v), (dx_is, k)
+
+
 @pytest.mark.parametrize("cols", (300, 6144))
 def test_what_is_not_a_number_stays_in_its_row(zt, cols):
     import torch
