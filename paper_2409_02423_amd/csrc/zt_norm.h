@@ -13,15 +13,15 @@ namespace {
 
 // How a row lies over lanes.  A workgroup takes whole rows, one at a time; a lane has NV vectors of 16 bytes of a row, neighbouring
 // lanes neighbouring ones.  NV = 0 is the form for rows that registers do not hold: as many
-// vectors as it takes, operands loaded where they are used and the row's fp32 values in LDS.  NV = kShort16 and kShort32 are those for rows of
-// 16 and 32 vectors at most, which as many lanes take each, four or two rows to a wavefront; they may be shorter than a vector.
+// vectors as it takes, operands loaded where they are used and the row's fp32 values in LDS.  NV = kShort16, kShort32 and kShort64 are those for rows of
+// 16, 32 and 64 vectors at most, which as many lanes take each, four, two or one to a wavefront and 16, 8 or 4 to a workgroup; they may be shorter than a vector.
 //
 // So that every load is a whole one, a row's last vector is moved to end where the row does.  What it then shares with the one ahead of
 // it is not its own: it is loaded but counts for nothing and is not stored.  (Loading the last values one by one, in a branch of
 // their own, held up each row's first sum: 8192 x 4099 values in fp32 150 us forward, now 111.)  Which lane has which column does not depend on where
 // tensors lie, nor do the results, bit for bit.  (Vectors that start where memory is aligned to them made 8192 x 4099 in bf16 12 % faster, at that price.)
-constexpr int kShort16 = -1, kShort32 = -2;
-template <int NV> constexpr int kShortLanes = NV == kShort16 ? 16 : NV == kShort32 ? 32 : 0;   // of a row, where a workgroup has several
+constexpr int kShort16 = -1, kShort32 = -2, kShort64 = -3;
+template <int NV> constexpr int kShortLanes = NV == kShort16 ? 16 : NV == kShort32 ? 32 : NV == kShort64 ? 64 : 0;   // of a row, where a workgroup has several
 template <int NV> constexpr int kHeld = NV > 0 ? NV : 1;   // vectors that registers hold, if any
 
 template <int DT, int NV>
@@ -35,6 +35,7 @@ struct Lanes {
       lanes = kShortLanes<NV>;
       lane = threadIdx.x % kShortLanes<NV>;
       first = (blockIdx.x * blockDim.x + threadIdx.x) / kShortLanes<NV>;
+      if constexpr (NV == kShort64) first = __builtin_amdgcn_readfirstlane(first);
       step = gridDim.x * blockDim.x / kShortLanes<NV>;
     } else {
       lane = threadIdx.x;
@@ -194,7 +195,7 @@ struct Sums {
     if constexpr (NV < 0) {
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        v[k] = row_sum(v[k]);
+        v[k] = NV == kShort64 ? wave_sum(v[k]) : row_sum(v[k]);
         if constexpr (NV == kShort32) v[k] += __shfl_xor(v[k], 16);
       }
     } else {
@@ -215,11 +216,12 @@ struct Layout {
 };
 int vector_values(int dtype) { return dtype == ZC_F32 ? 4 : 8; }
 size_t row_vectors(size_t cols, int dtype) { return (cols + vector_values(dtype) - 1) / vector_values(dtype); }
-// Rows that leave most of a wavefront idle share one.  us in bf16 with a wavefront for each row and with this, forward and
-// backward: 262144 x 7 values 3066 and 38, 6226 and 80 (values of rows shorter than a vector were loaded one by one by the only lane that had any);
-// x 64 96 and 29, 252 and 53; 131072 x 129 65 and 37, 152 and 62; x 200 60 and 39, 148 and 65.
-bool short_rows(size_t vectors) { return vectors <= 32; }
-Layout short_layout(size_t vectors) { return vectors <= 16 ? Layout{kShort16, 256, 256, 16} : Layout{kShort32, 256, 256, 8}; }
+// Short rows share a workgroup, and those that would leave most of a wavefront idle a wavefront, too. us in bf16 with a workgroup of one
+// wavefront for each row and with this, forward and backward: 262144 x 7 values 3066 and 38, 6226 and 80 (values of rows shorter than a vector were loaded one by
+// one by the only lane that had any); x 64 96 and 29, 252 and 53; 131072 x 129 65 and 37, 152 and 62; x 200 60 and 39, 148 and 65; 65536 x 257 49 and 44, 86 and 69;
+// x 400 40 and 41, 78 and 65; x 512 48 and 47, 86 and 81.
+bool short_rows(size_t vectors) { return vectors <= 64; }
+Layout short_layout(size_t vectors) { return vectors <= 16 ? Layout{kShort16, 256, 256, 16} : vectors <= 32 ? Layout{kShort32, 256, 256, 8} : Layout{kShort64, 256, 256, 4}; }
 int lanes_for(size_t vectors, int each) { return (int)(((vectors + each - 1) / each + 63) / 64 * 64); }
 
 int check_form(const zt_residual* f) {

@@ -141,6 +141,7 @@ void launch(const NormArgs& a, const Layout& l, hipStream_t s) {
   switch (l.most * 8 + l.vectors) {
     case 256 * 8 + kShort16: CALL(kShort16, 256); break;
     case 256 * 8 + kShort32: CALL(kShort32, 256); break;
+    case 256 * 8 + kShort64: CALL(kShort64, 256); break;
     case 256 * 8 + 1: CALL(1, 256); break;
     case 256 * 8 + 2: CALL(2, 256); break;
     case 256 * 8 + 3: CALL(3, 256); break;

@@ -95,7 +95,7 @@ struct Columns {
         for (int j = 0; j < V; ++j) {
           float s = held[k][0][j];
           if constexpr (kLanes == 16) s += __shfl_xor(s, 16);
-          s += __shfl_xor(s, 32);
+          if constexpr (kLanes < 64) s += __shfl_xor(s, 32);
           if ((threadIdx.x & 63) < kLanes) parts[k][wave][at.lane][j] = s;
         }
       __syncthreads();
@@ -343,11 +343,12 @@ Layout backward_layout(const zt_residual& f) {
 }
 
 // Workgroups, each of which leaves one partial sum for each column: as few as keep memory busy.  us with 1, 2, 3, 4, 6, 8 and 12
-// a CU: 256 lanes (8192 x 2048 as above) 49.2, 45.3, 46.8, 52.8, 54.5, 57.0, 63.4; 128 lanes (16384 x 1024) 81.9, 56.1, 45.2, 48.5, 49.9, 57.4, 61.8; 64 lanes
-// (32768 x 512) 137, 87.0, 58.7, 50.3, 49.7, 50.7, 54.5; 512 and 768 lanes with 1 and 2 78.2 and 83.2, 115.7 and 123.5.
-// Short rows with 2, 3, 4 and 6: 262144 x 64 in bf16 57.1, 53.4, 50.4, 54.6; 131072 x 128 45.1, 45.0, 47.3, 50.1; x 200 65.6, 65.2, 70.7, 74.4.
-size_t backward_groups(size_t rows, const Layout& l) {
-  const size_t per_cu = l.vectors < 0 ? 3 : l.vectors == 0 || l.lanes > 256 ? 1 : l.lanes > 128 ? 2 : l.lanes > 64 ? 3 : 6;
+// a CU: 256 lanes (8192 x 2048 as above) 49.2, 45.3, 46.8, 52.8, 54.5, 57.0, 63.4; 128 lanes (16384 x 1024) 81.9, 56.1, 45.2, 48.5, 49.9, 57.4, 61.8; 512 and 768 lanes with 1 and 2 78.2 and 83.2, 115.7 and 123.5.
+// Short rows with 2, 3, 4 and 6: 262144 x 64 in bf16 57.1, 53.4, 50.4, 54.6; 131072 x 128 45.1, 45.0, 47.3, 50.1; x 200 65.6, 65.2, 70.7, 74.4; 65536 x 512
+// 78.3, 81.5, 88.1, 84.8; in fp32, whose vectors have half the sums and leave room for more, 262144 x 64 101, 81.3, 76.3, 93.0; 65536 x 256 113, 88.9, 79.3, 81.7.
+size_t backward_groups(const zt_residual& f, const Layout& l) {
+  const size_t rows = f.rows;
+  const size_t per_cu = l.vectors < 0 ? (f.dtype == ZC_F32 ? 4 : 3) : l.vectors == 0 || l.lanes > 256 ? 1 : l.lanes > 128 ? 2 : 3;
   const size_t groups = (rows + l.rows - 1) / l.rows;
   return groups < kCUs * per_cu ? groups : kCUs * per_cu;
 }
@@ -363,6 +364,7 @@ void launch(const BackwardArgs& a, const Layout& l, unsigned groups, hipStream_t
 #define CALL(NV, MOST, HOW) hipLaunchKernelGGL((norm_backward_kernel<DT, LAYER, POST, CHANNEL, NV, MOST, HOW>), dim3(groups), dim3(l.lanes), 0, s, a)
   if (l.vectors == kShort16) CALL(kShort16, 256, kAll);
   else if (l.vectors == kShort32) CALL(kShort32, 256, kAll);
+  else if (l.vectors == kShort64) CALL(kShort64, 256, kAll);
   else if (l.vectors == 1 && l.most == 256) CALL(1, 256, kAll);
   else if (l.vectors == 1) CALL(1, 768, kAll);
   else if (l.vectors == 2 && l.most == 512) CALL(2, 512, kAll);
@@ -395,7 +397,7 @@ extern "C" {
 size_t zt_residual_work_bytes(const struct zt_residual* form) {
   if (check_form(form) != ZC_OK || form->rows == 0 || form->cols == 0) return 0;
   const Layout l = backward_layout(*form);
-  return backward_groups(form->rows, l) * (size_t)sums_of(*form) * padded_cols(form->cols) * sizeof(float);
+  return backward_groups(*form, l) * (size_t)sums_of(*form) * padded_cols(form->cols) * sizeof(float);
 }
 
 int zt_residual_norm_backward(const struct zt_residual* form, const void* d_dy, const void* d_dh, const void* d_y, const void* d_b,
@@ -445,7 +447,7 @@ int zt_residual_norm_backward(const struct zt_residual* form, const void* d_dy, 
   a.scale = f.residual_scale;
   a.inv_cols = (float)(1.0 / (double)f.cols);
   const Layout l = backward_layout(f);
-  const size_t groups = backward_groups(f.rows, l);
+  const size_t groups = backward_groups(f, l);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (f.rows != 0) {
     if (f.dtype == ZC_F32) launch<kF32>(f, a, l, (unsigned)groups, s);

@@ -154,7 +154,7 @@ def test_every_form_at_the_lines_between_layouts(zt, dtype, cols, layer, post, g
 
 
 # more rows than workgroups, so that each adds up several
-@pytest.mark.parametrize("dtype, rows, cols", (("bf16", 13001, 100), ("f32", 12999, 50), ("f16", 6500, 200), ("f32", 6300, 101), ("bf16", 300, 5001), ("f32", 300, 5001),
+@pytest.mark.parametrize("dtype, rows, cols", (("bf16", 13001, 100), ("f32", 12999, 50), ("f16", 6500, 200), ("f32", 6300, 101), ("f16", 3200, 300), ("f32", 4200, 250), ("bf16", 300, 5001), ("f32", 300, 5001),
                                                ("f32", 270, 9000), ("f16", 300, 8200), ("bf16", 300, 12289), ("bf16", 270, 16400)))
 def test_workgroups_with_several_rows(zt, dtype, rows, cols):
     print("several rows", dtype, rows, cols, flush=True)
