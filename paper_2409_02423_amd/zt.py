@@ -307,7 +307,10 @@ def zt_clip(tensors, max_norm, scale=1.0, d_out=None, d_slots=None, d_norm=None,
 def zt_adamw(d_grad, d_param, d_m, d_v, lr, beta1, beta2, eps, weight_decay, step, d_half=None, d_slots=None, scale=1.0, max_norm=float("inf"),
              d_norm=None, stream=None):
     """One AdamW step on a shard, in place: d_param, d_m and d_v are fp32, d_grad any type, d_half (bfloat16 or float16) gets
-    the new parameters.  With d_slots (zt_sum_squares) the gradients are clipped to max_norm and the norm is returned."""
+    the new parameters.  With d_slots (zt_sum_squares) the gradients are clipped to max_norm and the norm is returned; a limit
+    without them is refused, since the norm to hold against it is that of all gradients and not of this shard's."""
+    if d_slots is None and max_norm != float("inf"):
+        raise ValueError("max_norm needs d_slots")
     device = _current(d_grad, "d_grad")
     n, code = d_grad.numel(), _DTYPES.get(d_grad.dtype)
     if code is None:

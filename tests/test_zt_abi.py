@@ -196,3 +196,11 @@ def test_binding_rejects_host_tensors_and_wrong_combinations():
             call()
     with pytest.raises(ValueError):
         zt.zt_sum_squares([], accumulate=True)
+
+
+def test_adamw_takes_no_limit_without_the_sum_of_squares():
+    """A limit that nothing is held against would leave the gradients as they are, and the step unguarded."""
+    t = torch.zeros(4)
+    for limit in (1.0, 1e30, float("nan")):
+        with pytest.raises(ValueError):
+            zt.zt_adamw(t, t, t, t, 1e-3, 0.9, 0.95, 1e-8, 0.0, 1, max_norm=limit)
