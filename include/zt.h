@@ -112,9 +112,11 @@ int zt_sum_squares(const void* const* d_in, const size_t* n, const int* dtype, i
  * multiplied by scale (1 / ranks for sums over ranks, 1 / loss scale).  scale > 0, finite. */
 int zt_norm(const double* d_slots, float scale, float* d_norm, void* stream);
 
-/* Clipping: d_out[i] = c * d_in[i] for every tensor, with norm as zt_norm gives it and
+/* Clipping: d_out[i] = c * d_in[i] for every tensor, with zt_norm's formula and
  *     c = scale                      if norm <= max_norm
  *     c = scale * max_norm / norm    otherwise (NaN if the norm is NaN).
+ * c is made in 64 bits, of the norm before it is rounded, and rounded to fp32: a norm that 64 bits
+ * hold and fp32 does not is clipped by as it is, although d_norm gets infinity.
  * max_norm > 0; infinity asks for no clipping.  In place with c = 1 nothing is written.  Tensor i is read as dtype_in[i] and written as
  * dtype_out[i]; d_out[i] may be d_in[i] if the types are the same, no other overlap.  d_norm
  * may be NULL. */
@@ -130,8 +132,8 @@ int zt_clip(const void* const* d_in, const size_t* n, const int* dtype_in, void*
  *
  * param, m and v are fp32, grad of type grad_dtype; d_half, if not NULL, gets the new
  * parameters rounded to half_dtype (ZC_BF16 or ZC_F16): the message of the parameter
- * all-gather.  If the norm is not finite nothing is changed, and d_half gets the old
- * parameters.  d_slots may be NULL: c = scale.  d_norm may be NULL.  No overlap.
+ * all-gather.  If the norm that d_norm gets (fp32) is not finite nothing is changed, and d_half gets the
+ * old parameters.  d_slots may be NULL: c = scale.  d_norm may be NULL.  No overlap.
  */
 struct zt_adamw_form {
   size_t n;

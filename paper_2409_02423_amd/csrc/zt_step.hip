@@ -255,7 +255,7 @@ __device__ __forceinline__ void adamw_tile(const AdamwArgs& a, size_t start, int
     const double norm = (double)a.scale * sqrt(slots_total(a.slots, buffer));
     if (a.norm_out && blockIdx.x == 0 && threadIdx.x == 0) a.norm_out[0] = (float)norm;
     factor = clip_factor(norm, a.scale, a.max_norm);
-    finite = norm < __builtin_inf();
+    finite = (float)norm < __builtin_inff();   // as it is reported: the caller learns from that whether there was a step
   }
   float g[kN], p[kN], m[kN], v[kN];
   rg.unpack(g);

@@ -292,3 +292,40 @@ def test_refusals_of_the_binding(zt):
         zt.zt_adamw(a, a.half(), a, a, 1e-3, 0.9, 0.95, 1e-8, 0.0, 1)
     with pytest.raises(zt.ZcError):
         zt.zt_adamw(a, a, a, a, 1e-3, 0.9, 0.95, 1e-8, 0.0, 0)
+
+
+@pytest.mark.parametrize("scale", (1.0, 0.5))
+def test_adamw_is_left_out_where_the_norm_it_reports_is_not_finite(zt, scale):
+    """70000 gradients of 3e38 have a norm that 64 bits hold and the reported value, of 32, does not: the caller is told that the step was
+    left out."""
+    import torch
+    g = torch.full((70000,), 3e38, device="cuda")
+    p, m = _tensors(50, [70000, 70000], "f32")
+    v = m ** 2
+    kept = [t.clone() for t in (p, m, v)]
+    h = torch.zeros(70000, dtype=torch.bfloat16, device="cuda")
+    norm = zt.zt_adamw(g, p, m, v, 1e-2, 0.9, 0.95, 1e-8, 0.1, 1, d_half=h, d_slots=zt.zt_sum_squares([g]), scale=scale, max_norm=1.0)
+    assert float(norm) == math.inf
+    assert all(torch.equal(a, b) for a, b in zip((p, m, v), kept)) and torch.equal(h, p.bfloat16())
+
+
+def test_adamw_is_taken_at_the_largest_norms(zt):
+    """Four gradients of 1.6e38: a norm of 3.2e38 is finite."""
+    import torch
+    g = torch.full((4,), 1.6e38, device="cuda")
+    p, m, v = torch.ones(4, device="cuda"), torch.zeros(4, device="cuda"), torch.zeros(4, device="cuda")
+    norm = zt.zt_adamw(g, p, m, v, 1e-2, 0.9, 0.95, 1e-8, 0.0, 1, d_slots=zt.zt_sum_squares([g]), max_norm=1.0)
+    assert abs(float(norm) / 3.2e38 - 1) < 1e-6
+    assert np.allclose(m.cpu().numpy(), 0.1 * 0.5, rtol=1e-6) and np.allclose(p.cpu().numpy(), 1 - 1e-2, rtol=1e-6)
+
+
+def test_clip_by_a_norm_that_32_bits_do_not_hold(zt):
+    """The factor is made of the norm in 64 bits: 70000 gradients of 3e38 are clipped to 1 although the norm is reported as infinite."""
+    import torch
+    t = torch.full((70000,), 3e38, device="cuda")
+    norm = zt.zt_clip([t], 1.0)
+    assert float(norm) == math.inf
+    # the factor is below fp32's normal numbers, 1 / 7.9e40: 2^-149 / 2 off at most, which 3e38 values of the same size make 2e-7 of them
+    want = 1 / math.sqrt(70000)
+    print("clipped", float(t[0]), "want", want, flush=True)
+    assert bool(((t.double() - want).abs() <= 3e38 * 2.0 ** -150 + want * 2.0 ** -23).all())
