@@ -15,8 +15,8 @@
  *     frees nor keeps them; arrays of pointers are HOST arrays, read before the call returns.
  *   - `stream` is a hipStream_t as void*; calls enqueue kernels on it and return without
  *     synchronising.  They only launch kernels, so sequences of them can be captured in a HIP
- *     graph.  Calls on different streams may run concurrently where they share no output and
- *     no workspace.
+ *     graph; its replays repeat the numbers that the calls were given (zt_adamw: see d_state).
+ *     Calls on different streams may run concurrently where they share no output and no workspace.
  *   - Return value: ZC_OK or a negative code of include/zc.h; on error nothing is launched.
  *   - dtype: enum zc_dtype.  Sums, statistics and products are held in fp32 (sums of squares
  *     in 64 bits); a value is rounded once, to the nearest with ties to even, where it is
@@ -134,6 +134,13 @@ int zt_clip(const void* const* d_in, const size_t* n, const int* dtype_in, void*
  * parameters rounded to half_dtype (ZC_BF16 or ZC_F16): the message of the parameter
  * all-gather.  If the norm that d_norm gets (fp32) is not finite nothing is changed, and d_half gets the
  * old parameters.  d_slots may be NULL: c = scale.  d_norm may be NULL.  No overlap.
+ *
+ * step and lr are numbers of the call: one that is captured in a graph repeats that one step in each
+ * replay, and whether a step was left out is known to the GPU alone.  With d_state (device, 4 values,
+ * aligned to 16) the call counts for itself: d_state[0] is the number of steps taken before it (>= 0),
+ * to which it adds one unless it leaves the step out, d_state[1] the learning rate (>= 0), and it writes
+ * what it needs into the other two.  step and lr of the form are then not read.  Each shard has a
+ * state of its own.  One more small kernel is launched.
  */
 struct zt_adamw_form {
   size_t n;
@@ -141,6 +148,7 @@ struct zt_adamw_form {
   long long step;               /* >= 1, counting this one */
   double lr, beta1, beta2, eps, weight_decay;   /* lr, eps, weight_decay >= 0; 0 <= beta < 1 */
   float scale, max_norm;        /* as in zt_clip; max_norm is read if d_slots is not NULL */
+  double* d_state;              /* NULL, or in place of step and lr */
 };
 int zt_adamw(const struct zt_adamw_form* form, const void* d_grad, const double* d_slots, float* d_param, float* d_m,
              float* d_v, void* d_half, float* d_norm, void* stream);

@@ -35,7 +35,7 @@ class AdamwForm(ctypes.Structure):
     """struct zt_adamw_form"""
     _fields_ = [("n", ctypes.c_size_t), ("grad_dtype", ctypes.c_int), ("half_dtype", ctypes.c_int), ("step", ctypes.c_longlong),
                 ("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
-                ("weight_decay", ctypes.c_double), ("scale", ctypes.c_float), ("max_norm", ctypes.c_float)]
+                ("weight_decay", ctypes.c_double), ("scale", ctypes.c_float), ("max_norm", ctypes.c_float), ("d_state", ctypes.c_void_p)]
 
 
 _lib = None
@@ -305,10 +305,15 @@ def zt_clip(tensors, max_norm, scale=1.0, d_out=None, d_slots=None, d_norm=None,
 
 
 def zt_adamw(d_grad, d_param, d_m, d_v, lr, beta1, beta2, eps, weight_decay, step, d_half=None, d_slots=None, scale=1.0, max_norm=float("inf"),
-             d_norm=None, stream=None):
+             d_norm=None, stream=None, d_state=None):
     """One AdamW step on a shard, in place: d_param, d_m and d_v are fp32, d_grad any type, d_half (bfloat16 or float16) gets
     the new parameters.  With d_slots (zt_sum_squares) the gradients are clipped to max_norm and the norm is returned; a limit
-    without them is refused, since the norm to hold against it is that of all gradients and not of this shard's."""
+    without them is refused, since the norm to hold against it is that of all gradients and not of this shard's.
+
+    lr and step are the call's: captured in a graph, it takes that step again in each replay.  With d_state, a float64 tensor of 4
+    values [steps taken, learning rate, 0, 0], they are None; the call counts the step on the GPU, and does not where it leaves it out."""
+    if (lr is None) != (d_state is not None) or (step is None) != (d_state is not None):
+        raise ValueError("lr and step, or d_state in their place")
     if d_slots is None and max_norm != float("inf"):
         raise ValueError("max_norm needs d_slots")
     device = _current(d_grad, "d_grad")
@@ -329,6 +334,9 @@ def zt_adamw(d_grad, d_param, d_m, d_v, lr, beta1, beta2, eps, weight_decay, ste
         d_norm, norm = _norm(d_norm, device, stream)
     elif d_norm is not None:
         raise ValueError("d_norm needs d_slots")
-    form = AdamwForm(n, code, half_code, step, lr, beta1, beta2, eps, weight_decay, scale, max_norm)
+    if d_state is None:
+        form = AdamwForm(n, code, half_code, step, lr, beta1, beta2, eps, weight_decay, scale, max_norm, None)
+    else:
+        form = AdamwForm(n, code, half_code, 0, 0.0, beta1, beta2, eps, weight_decay, scale, max_norm, _flat(d_state, "d_state", torch.float64, device, 4))
     _check(lib().zt_adamw(form, grad, slots, param, m, v, half, norm, zc._stream_handle(stream)), "zt_adamw")
     return d_norm

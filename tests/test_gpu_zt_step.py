@@ -329,3 +329,106 @@ def test_clip_by_a_norm_that_32_bits_do_not_hold(zt):
     want = 1 / math.sqrt(70000)
     print("clipped", float(t[0]), "want", want, flush=True)
     assert bool(((t.double() - want).abs() <= 3e38 * 2.0 ** -150 + want * 2.0 ** -23).all())
+
+
+def _state(lr, steps=0):
+    import torch
+    return torch.tensor([steps, lr, 0.0, 0.0], dtype=torch.float64, device="cuda")
+
+
+@pytest.mark.parametrize("n, grad, half, clip", [(n, g, h, c) for n in (1, 5, 1025, 70001) for g, h in (("f32", "none"), ("bf16", "bf16"), ("f16", "f16")) for c in (True, False)])
+def test_adamw_that_counts_its_steps(zt, n, grad, half, clip):
+    """Steps with the count and the learning rate on the GPU, one of them left out and the rate changed on the way, each against the formula
+    in 64 bits from where the one before it ended."""
+    import torch
+    p, m = _tensors(60, [n, n], "f32", std=0.5)
+    v = _tensors(61, [n], "f32", std=0.3)[0] ** 2
+    h = None if half == "none" else torch.empty(n, dtype=_dtypes()[half], device="cuda")
+    fixed = dict(beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.1)
+    state, taken = _state(3e-3), 0
+    for turn, lr in enumerate((3e-3, 3e-3, 1e-3, 1e-3, 5e-4)):
+        g = _tensors(62 + turn, [n], grad, std=0.2)[0]
+        bad = clip and turn == 2
+        if bad:
+            g[n // 2] = math.inf
+        before = [t.double().cpu().numpy() for t in (g, p, m, v)]
+        kept = [t.clone() for t in (p, m, v)]
+        state[1] = lr
+        limit = dict(d_slots=zt.zt_sum_squares([g]), max_norm=0.75) if clip else {}
+        norm = zt.zt_adamw(g, p, m, v, None, step=None, d_state=state, d_half=h, scale=0.5, **limit, **fixed)
+        taken += 0 if bad else 1
+        assert float(state[0]) == taken and float(state[1]) == lr
+        if bad:
+            assert float(norm) == math.inf and all(torch.equal(a, b) for a, b in zip((p, m, v), kept))
+        else:
+            factor = 0.5
+            if clip:
+                exact_norm = 0.5 * math.sqrt(_squares([g]))
+                assert abs(float(norm) - exact_norm) <= 2.0 ** -23 * exact_norm
+                factor = zt_ref.clip_factor(exact_norm, 0.5, 0.75)
+            want, bound = zt_ref.adamw(*before, factor, lr=lr, step=taken, **fixed)
+            for name, got, w, e in zip(("param", "m", "v"), (p, m, v), want, bound):
+                off = np.abs(got.double().cpu().numpy() - w)
+                assert np.all(off <= e), (turn, name, float((off / e).max()))
+        if h is not None:
+            assert torch.equal(h, p.to(h.dtype))
+
+
+def test_a_captured_adamw_goes_on_from_step_to_step(zt):
+    """Replays of one graph, a step among them that is left out, against eager calls with the same state, bit for bit, and against calls that
+    are given the numbers of the steps."""
+    import torch
+    n, fixed = 60001, dict(beta1=0.9, beta2=0.95, eps=1e-8, weight_decay=0.1)
+    grads = [_tensors(70 + i, [n], "f32")[0] for i in range(7)]
+    grads[3][n - 1] = math.nan
+    start = _tensors(80, [n, n], "f32")
+
+    def fresh():
+        return start[0].clone(), torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+
+    def step(g, t, norm, slots, stream=None, **numbers):
+        zt.zt_sum_squares([g], d_slots=slots, stream=stream)
+        zt.zt_adamw(g, *t, **numbers, d_slots=slots, max_norm=1.0, d_norm=norm, stream=stream, **fixed)
+
+    def scratch():
+        return torch.empty(1, device="cuda"), torch.empty(zt.ZT_SLOTS, dtype=torch.float64, device="cuda")
+
+    eager, state, out = fresh(), _state(1e-2), scratch()
+    numbered, count, out2 = fresh(), 0, scratch()
+    after = []
+    for i, g in enumerate(grads):
+        step(g, eager, *out, lr=None, step=None, d_state=state)
+        count += 0 if i == 3 else 1
+        step(g, numbered, *out2, lr=1e-2, step=max(count, 1))
+        torch.cuda.synchronize()
+        assert float(state[0]) == count
+        # the corrections are rounded once more or less: a step of fp32 of the update, and of the parameter
+        assert float((eager[0] - numbered[0]).abs().max()) <= 8 * (i + 1) * (1e-2 * 2.0 ** -22 + 8 * 2.0 ** -24)
+        after.append([t.clone() for t in (*eager, state, out[0])])
+    x, live, state, (norm, slots), side = torch.empty(n, device="cuda"), fresh(), _state(1e-2), scratch(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step(x, live, norm, slots, lr=None, step=None, d_state=state)
+    for i, g in enumerate(grads):
+        print("graph replay", i, flush=True)
+        x.copy_(g)
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, want in zip((*live, state, norm), after[i]):
+            assert torch.equal(got, want) or (i == 3 and bool(got.isnan().all()) and bool(want.isnan().all())), i
+
+
+def test_an_empty_shard_counts_its_steps(zt):
+    import torch
+    e, state = torch.empty(0, device="cuda"), _state(1e-2, 4)
+    g = torch.ones(16, device="cuda")
+    norm = zt.zt_adamw(e, e, e, e, None, 0.9, 0.95, 1e-8, 0.0, None, d_slots=zt.zt_sum_squares([g]), max_norm=1.0, d_state=state)
+    assert float(norm) == 4.0 and float(state[0]) == 5.0
+    g[3] = math.inf
+    norm = zt.zt_adamw(e, e, e, e, None, 0.9, 0.95, 1e-8, 0.0, None, d_slots=zt.zt_sum_squares([g]), max_norm=1.0, d_state=state)
+    assert float(norm) == math.inf and float(state[0]) == 5.0
+    with pytest.raises(TypeError):
+        zt.zt_adamw(g, g, g, g, None, 0.9, 0.95, 1e-8, 0.0, None, d_state=torch.zeros(4, device="cuda"))
+    with pytest.raises(ValueError):
+        zt.zt_adamw(g, g, g, g, None, 0.9, 0.95, 1e-8, 0.0, None, d_state=torch.zeros(3, dtype=torch.float64, device="cuda"))

@@ -204,3 +204,15 @@ def test_adamw_takes_no_limit_without_the_sum_of_squares():
     for limit in (1.0, 1e30, float("nan")):
         with pytest.raises(ValueError):
             zt.zt_adamw(t, t, t, t, 1e-3, 0.9, 0.95, 1e-8, 0.0, 1, max_norm=limit)
+
+
+def test_adamw_with_its_state_on_the_gpu_takes_no_numbers_in_its_place():
+    L = zt.lib()
+    good = dict(n=8, grad_dtype=zc.ZC_F32, beta1=0.9, beta2=0.95, eps=1e-8, weight_decay=0.1, scale=1.0, max_norm=1.0)
+    for change, code in ((dict(d_state=0x10008), zc.ZC_ERR_ALIGN), (dict(d_state=GOOD, beta1=1.0), zt.ZC_ERR_ARG), (dict(d_state=GOOD, eps=-1.0), zt.ZC_ERR_ARG),
+                         (dict(d_state=None, step=0), zt.ZC_ERR_ARG), (dict(d_state=None, step=1, lr=-1.0), zt.ZC_ERR_ARG)):
+        assert L.zt_adamw(zt.AdamwForm(**dict(good, **change)), GOOD, GOOD, GOOD, GOOD, GOOD, None, None, None) == code, change
+    t = torch.zeros(4)
+    for lr, step, state in ((1e-3, 1, t), (None, 1, t), (1e-3, None, t), (None, None, None), (None, 1, None), (1e-3, None, None)):
+        with pytest.raises(ValueError):
+            zt.zt_adamw(t, t, t, t, lr, 0.9, 0.95, 1e-8, 0.0, step, d_state=state)
