@@ -466,3 +466,21 @@ def test_refusals_of_the_binding(zt):
         zt.zt_residual_norm(torch.zeros((1, zt.ZT_MAX_COLS + 1), device="cuda"))
     with pytest.raises(ValueError):
         zt.zt_residual_norm_backward(x, x, x, x, torch.zeros(3, device="cuda"))
+
+
+def test_sums_over_rows_lose_no_more_than_a_tree_does(zt):
+    """One row with gradient 1 and 511 with 2^-28, each in a workgroup of its own: added one after the other, what is small would be lost
+    64 times over.  Eight partial sums a lane, then a tree of 64: no term goes through more than 13 additions."""
+    import torch
+    rows, cols = 512, 516
+    print("sums over rows", rows, cols, flush=True)
+    dh = torch.full((rows, cols), 2.0 ** -28, device="cuda")
+    dh[0] = 1.0
+    y, stats = torch.ones_like(dh), torch.tensor([0.0, 1.0, 0.0, 1.0], device="cuda").expand(rows, 4).contiguous()
+    weight = torch.ones(cols, device="cuda")
+    for kind, bias in ((zt.ZT_RMS, None), (zt.ZT_LAYER, torch.zeros(cols, device="cuda"))):
+        got = zt.zt_residual_norm_backward(None, dh, y, None, stats, kind=kind, pre_weight=weight, pre_bias=bias)
+        want = 1.0 + 511 * 2.0 ** -28
+        for name in ("pre_weight", "pre_bias"):
+            if got[name] is not None:
+                assert float((got[name].double() - want).abs().max()) <= 13 * 2.0 ** -24 * want, name
