@@ -484,3 +484,65 @@ def test_sums_over_rows_lose_no_more_than_a_tree_does(zt):
         for name in ("pre_weight", "pre_bias"):
             if got[name] is not None:
                 assert float((got[name].double() - want).abs().max()) <= 13 * 2.0 ** -24 * want, name
+
+
+# a form for each way in which the backward kernel lays rows out and holds them, with the sums that make it so
+LAYOUTS = [("bf16", 5, 40), ("f32", 100, 40), ("bf16", 500, 12), ("f16", 1000, 5), ("bf16", 5003, 5), ("f16", 8191, 5), ("f32", 4099, 5), ("bf16", 12001, 4),
+           ("f16", 16381, 4), ("f32", 8191, 4), ("f32", 16381, 3), ("f32", 16390, 3), ("bf16", 16397, 3)]
+
+
+@pytest.mark.parametrize("layer, post, gate", ((False, True, "channel"), (True, True, "channel"), (True, True, "full"), (False, False, "full"), (True, False, "none")))
+@pytest.mark.parametrize("dtype, cols, rows", LAYOUTS)
+def test_outputs_that_are_not_wanted(zt, dtype, cols, rows, layer, post, gate):
+    """The C call with each output left out in turn, and with all of them: the others are what they are with all of them, bit for bit, and
+    a full gate's gradient may be a slice of wider rows."""
+    import ctypes
+    import torch
+    print("outputs", dtype, cols, layer, post, gate, flush=True)
+    d, h = _inputs(630, rows, cols, dtype, layer, post, gate)
+    stats = _stats_of(h, layer, post, h["x"])
+    form = zt.Residual(rows=rows, cols=cols, dtype=zt._DTYPES[_torch_dtype(dtype)], kind=_kind(zt, layer), post=int(post),
+                       gate={"none": zt.ZT_GATE_NONE, "channel": zt.ZT_GATE_CHANNEL, "full": zt.ZT_GATE_FULL}[gate], residual_scale=0.7, eps=0.0)
+    wide = cols + 5
+    if gate == "full":
+        form.stride_dgate = wide
+    size = zt.lib().zt_residual_work_bytes(form)
+    work = torch.empty(size, dtype=torch.uint8, device="cuda")
+    names = ["x", "b"] + ["gate"] * (gate != "none") + ["pre_weight"] + ["pre_bias"] * layer + ["post_weight"] * post + ["post_bias"] * (layer and post)
+
+    def call(without):
+        out = {}
+        for k in names:
+            if k in without:
+                continue
+            if k in ("x", "b"):
+                out[k] = torch.full((rows, cols), 7.0, dtype=d["x"].dtype, device="cuda")
+            elif k == "gate" and gate == "full":
+                out[k] = torch.full((rows, wide), 7.0, dtype=d["x"].dtype, device="cuda")
+            else:
+                out[k] = torch.full((cols,), 7.0, device="cuda")
+
+        def at(t):
+            return None if t is None else t.data_ptr()
+
+        dgate = out.get("gate")
+        if dgate is not None and gate == "full":
+            dgate = dgate[:, 2:2 + cols]
+        rc = zt.lib().zt_residual_norm_backward(form, at(d["dy"]), at(d["dh"]), at(d["x"]), at(d["b"]), at(d["gate"]), at(d["pre_weight"]), at(d["post_weight"]),
+                                                at(d["post_bias"]), at(stats), at(out.get("x")), at(out.get("b")), at(dgate), at(out.get("pre_weight")),
+                                                at(out.get("pre_bias")), at(out.get("post_weight")), at(out.get("post_bias")), at(work), size,
+                                                ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
+        assert rc == 0
+        return out
+
+    want = call(())
+    through = zt.zt_residual_norm_backward(d["dy"], d["dh"], d["x"], d["b"], stats, **_form(zt, d, layer, post, 0.7))
+    for k, t in want.items():
+        if k == "gate" and gate == "full":
+            assert bool((t[:, :2] == 7).all()) and bool((t[:, 2 + cols:] == 7).all())
+            t = t[:, 2:2 + cols]
+        assert torch.equal(t, through[k]), k
+    for without in [(k,) for k in names] + [tuple(names), ("x", "b"), tuple(k for k in names if k not in ("x", "b"))]:
+        got = call(without)
+        for k, t in got.items():
+            assert torch.equal(t, want[k]), (without, k)
