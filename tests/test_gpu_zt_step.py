@@ -432,3 +432,28 @@ def test_an_empty_shard_counts_its_steps(zt):
         zt.zt_adamw(g, g, g, g, None, 0.9, 0.95, 1e-8, 0.0, None, d_state=torch.zeros(4, device="cuda"))
     with pytest.raises(ValueError):
         zt.zt_adamw(g, g, g, g, None, 0.9, 0.95, 1e-8, 0.0, None, d_state=torch.zeros(3, dtype=torch.float64, device="cuda"))
+
+
+@pytest.mark.parametrize("place", ("apart", "in place", "bf16"))
+def test_what_clipping_writes_where_the_norm_is_not_finite(zt, place):
+    """scale * max_norm / norm of an infinite norm is 0, which makes NaN of the infinite value alone; of a norm that is NaN, NaN of all."""
+    import torch
+    for bad in (math.inf, -math.inf, math.nan):
+        tensors = _tensors(2, [5000, 20001], "f32")
+        tensors[1][19999] = bad
+        out = tensors if place == "in place" else [torch.full_like(t, 7.0, dtype=torch.bfloat16 if place == "bf16" else None) for t in tensors]
+        norm = zt.zt_clip(tensors, 1.0, scale=0.5, d_out=out)
+        if math.isnan(bad):
+            assert math.isnan(float(norm)) and all(bool(o.isnan().all()) for o in out)
+        else:
+            assert float(norm) == math.inf
+            assert bool(out[1][19999].isnan()) and sum(int((o == 0).sum()) for o in out) == 25000
+        # no limit: scale alone, whatever the norm (NaN is not below it)
+        tensors = _tensors(2, [5000, 20001], "f32")
+        tensors[1][19999] = bad
+        want = [0.5 * t for t in tensors]
+        zt.zt_clip(tensors, math.inf, scale=0.5)
+        if math.isnan(bad):
+            assert all(bool(t.isnan().all()) for t in tensors)
+        else:
+            assert all(torch.equal(a, b) for a, b in zip(tensors, want))
