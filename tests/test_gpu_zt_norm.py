@@ -546,3 +546,22 @@ def test_outputs_that_are_not_wanted(zt, dtype, cols, rows, layer, post, gate):
         got = call(without)
         for k, t in got.items():
             assert torch.equal(t, want[k]), (without, k)
+
+
+def test_sums_over_more_rows_than_a_grid_has(zt):
+    """2^21 + 77 short rows, 16 to a workgroup, 768 workgroups.  A lane's 171 rows, each one multiplication and addition, and the two that
+    make the normed value; 4 additions over a workgroup's lanes, 11 of partial sums, 6 in the tree over them: 194 roundings at most."""
+    import torch
+    rows, cols = (1 << 21) + 77, 16
+    print("sums over rows", rows, flush=True)
+    g = torch.Generator(device="cuda").manual_seed(14)
+    y, dh = (torch.randn((rows, cols), generator=g, device="cuda").bfloat16() for _ in range(2))
+    stats = torch.rand((rows, 4), generator=g, device="cuda") + 0.5
+    stats[:, 2] -= 1.0
+    weight = torch.ones(cols, device="cuda").bfloat16()
+    got = zt.zt_residual_norm_backward(None, dh, y, None, stats, kind=zt.ZT_LAYER, pre_weight=weight, pre_bias=weight)
+    unit = (y.double() - stats[:, 2:3].double()) * stats[:, 3:4].double()
+    for name, terms in (("pre_weight", dh.double() * unit), ("pre_bias", dh.double())):
+        off, magnitude = (got[name].double() - terms.sum(0)).abs(), terms.abs().sum(0)
+        print(name, float((off / magnitude).max() / 2.0 ** -24), "roundings", flush=True)
+        assert bool((off <= 195 * 2.0 ** -24 * magnitude).all()), name
