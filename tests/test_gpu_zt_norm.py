@@ -548,16 +548,20 @@ def test_outputs_that_are_not_wanted(zt, dtype, cols, rows, layer, post, gate):
             assert torch.equal(t, want[k]), (without, k)
 
 
-def test_sums_over_more_rows_than_a_grid_has(zt):
+@pytest.mark.parametrize("values", ("random", "the same"))
+def test_sums_over_more_rows_than_a_grid_has(zt, values):
     """2^21 + 77 short rows, 16 to a workgroup, 768 workgroups.  A lane's 171 rows, each one multiplication and addition, and the two that
-    make the normed value; 4 additions over a workgroup's lanes, 11 of partial sums, 6 in the tree over them: 194 roundings at most."""
+    make the normed value; 4 additions over a workgroup's lanes, 11 of partial sums, 6 in the tree over them: 194 roundings at most.
+    Rows that are all the same one make roundings that all go the same way."""
     import torch
     rows, cols = (1 << 21) + 77, 16
-    print("sums over rows", rows, flush=True)
+    print("sums over rows", rows, values, flush=True)
     g = torch.Generator(device="cuda").manual_seed(14)
     y, dh = (torch.randn((rows, cols), generator=g, device="cuda").bfloat16() for _ in range(2))
     stats = torch.rand((rows, 4), generator=g, device="cuda") + 0.5
     stats[:, 2] -= 1.0
+    if values == "the same":
+        y, dh, stats = (t[:1].expand(t.shape).contiguous() for t in (y, dh, stats))
     weight = torch.ones(cols, device="cuda").bfloat16()
     got = zt.zt_residual_norm_backward(None, dh, y, None, stats, kind=zt.ZT_LAYER, pre_weight=weight, pre_bias=weight)
     unit = (y.double() - stats[:, 2:3].double()) * stats[:, 3:4].double()
