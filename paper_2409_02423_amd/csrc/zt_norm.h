@@ -145,15 +145,15 @@ struct Operand {
   }
 };
 
-// A row's fp32 values: in registers, or in LDS, where a lane reads only what it has written.
-template <int DT, int NV, bool HOLD = (NV != 0)>
+// A row's fp32 values: in registers, or in LDS, where a lane reads only what it has written (of MOST lanes at most).
+template <int DT, int NV, int MOST, bool HOLD = (NV != 0)>
 struct Values {
   static constexpr int V = kVec<DT>;
   float held[kHeld<NV>][V];
   float4* lds;
   __device__ __forceinline__ Values() {
     if constexpr (!HOLD) {
-      __shared__ float4 row[NV > 0 ? 1024 * NV * V / 4 : ZT_MAX_COLS / 4];
+      __shared__ float4 row[NV > 0 ? MOST * NV * V / 4 : ZT_MAX_COLS / 4];
       lds = row;
     }
   }

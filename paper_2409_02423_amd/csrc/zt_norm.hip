@@ -23,8 +23,8 @@ struct NormArgs {
 };
 
 // Takes the mean from a row's values (with LAYER); its 1 / deviation.
-template <int DT, bool LAYER, int NV>
-__device__ __forceinline__ void centre(Values<DT, NV>& values, const Lanes<DT, NV>& at, Sums<1, NV>& sums, float inv_cols, float eps, float& mean, float& r) {
+template <int DT, bool LAYER, int NV, int MOST>
+__device__ __forceinline__ void centre(Values<DT, NV, MOST>& values, const Lanes<DT, NV>& at, Sums<1, NV>& sums, float inv_cols, float eps, float& mean, float& r) {
   constexpr int V = kVec<DT>;
   float s[1] = {0.0f};
   mean = 0.0f;
@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(MOST) norm_kernel(NormArgs a) {
   const Lanes<DT, NV> at(a.cols);
   const size_t row = at.first;
   if (NV < 0 && row >= a.rows) return;
-  Values<DT, NV> values;
+  Values<DT, NV, MOST> values;
   Operand<DT, NV> pre_w, pre_c, post_w, post_c, gate, x, b;
   x.open(at, a.x + row * a.sx);
   b.open(at, a.b ? a.b + row * a.sb : nullptr);

@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(MOST) norm_backward_kernel(BackwardArgs a) {
   __shared__ float buffers[2][K][kMostWaves];
   Sums<K, NV> sums{buffers};
   const Lanes<DT, NV> at(a.cols);
-  Values<DT, NV, HOLD> values;   // the gradient of y, then of z
+  Values<DT, NV, MOST, HOLD> values;   // the gradient of y, then of z
   Operand<DT, NV, HOLD> pre_w, post_w, post_c;
   const auto open_weights = [&] {
     pre_w.open(at, a.pre_w, 1.0f);

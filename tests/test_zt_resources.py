@@ -52,3 +52,17 @@ def test_scalar_loads_add_up_whole_words(assembly):
         if m:
             written[m.group(1)] = line
     assert loads > 0
+
+
+def test_rows_in_lds_take_what_a_workgroup_has_of_them(assembly):
+    """Where a row's values lie in LDS the backward kernel asks for its workgroup's lanes, 16-byte vectors as fp32 for each, and little beside."""
+    kernels = re.findall(r"\.amdhsa_kernel (\S*norm_backward_kernel\S+)\n(.*?)\.end_amdhsa_kernel", assembly["zt_norm_backward.hip"], flags=re.S)
+    seen = 0
+    for name, meta in kernels:
+        # type, LayerNorm, post, channel gate, vectors a lane (n..: short rows; 0: any width), lanes, what registers hold (2: all)
+        dtype, post, vectors, most, hold = re.search(r"ILi(\d)ELb\dELb(\d)ELb\dELi(n?\d+)ELi(\d+)EL\S*HoldE(\d)E", name).groups()
+        if post == "0" or hold == "2" or vectors == "0" or vectors.startswith("n"):
+            continue
+        seen += 1
+        assert int(re.search(r"\.amdhsa_group_segment_fixed_size (\d+)", meta).group(1)) <= int(most) * int(vectors) * (4 if dtype == "0" else 8) * 4 + 1024, name
+    assert seen >= 12
