@@ -125,6 +125,8 @@ __global__ void __launch_bounds__(MOST) norm_kernel(NormArgs a) {
 // vectors a lane: 8192 x 1500 in bf16 18.4, 22.8, 22.0, 29.2 and 33.1 (3, 2, 1, 1 and 1 wavefronts); x 2561 44.4, 36.8, 37.5, 43.7, 58.7 (6, 3, 2, 2, 2);
 // x 4099 84.7, 68.7, 61.8, 74.4, 74.0 (9, 5, 3, 3, 2); x 6144 74.1, 72.9, 69.8, 74.6, 93.2 (12, 6, 4, 3, 3); 4000 x 4099 in fp32, a gate for each
 // value, 2 to 5 vectors 78.1, 82.9, 90.1, 64.2 (9, 6, 5, 4).
+// Rows of more than 2048 vectors have 16 wavefronts and lie in LDS, one workgroup a CU: 4096 x 8193 in fp32 133 us, 4.0 TB/s (x 8192, in registers, 100);
+// x 12288 165, 4.9; 2048 x 16391 in bf16 93, 2.9 (x 16384 53); x 20480 84, 4.0; x 32768 119, 4.5.
 Layout forward_layout(size_t cols, int dtype) {
   const size_t vectors = row_vectors(cols, dtype);
   if (short_rows(vectors)) return short_layout(vectors);

@@ -6,8 +6,8 @@
 // launches.  The sum of squares is left as one double per workgroup of the first pass (ZT_SLOTS of them), which every workgroup of the
 // second pass adds up for itself, in the same order, while its values are under way: no launch in between, and no atomics.
 //
-// What they reach, in bytes read and written: sum of squares 6.2 TB/s (2.3e8 fp32 values in 147 us), clipping 6.6 (272 us), AdamW 5.9 to 6.2
-// (1.5e8 parameters with fp32 gradients and a bf16 copy, 730 to 770 us by card).  The second pass has one tile or chunk for each workgroup and no loop (AdamW
+// What they reach, in bytes read and written: sum of squares 6.2 TB/s (2.3e8 fp32 values in 147 us), clipping 6.6 (272 us), AdamW 5.8 to 6.2
+// (1.5e8 parameters with fp32 gradients and a bf16 copy, 720 to 770 us by card).  The second pass has one tile or chunk for each workgroup and no loop (AdamW
 // in a loop with 2048 workgroups 1007 us, without 830), and asks for its values as ones that do not come again (nontemporal: 808 in that measurement,
 // scaling 212 to 188); the first does not, so that what fits the last-level cache is there for the second (2.5e7 fp32 values, both passes, 47 us with
 // nontemporal loads in the first, 38 without).
