@@ -226,7 +226,7 @@ def run(s):
         loss, lse = ze.ze_join_loss(s["stats"], s["labels"])
         return {"loss": loss, "lse": lse}
     d_hidden, d_weight = ze.ze_vocab_loss_backward(s["hidden"], s["weight"], s["labels"], s["lse"], s["d_loss"], first=s["first"], scale=s["scale"],
-                                                   d_dhidden=s["d_hidden"], d_dweight=s["d_weight"])
+                                                   d_dhidden=s["d_hidden"], d_dtable=s["d_weight"])
     return {"hidden": d_hidden, "weight": d_weight}
 
 
