@@ -1,0 +1,41 @@
+// ze_host.h -- what the host sides of the vocabulary's operators share: checks of a form, places in a workspace.
+#ifndef ZE_HOST_H
+#define ZE_HOST_H
+
+#include <math.h>
+
+#include "../../include/ze.h"
+#include "zt_device.h"
+
+namespace {
+
+constexpr size_t kMaxStride = (size_t)1 << 20;   // elements: a tile's rows are told apart by 32 bits
+
+size_t up(size_t n, size_t to) { return (n + to - 1) / to * to; }
+size_t parts(size_t n, size_t of) { return (n + of - 1) / of; }
+
+int check_form(const struct ze_form* f) {
+  if (!f) return ZC_ERR_NULL;
+  if (!known_dtype(f->dtype)) return ZC_ERR_DTYPE;
+  if ((f->id_dtype != ZE_I32 && f->id_dtype != ZE_I64) || f->first < 0 || !isfinite(f->scale)) return ZC_ERR_ARG;
+  if (f->tokens > ZE_MAX_TOKENS || f->rows > ZE_MAX_ROWS || f->cols > ZE_MAX_COLS) return ZC_ERR_SIZE;
+  if (f->stride_table > kMaxStride || f->stride_tokens > kMaxStride) return ZC_ERR_ARG;
+  return ZC_OK;
+}
+// An output's rows do not overlap.
+bool good_output(size_t stride, size_t cols) { return stride == 0 || (stride >= cols && stride <= kMaxStride); }
+size_t stride_of(size_t stride, size_t cols) { return stride ? stride : cols; }
+bool aligned_ids(const void* p, int id_dtype) { return aligned(p, id_dtype == ZE_I64 ? 8 : 4); }
+
+// Places in a workspace, one behind the other, at multiples of 256 bytes.
+struct Places {
+  size_t at = 0;
+  size_t take(size_t bytes) {
+    const size_t here = at;
+    at += up(bytes, 256);
+    return here;
+  }
+};
+
+}  // namespace
+#endif  // ZE_HOST_H

@@ -1,0 +1,831 @@
+// ze_loss.hip -- gfx950 kernels and C ABI of the softmax cross entropy in include/ze.h.
+//
+// Forward: one matrix product of hidden states and output matrix whose tiles of logits stay in registers; each wavefront leaves the greatest
+// logit and the sum of exponentials of its part of a row, a second kernel joins them.  Backward, for a piece of the vocabulary at a time: the same product again,
+// whose tiles become g = dloss (softmax - onehot) in the workspace, and two products that read it, along the vocabulary for the hidden states'
+// gradient and across it for the matrix's.  Tokens without a label are left out before anything else: the products work on a list of those that have
+// one, so what the others hold is not read at all.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/ze.h"
+#include "ze_host.h"
+#include "ze_product.h"
+
+namespace {
+
+constexpr float kLog2E = 1.44269504088896340736f;
+constexpr float kInf = __builtin_inff();
+
+// ---- the tokens that have a label --------------------------------------------------------
+
+struct Head {          // of a workspace, made on the GPU
+  int rows;            // tokens with a label
+  float most;          // the greatest finite |dloss| of theirs
+};
+constexpr size_t kHeadBytes = 256;
+
+// Rows are numbered as the tokens with a label come; `padded` places each (a multiple of 256), those behind the last row empty.
+struct List {
+  Head* head;
+  int* row_of;         // of each token: its row, or -1
+  int* token_of;       // of each row: its token, or -1
+  int* label_of;       // of each row: its label among this rank's, or -1
+  float* target;       // forward: -inf, until the label's logit is known
+  float *lse, *dloss;  // backward: the token's
+  size_t padded;
+};
+
+constexpr int kListThreads = 1024, kListRounds = 8;
+
+// One workgroup.  A token's row is the number of those before it: counted in the lanes before its own, the wavefronts before its own, and
+// the rounds before its own, 8 x 1024 tokens at a time.
+template <class ID>
+__global__ void __launch_bounds__(kListThreads) list_kernel(const ID* ids, int tokens, long long first, long long rows, const float* lse, const float* dloss, List list) {
+  __shared__ int counts[kListRounds * 16 + 1];
+  __shared__ float greatest[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
+  int before = 0;
+  float most = 0.0f;
+  for (int base = 0; base < tokens; base += kListRounds * kListThreads) {
+    long long id[kListRounds];
+#pragma unroll
+    for (int i = 0; i < kListRounds; ++i) {
+      const int n = base + i * kListThreads + tid;
+      id[i] = n < tokens ? (long long)ids[n] : -1;
+    }
+    uint64_t there[kListRounds];
+#pragma unroll
+    for (int i = 0; i < kListRounds; ++i) {
+      there[i] = __builtin_amdgcn_ballot_w64(id[i] >= 0);
+      if (lane == 0) counts[i * 16 + wave] = __builtin_popcountll(there[i]);
+    }
+    __syncthreads();
+    if (wave == 0) {
+      const int a = counts[2 * lane], b = counts[2 * lane + 1];
+      int sum = a + b;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const int other = __shfl_up(sum, d);
+        if (lane >= d) sum += other;
+      }
+      counts[2 * lane] = sum - a - b;
+      counts[2 * lane + 1] = sum - b;
+      if (lane == 63) counts[kListRounds * 16] = sum;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kListRounds; ++i) {
+      const int n = base + i * kListThreads + tid;
+      if (n >= tokens) continue;
+      const int row = before + counts[i * 16 + wave] + __builtin_popcountll(there[i] & (((uint64_t)1 << lane) - 1));
+      const bool has = id[i] >= 0;
+      list.row_of[n] = has ? row : -1;
+      if (!has) continue;
+      const long long local = id[i] - first;
+      list.token_of[row] = n;
+      list.label_of[row] = local >= 0 && local < rows ? (int)local : -1;
+      if (list.target) list.target[row] = -kInf;
+      if (lse) {
+        const float d = dloss[n], size = fabsf(d);
+        list.lse[row] = lse[n];
+        list.dloss[row] = d;
+        if (size < kInf) most = fmaxf(most, size);
+      }
+    }
+    before += counts[kListRounds * 16];
+    __syncthreads();
+  }
+  for (size_t row = (size_t)before + tid; row < list.padded; row += kListThreads) {
+    list.token_of[row] = -1;
+    list.label_of[row] = -1;
+    if (lse) list.lse[row] = list.dloss[row] = 0.0f;
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+  if (lane == 0) greatest[wave] = most;
+  __syncthreads();
+  if (tid == 0) {
+    for (int w = 1; w < 16; ++w) most = fmaxf(most, greatest[w]);
+    list.head->rows = before;
+    list.head->most = most;
+  }
+}
+
+// ---- rows where the products can read them -----------------------------------------------
+
+constexpr int kThreads = 256;
+
+// A copy of rows of `cols` values whose rows start at multiples of 128 bytes and end in zeros.  Row r of the copy is row token_of[r] of `in`, or of
+// zeros where that is negative; without a list row r, of `rows`.
+struct PackArgs {
+  const char* in;
+  size_t stride;        // bytes
+  const int* token_of;
+  size_t rows;          // of `in`, without a list
+  char* out;
+  size_t out_stride;    // bytes, a multiple of 128
+  int cols;
+};
+
+template <int DT>
+__device__ __forceinline__ void pack_row(const PackArgs& a, size_t r) {
+  constexpr int kN = kVec<DT>;
+  const long long source = a.token_of ? (long long)a.token_of[r] : r < a.rows ? (long long)r : -1;
+  const char* in = a.in + (source < 0 ? 0 : (size_t)source) * a.stride;
+  char* out = a.out + r * a.out_stride;
+  for (uint32_t at = threadIdx.x * 16; at < a.out_stride; at += kThreads * 16) {
+    Raw<DT> raw;
+    const int valid = source < 0 ? 0 : a.cols - (int)(at / kBytes<DT>);
+    if (valid >= kN) {
+      raw.load(in, at);
+    } else {
+#pragma unroll
+      for (int i = 0; i < raw.kWords; ++i) raw.w[i] = 0;
+      if (valid > 0) raw.load(in, at, valid);
+    }
+    raw.store(out, at);
+  }
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kThreads) pack_kernel(PackArgs a, size_t from) {
+  pack_row<DT>(a, from + blockIdx.x);
+}
+
+__device__ __forceinline__ void zero_row(char* row, size_t bytes) {
+  const size_t head = (16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15;
+  if (bytes <= head) {
+    for (size_t i = threadIdx.x * 2; i < bytes; i += kThreads * 2) *reinterpret_cast<uint16_t*>(row + i) = 0;
+    return;
+  }
+  const size_t body = (bytes - head) / 16;
+  for (size_t i = threadIdx.x; i < body; i += kThreads) reinterpret_cast<i32x4*>(row + head)[i] = i32x4{0, 0, 0, 0};
+  for (size_t i = threadIdx.x * 2; i < head; i += kThreads * 2) *reinterpret_cast<uint16_t*>(row + i) = 0;
+  for (size_t i = head + body * 16 + threadIdx.x * 2; i < bytes; i += kThreads * 2) *reinterpret_cast<uint16_t*>(row + i) = 0;
+}
+
+// The rows with a label, packed; and zeros for the gradients of the hidden states of tokens without one.
+template <int DT>
+__global__ void __launch_bounds__(kThreads) pack_hidden_kernel(PackArgs a, size_t from, const int* row_of, size_t tokens, char* dhidden, size_t dhidden_stride) {
+  const size_t r = from + blockIdx.x;
+  pack_row<DT>(a, r);
+  if (dhidden && r < tokens && row_of[r] < 0) zero_row(dhidden + r * dhidden_stride, (size_t)a.cols * kBytes<DT>);
+}
+
+__global__ void __launch_bounds__(kThreads) zero_rows_kernel(char* out, size_t stride, size_t bytes, size_t from) {
+  zero_row(out + (from + blockIdx.x) * stride, bytes);
+}
+
+// ---- forward -----------------------------------------------------------------------------
+
+struct Part {
+  float most, sum;
+};
+
+struct LogitsArgs {
+  Matrix table, hidden;        // the piece's rows; the rows with a label
+  const Head* head;
+  const int* label_of;
+  int nx, ny, steps;           // tiles, and steps of k
+  int v0, rows;                // the piece's first row and number of rows
+  float scale;
+  Part* parts;                 // [rows with a label][stride], this piece's first
+  size_t parts_stride;
+  float* target;
+};
+
+// The greatest logit and the sum of exponentials in each wavefront's part of a row.  In a tile that is all there is of them: 4 x 16 columns to
+// a lane group, so a row's maximum takes NX x 4 comparisons in a lane and two across lanes.
+template <int DT, class S>
+__global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a) {
+  int tx, ty;
+  tile_of(a.nx, a.ny, tx, ty);
+  const int there = a.head->rows;
+  if (ty * S::BY >= there) return;
+  f32x4 sum[S::NX][S::NY];
+  product<DT, S, kAlong, kAlong>(a.table, a.hidden, (size_t)tx * S::BX, (size_t)ty * S::BY, a.steps, sum);
+  const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, wx = wave % S::WX, wy = wave / S::WX;
+  const int x0 = tx * S::BX + wx * (S::BX / S::WX) + lane / 16 * 4, y0 = ty * S::BY + wy * (S::BY / S::WY) + (lane & 15);
+#pragma unroll
+  for (int j = 0; j < S::NY; ++j) {
+    const int y = y0 + 16 * j;
+    if (y >= there) continue;
+    const int label = a.label_of[y] - a.v0;
+    float most = -kInf;
+#pragma unroll
+    for (int i = 0; i < S::NX; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int x = x0 + 16 * i + r;
+        const float l = x < a.rows ? a.scale * sum[i][j][r] : -kInf;
+        sum[i][j][r] = l;
+        most = fmaxf(most, l);
+        if (x == label && x < a.rows) a.target[y] = l;
+      }
+    most = fmaxf(most, __shfl_xor(most, 16));
+    most = fmaxf(most, __shfl_xor(most, 32));
+    const float from = most == -kInf ? 0.0f : most;   // nothing there: exp(-inf) = 0 each
+    float total = 0.0f;
+#pragma unroll
+    for (int i = 0; i < S::NX; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) total += __builtin_amdgcn_exp2f((sum[i][j][r] - from) * kLog2E);
+    total += __shfl_xor(total, 16);
+    total += __shfl_xor(total, 32);
+    if (lane < 16) a.parts[y * a.parts_stride + tx * S::WX + wx] = Part{most, total};
+  }
+}
+
+// Joins a row's parts: a wavefront for each token.
+__global__ void __launch_bounds__(kThreads) stats_kernel(const int* row_of, size_t tokens, const Part* parts, size_t stride, size_t count, const float* target,
+                                                         float* stats) {
+  const size_t n = (size_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
+  const int lane = threadIdx.x & 63;
+  if (n >= tokens) return;
+  const int row = row_of[n];
+  float most = -kInf, total = 0.0f;
+  if (row >= 0) {
+    const Part* p = parts + (size_t)row * stride;
+    for (size_t i = lane; i < count; i += 64) most = fmaxf(most, p[i].most);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+    const float from = most == -kInf ? 0.0f : most;
+    for (size_t i = lane; i < count; i += 64) total += p[i].sum * __builtin_amdgcn_exp2f((p[i].most - from) * kLog2E);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d);
+  }
+  if (lane == 0) {
+    stats[n] = most;
+    stats[tokens + n] = total;
+    stats[2 * tokens + n] = row < 0 ? 0.0f : target[row];
+  }
+}
+
+template <class ID>
+__global__ void __launch_bounds__(kThreads) join_kernel(size_t tokens, int ranks, const float* stats, const ID* ids, float* loss, float* lse) {
+  const size_t n = (size_t)blockIdx.x * kThreads + threadIdx.x;
+  if (n >= tokens) return;
+  if (ids[n] < 0) {
+    if (loss) loss[n] = 0.0f;
+    lse[n] = 0.0f;
+    return;
+  }
+  float most = -kInf, target = -kInf;
+  for (int r = 0; r < ranks; ++r) {
+    most = fmaxf(most, stats[(size_t)r * 3 * tokens + n]);
+    target = fmaxf(target, stats[((size_t)r * 3 + 2) * tokens + n]);
+  }
+  const float from = most == -kInf ? 0.0f : most;
+  float total = 0.0f;
+  for (int r = 0; r < ranks; ++r)
+    total += stats[((size_t)r * 3 + 1) * tokens + n] * __builtin_amdgcn_exp2f((stats[(size_t)r * 3 * tokens + n] - from) * kLog2E);
+  const float l = from + logf(total);
+  lse[n] = l;
+  if (loss) loss[n] = l - target;
+}
+
+// ---- backward ----------------------------------------------------------------------------
+
+// What g is multiplied by before it is rounded, beside 1 / max |dloss|.
+template <int DT> constexpr float kLift = DT == kF16 ? 32768.0f : 1.0f;
+
+struct GradientArgs {
+  Matrix table, hidden;
+  const Head* head;
+  const int* label_of;
+  const float *lse, *dloss;
+  int nx, ny, steps;
+  int v0, rows, rows_padded;   // of the piece; padded to whole steps
+  float scale;
+  char* g;                     // [rows with a label, to a whole step][rows_padded]
+};
+
+// g of a tile, zeros behind the piece's last row and behind the last row with a label, up to whole steps of the products that read it.
+template <int DT, class S>
+__global__ void __launch_bounds__(S::kThreads) gradient_kernel(GradientArgs a) {
+  int tx, ty;
+  tile_of(a.nx, a.ny, tx, ty);
+  const int there = a.head->rows;
+  if (ty * S::BY >= there) return;
+  f32x4 sum[S::NX][S::NY];
+  product<DT, S, kAlong, kAlong>(a.table, a.hidden, (size_t)tx * S::BX, (size_t)ty * S::BY, a.steps, sum);
+  const float most = a.head->most;
+  const int padded = (there + kStep<DT> - 1) / kStep<DT> * kStep<DT>;
+  const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, wx = wave % S::WX, wy = wave / S::WX;
+  const int x0 = tx * S::BX + wx * (S::BX / S::WX) + lane / 16 * 4, y0 = ty * S::BY + wy * (S::BY / S::WY) + (lane & 15);
+#pragma unroll
+  for (int j = 0; j < S::NY; ++j) {
+    const int y = y0 + 16 * j;
+    if (y >= padded) continue;
+    const int label = a.label_of[y] - a.v0;
+    const float lse = a.lse[y], factor = most > 0.0f ? a.dloss[y] / most * kLift<DT> : a.dloss[y];
+    char* const row = a.g + (size_t)y * a.rows_padded * kBytes<DT>;
+#pragma unroll
+    for (int i = 0; i < S::NX; ++i) {
+      const int x = x0 + 16 * i;
+      float v[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float p = __builtin_amdgcn_exp2f((a.scale * sum[i][j][r] - lse) * kLog2E);
+        v[r] = x + r < a.rows && y < there ? factor * (p - (x + r == label ? 1.0f : 0.0f)) : 0.0f;
+      }
+      Raw<DT, 4> raw;
+      raw.pack(v);
+      if (x < a.rows_padded) raw.store(row, x * kBytes<DT>);
+    }
+  }
+}
+
+// out[y][x] from a tile's sums.
+struct OutArgs {
+  Matrix mx, my;
+  const Head* head;
+  int nx, ny, steps;
+  int cols, rows;              // of the output: x, and y where they are not the rows with a label
+  float scale;
+  char* out;                   // of type DT
+  size_t out_stride;           // bytes
+  const int* token_of;         // of each y: its row of the output
+  float* kept;                 // fp32 sums, [splits][rows][kept_stride], or NULL
+  size_t kept_stride, kept_split;
+  int add, finish, splits;     // whether kept sums are added, whether the output is written
+};
+
+// The matrix's gradient: x along the columns, y the piece's rows, k the rows with a label.
+template <int DT, class S>
+__global__ void __launch_bounds__(S::kThreads) table_gradient_kernel(OutArgs a) {
+  int tx, ty;
+  tile_of(a.nx, a.ny, tx, ty);
+  f32x4 sum[S::NX][S::NY];
+  const int there = a.head->rows;
+  product<DT, S, kAcross, kAcross>(a.mx, a.my, (size_t)tx * S::BX, (size_t)ty * S::BY, (there + kStep<DT> - 1) / kStep<DT>, sum);
+  const float factor = a.scale * (a.head->most / kLift<DT>);
+  const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, wx = wave % S::WX, wy = wave / S::WX;
+  const int x0 = tx * S::BX + wx * (S::BX / S::WX) + lane / 16 * 4, y0 = ty * S::BY + wy * (S::BY / S::WY) + (lane & 15);
+#pragma unroll
+  for (int j = 0; j < S::NY; ++j) {
+    const int y = y0 + 16 * j;
+    if (y >= a.rows) continue;
+    char* const row = a.out + (size_t)y * a.out_stride;
+#pragma unroll
+    for (int i = 0; i < S::NX; ++i) {
+      const int x = x0 + 16 * i;
+      float v[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r] = factor * sum[i][j][r];
+      Raw<DT, 4> raw;
+      raw.pack(v);
+      raw.store(row, x * kBytes<DT>, a.cols - x);
+    }
+  }
+}
+
+// The hidden states' gradient: x along the columns, y the rows with a label, k the piece's rows, which `splits` workgroups share.
+template <int DT, class S>
+__global__ void __launch_bounds__(S::kThreads) hidden_gradient_kernel(OutArgs a) {
+  int tx, ty;
+  tile_of(a.nx, a.ny, tx, ty);
+  const int there = a.head->rows;
+  if (ty * S::BY >= there) return;
+  const int split = blockIdx.y, from = (int)((long long)a.steps * split / a.splits), to = (int)((long long)a.steps * (split + 1) / a.splits);
+  Matrix mx = a.mx, my = a.my;
+  const size_t skip = (size_t)from * kStep<DT> * mx.stride;
+  mx.at += skip < mx.bytes ? skip : mx.bytes;
+  mx.bytes -= skip < mx.bytes ? skip : mx.bytes;
+  my.at += (size_t)from * kStepBytes;
+  my.bytes -= (size_t)from * kStepBytes;
+  f32x4 sum[S::NX][S::NY];
+  product<DT, S, kAcross, kAlong>(mx, my, (size_t)tx * S::BX, (size_t)ty * S::BY, to - from, sum);
+  const float factor = a.scale * (a.head->most / kLift<DT>);
+  const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, wx = wave % S::WX, wy = wave / S::WX;
+  const int x0 = tx * S::BX + wx * (S::BX / S::WX) + lane / 16 * 4, y0 = ty * S::BY + wy * (S::BY / S::WY) + (lane & 15);
+#pragma unroll
+  for (int j = 0; j < S::NY; ++j) {
+    const int y = y0 + 16 * j;
+    if (y >= there) continue;
+    char* const row = a.finish ? a.out + (size_t)a.token_of[y] * a.out_stride : nullptr;
+    float* const kept = a.kept + split * a.kept_split + (size_t)y * a.kept_stride;
+#pragma unroll
+    for (int i = 0; i < S::NX; ++i) {
+      const int x = x0 + 16 * i;
+      if (x >= a.cols) continue;   // (kept rows are a multiple of 4 wide)
+      f32x4 s = sum[i][j];
+      if (a.add) s += *reinterpret_cast<const f32x4*>(kept + x);
+      if (!a.finish) {
+        *reinterpret_cast<f32x4*>(kept + x) = s;
+        continue;
+      }
+      float v[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r] = factor * s[r];
+      Raw<DT, 4> raw;
+      raw.pack(v);
+      raw.store(row, x * kBytes<DT>, a.cols - x);
+    }
+  }
+}
+
+// The sums that `splits` workgroups have kept of each place, one after the other.
+template <int DT>
+__global__ void __launch_bounds__(kThreads) hidden_finish_kernel(OutArgs a) {
+  const int y = blockIdx.y * 65535 + blockIdx.z, x = (blockIdx.x * kThreads + threadIdx.x) * 4;
+  if (y >= a.head->rows || x >= a.cols) return;
+  const float* kept = a.kept + (size_t)y * a.kept_stride + x;
+  f32x4 s = *reinterpret_cast<const f32x4*>(kept);
+  for (int i = 1; i < a.splits; ++i) s += *reinterpret_cast<const f32x4*>(kept + i * a.kept_split);
+  const float factor = a.scale * (a.head->most / kLift<DT>);
+  float v[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) v[r] = factor * s[r];
+  Raw<DT, 4> raw;
+  raw.pack(v);
+  raw.store(a.out + (size_t)a.token_of[y] * a.out_stride, x * kBytes<DT>, a.cols - x);
+}
+
+// ---- host: how a call is laid out ----------------------------------------------------------
+
+using Large = Shape<256, 256, 2, 4, 2>;
+using Medium = Shape<128, 128, 2, 2, 2>;
+using Small = Shape<64, 64, 2, 2, 4>;
+enum { kLarge, kMedium, kSmall };
+constexpr int kComputeUnits = 256;
+constexpr size_t kMostTiles = (size_t)1 << 22;   // of one launch
+
+size_t tiles(int shape, size_t nx, size_t ny) {
+  const size_t b = shape == kLarge ? Large::BX : shape == kMedium ? Medium::BX : Small::BX;
+  return parts(nx, b) * parts(ny, b);
+}
+int shape_for(int dtype, size_t nx, size_t ny) {
+  if (dtype != ZC_F32 && tiles(kLarge, nx, ny) >= kComputeUnits * 3 / 4) return kLarge;
+  return tiles(kMedium, nx, ny) >= kComputeUnits * 3 / 4 ? kMedium : kSmall;
+}
+
+#define ZE_BY_SHAPE(SHAPE, DT, LAUNCH)              \
+  do {                                              \
+    if ((SHAPE) == kMedium) LAUNCH(DT, Medium);     \
+    else if ((SHAPE) == kSmall) LAUNCH(DT, Small);  \
+    else if constexpr (DT != kF32) LAUNCH(DT, Large); \
+  } while (0)
+#define ZE_BY_TYPE(TYPE, CALL)             \
+  do {                                     \
+    if ((TYPE) == ZC_F32) CALL(kF32);      \
+    else if ((TYPE) == ZC_BF16) CALL(kBF16); \
+    else CALL(kF16);                       \
+  } while (0)
+
+// A call's workspace and the way it takes.
+struct Plan {
+  size_t e, padded;                  // bytes of a value; tokens, to whole tiles
+  size_t cols_padded;                // to whole steps
+  size_t stride_hidden, stride_table;   // bytes
+  bool pack_hidden, pack_table;
+  size_t piece;                      // rows of the table at a time
+  int shape;                         // of the logits
+  size_t parts;                      // forward: of a row
+  int hidden_shape, splits;          // backward
+  bool keep;                         // backward: sums of the hidden states' gradient are kept from piece to piece
+  size_t list[7], packed_hidden, packed_table, part, g, kept, bytes;
+};
+
+constexpr size_t kMostPacked = (size_t)64 << 20;   // bytes of the table that are copied at a time
+
+bool readable(const void* p, size_t stride_bytes, size_t cols, size_t e) {
+  return aligned(p, 16) && stride_bytes % 16 == 0 && cols * e % kStepBytes == 0;
+}
+
+// Whether the operands are copied to where a product can read them decides what the workspace holds.
+Plan plan_with(const struct ze_form& f, bool backward, size_t piece, bool pack_hidden, bool pack_table) {
+  Plan p = {};
+  p.pack_hidden = pack_hidden;
+  p.pack_table = pack_table;
+  p.e = dtype_bytes(f.dtype);
+  p.padded = up(f.tokens, 256);
+  p.cols_padded = up(f.cols, kStepBytes / p.e);
+  p.stride_hidden = stride_of(f.stride_tokens, f.cols) * p.e;
+  p.stride_table = stride_of(f.stride_table, f.cols) * p.e;
+  if (backward) {
+    const size_t most = ((size_t)128 << 20) / (f.tokens ? f.tokens : 1);
+    p.piece = piece ? up(piece < f.rows ? piece : f.rows, 256) : most > 4096 ? most / 256 * 256 : 4096;
+  } else {
+    p.piece = f.rows;
+  }
+  const size_t limit = kMostTiles / parts(p.padded, 64) / 4 * 256;    // tiles of a launch, were they small ones
+  if (p.piece > limit) p.piece = limit;
+  if (pack_table) {
+    const size_t most = kMostPacked / (p.cols_padded * p.e) / 256 * 256;
+    if (p.piece > most) p.piece = most > 256 ? most : 256;
+  }
+  if (p.piece > f.rows) p.piece = f.rows;
+  if (backward && !piece && p.piece && p.piece < f.rows) {   // pieces of the same size
+    const size_t n = parts(f.rows, p.piece);
+    const size_t even = up(parts(f.rows, n), 256);
+    if (even < p.piece) p.piece = even;
+  }
+  p.shape = shape_for(f.dtype, p.piece, f.tokens);
+  Places places;
+  places.take(kHeadBytes);
+  for (int i = 0; i < 7; ++i) p.list[i] = places.take(p.padded * 4);
+  p.packed_hidden = places.take(backward || pack_hidden ? p.padded * p.cols_padded * p.e : 0);
+  p.packed_table = places.take(pack_table ? p.piece * p.cols_padded * p.e : 0);
+  if (!backward) {
+    const size_t part = p.shape == kLarge ? Large::BX / Large::WX : p.shape == kMedium ? Medium::BX / Medium::WX : Small::BX / Small::WX;
+    p.parts = p.piece ? parts(f.rows, p.piece) * parts(up(p.piece, 256), part) : 0;
+    p.part = places.take(f.tokens * p.parts * sizeof(Part));
+  } else {
+    const size_t padded = up(p.piece, kStepBytes / p.e);
+    p.g = places.take(p.padded * padded * p.e);
+    p.hidden_shape = shape_for(f.dtype, f.cols, f.tokens);
+    const size_t n = tiles(p.hidden_shape, f.cols, f.tokens), steps = padded * p.e / kStepBytes, most = steps / 16;
+    const size_t wanted = n ? 2 * kComputeUnits / n : 1;
+    p.splits = (int)(wanted < 1 || p.hidden_shape == kLarge ? 1 : wanted < most ? wanted : most ? most : 1);
+    p.keep = p.piece < f.rows || p.splits > 1;
+    if (p.keep) p.kept = places.take((size_t)p.splits * p.padded * up(f.cols, 4) * 4);
+  }
+  p.bytes = places.at;
+  return p;
+}
+
+// The plan for tensors where they lie; NULL: for the place that asks for most.
+Plan plan_for(const struct ze_form& f, bool backward, size_t piece, const void* d_hidden, const void* d_table) {
+  const size_t e = dtype_bytes(f.dtype), stride = stride_of(f.stride_tokens, f.cols) * e;
+  // a list of rows tells places apart by 32 bits
+  const bool pack_hidden = !d_hidden || !readable(d_hidden, stride, f.cols, e) || f.tokens * stride > 0xF0000000u;
+  return plan_with(f, backward, piece, pack_hidden, !d_table || !readable(d_table, stride_of(f.stride_table, f.cols) * e, f.cols, e));
+}
+size_t work_bytes_for(const struct ze_form& f, bool backward, size_t piece, const void* d_hidden, const void* d_table) {
+  const size_t bytes = plan_for(f, backward, piece, d_hidden, d_table).bytes;
+  if (d_hidden && d_table) return bytes;
+  // (A table that is not copied may be taken in larger pieces.)
+  const size_t other = plan_with(f, backward, piece, true, false).bytes;
+  return bytes > other ? bytes : other;
+}
+
+List list_in(const Plan& p, char* work, bool backward) {
+  const auto at = [&](int i) { return work + p.list[i]; };
+  List l;
+  l.head = reinterpret_cast<Head*>(work);
+  l.row_of = reinterpret_cast<int*>(at(0));
+  l.token_of = reinterpret_cast<int*>(at(1));
+  l.label_of = reinterpret_cast<int*>(at(2));
+  l.target = backward ? nullptr : reinterpret_cast<float*>(at(3));
+  l.lse = reinterpret_cast<float*>(at(4));
+  l.dloss = reinterpret_cast<float*>(at(5));
+  l.padded = p.padded;
+  return l;
+}
+
+void launch_list(const struct ze_form& f, const void* d_labels, const float* d_lse, const float* d_dloss, const List& list, hipStream_t s) {
+  if (f.id_dtype == ZE_I64)
+    hipLaunchKernelGGL(list_kernel<long long>, dim3(1), dim3(kListThreads), 0, s, static_cast<const long long*>(d_labels), (int)f.tokens, f.first, (long long)f.rows,
+                       d_lse, d_dloss, list);
+  else
+    hipLaunchKernelGGL(list_kernel<int>, dim3(1), dim3(kListThreads), 0, s, static_cast<const int*>(d_labels), (int)f.tokens, f.first, (long long)f.rows, d_lse,
+                       d_dloss, list);
+}
+
+constexpr size_t kMostGroups = (size_t)1 << 23;   // of one launch: a grid has fewer than 2^32 lanes
+
+// The rows `v0` to `v0 + count` of the table where a product can read them.
+template <int DT>
+Matrix table_piece(const struct ze_form& f, const Plan& p, const void* d_table, size_t v0, size_t count, char* work, hipStream_t s) {
+  Matrix m;
+  m.places = nullptr;
+  const char* at = static_cast<const char*>(d_table) + v0 * p.stride_table;
+  if (!p.pack_table) {
+    m.at = at;
+    m.stride = p.stride_table;
+    m.bytes = (count - 1) * m.stride + f.cols * p.e;
+    return m;
+  }
+  PackArgs a = {at, p.stride_table, nullptr, count, work + p.packed_table, p.cols_padded * p.e, (int)f.cols};
+  for (size_t from = 0; from < count; from += kMostGroups) {
+    const size_t groups = count - from < kMostGroups ? count - from : kMostGroups;
+    hipLaunchKernelGGL(pack_kernel<DT>, dim3((unsigned)groups), dim3(kThreads), 0, s, a, from);
+  }
+  m.at = a.out;
+  m.stride = a.out_stride;
+  m.bytes = count * a.out_stride;
+  return m;
+}
+
+template <int DT>
+void forward(const struct ze_form& f, const Plan& p, const void* d_hidden, const void* d_table, const List& list, char* work, float* d_stats, hipStream_t s) {
+  LogitsArgs a;
+  a.head = list.head;
+  a.label_of = list.label_of;
+  a.scale = f.scale;
+  a.target = list.target;
+  a.parts_stride = p.parts;
+  a.steps = (int)(p.cols_padded * p.e / kStepBytes);
+  if (p.piece) {
+    if (p.pack_hidden) {
+      PackArgs pack = {static_cast<const char*>(d_hidden), p.stride_hidden, list.token_of, 0, work + p.packed_hidden, p.cols_padded * p.e, (int)f.cols};
+      for (size_t from = 0; from < p.padded; from += kMostGroups) {
+        const size_t groups = p.padded - from < kMostGroups ? p.padded - from : kMostGroups;
+        hipLaunchKernelGGL(pack_kernel<DT>, dim3((unsigned)groups), dim3(kThreads), 0, s, pack, from);
+      }
+      a.hidden = Matrix{pack.out, p.padded * pack.out_stride, pack.out_stride, nullptr};
+    } else {
+      a.hidden = Matrix{static_cast<const char*>(d_hidden), (f.tokens - 1) * p.stride_hidden + f.cols * p.e, p.stride_hidden, list.token_of};
+    }
+  }
+  size_t part = 0;
+  for (size_t v0 = 0; v0 < f.rows; v0 += p.piece) {
+    const size_t count = f.rows - v0 < p.piece ? f.rows - v0 : p.piece;
+    a.table = table_piece<DT>(f, p, d_table, v0, count, work, s);
+    a.v0 = (int)v0;
+    a.rows = (int)count;
+    a.parts = reinterpret_cast<Part*>(work + p.part) + part;
+#define LAUNCH(D, S)                                                                                                                  \
+  do {                                                                                                                                \
+    a.nx = (int)parts(count, S::BX);                                                                                                  \
+    a.ny = (int)parts(f.tokens, S::BY);                                                                                               \
+    part += (size_t)a.nx * S::WX;                                                                                                     \
+    hipLaunchKernelGGL((logits_kernel<D, S>), dim3((unsigned)(a.nx * a.ny)), dim3(S::kThreads), 0, s, a);                             \
+  } while (0)
+    ZE_BY_SHAPE(p.shape, DT, LAUNCH);
+#undef LAUNCH
+  }
+  const size_t groups = parts(f.tokens, kThreads / 64);
+  hipLaunchKernelGGL(stats_kernel, dim3((unsigned)groups), dim3(kThreads), 0, s, list.row_of, f.tokens, reinterpret_cast<const Part*>(work + p.part), p.parts, part,
+                     list.target, d_stats);
+}
+
+template <int DT>
+void backward(const struct ze_form& f, const Plan& p, const void* d_hidden, const void* d_table, const List& list, char* work, void* d_dhidden, void* d_dtable,
+              hipStream_t s) {
+  const size_t dhidden_stride = stride_of(f.stride_dtokens, f.cols) * p.e, dtable_stride = stride_of(f.stride_dtable, f.cols) * p.e;
+  // the rows with a label, to a whole step of the product over them
+  PackArgs pack = {static_cast<const char*>(d_hidden), p.stride_hidden, list.token_of, 0, work + p.packed_hidden, p.cols_padded * p.e, (int)f.cols};
+  for (size_t from = 0; from < p.padded; from += kMostGroups) {
+    const size_t groups = p.padded - from < kMostGroups ? p.padded - from : kMostGroups;
+    hipLaunchKernelGGL(pack_hidden_kernel<DT>, dim3((unsigned)groups), dim3(kThreads), 0, s, pack, from, list.row_of, f.tokens, static_cast<char*>(d_dhidden),
+                       dhidden_stride);
+  }
+  const Matrix hidden = {pack.out, p.padded * pack.out_stride, pack.out_stride, nullptr};
+  for (size_t v0 = 0; v0 < f.rows; v0 += p.piece) {
+    const size_t count = f.rows - v0 < p.piece ? f.rows - v0 : p.piece, padded = up(count, kStep<DT>);
+    const Matrix table = table_piece<DT>(f, p, d_table, v0, count, work, s);
+    GradientArgs g;
+    g.table = table;
+    g.hidden = hidden;
+    g.head = list.head;
+    g.label_of = list.label_of;
+    g.lse = list.lse;
+    g.dloss = list.dloss;
+    g.steps = (int)(p.cols_padded * p.e / kStepBytes);
+    g.v0 = (int)v0;
+    g.rows = (int)count;
+    g.rows_padded = (int)padded;
+    g.scale = f.scale;
+    g.g = work + p.g;
+#define LAUNCH(D, S)                                                                                           \
+  do {                                                                                                         \
+    g.nx = (int)parts(count, S::BX);                                                                           \
+    g.ny = (int)parts(f.tokens, S::BY);                                                                        \
+    hipLaunchKernelGGL((gradient_kernel<D, S>), dim3((unsigned)(g.nx * g.ny)), dim3(S::kThreads), 0, s, g);    \
+  } while (0)
+    ZE_BY_SHAPE(p.shape, DT, LAUNCH);
+#undef LAUNCH
+    const Matrix gradient = {g.g, p.padded * padded * p.e, padded * p.e, nullptr};
+    OutArgs a = {};
+    a.head = list.head;
+    a.scale = f.scale;
+    a.cols = (int)f.cols;
+    if (d_dtable) {
+      a.mx = hidden;
+      a.my = gradient;
+      a.rows = (int)count;
+      a.out = static_cast<char*>(d_dtable) + v0 * dtable_stride;
+      a.out_stride = dtable_stride;
+#define LAUNCH(D, S)                                                                                               \
+  do {                                                                                                             \
+    a.nx = (int)parts(f.cols, S::BX);                                                                              \
+    a.ny = (int)parts(count, S::BY);                                                                               \
+    hipLaunchKernelGGL((table_gradient_kernel<D, S>), dim3((unsigned)(a.nx * a.ny)), dim3(S::kThreads), 0, s, a);  \
+  } while (0)
+      ZE_BY_SHAPE(shape_for(f.dtype, f.cols, count), DT, LAUNCH);
+#undef LAUNCH
+    }
+    if (d_dhidden) {
+      a.mx = table;
+      a.my = gradient;
+      a.steps = (int)(padded / kStep<DT>);
+      a.out = static_cast<char*>(d_dhidden);
+      a.out_stride = dhidden_stride;
+      a.token_of = list.token_of;
+      a.kept = p.keep ? reinterpret_cast<float*>(work + p.kept) : nullptr;
+      a.kept_stride = up(f.cols, 4);
+      a.kept_split = p.padded * a.kept_stride;
+      a.splits = p.splits;
+      a.add = v0 > 0;
+      a.finish = p.splits == 1 && v0 + count == f.rows;
+#define LAUNCH(D, S)                                                                                                                             \
+  do {                                                                                                                                           \
+    a.nx = (int)parts(f.cols, S::BX);                                                                                                            \
+    a.ny = (int)parts(f.tokens, S::BY);                                                                                                          \
+    hipLaunchKernelGGL((hidden_gradient_kernel<D, S>), dim3((unsigned)(a.nx * a.ny), (unsigned)a.splits), dim3(S::kThreads), 0, s, a);           \
+  } while (0)
+      ZE_BY_SHAPE(p.hidden_shape, DT, LAUNCH);
+#undef LAUNCH
+      if (!a.finish && v0 + count == f.rows)
+        hipLaunchKernelGGL(hidden_finish_kernel<DT>, dim3((unsigned)parts(f.cols, kThreads * 4), (unsigned)parts(f.tokens, 65535), (unsigned)(f.tokens < 65535 ? f.tokens : 65535)),
+                           dim3(kThreads), 0, s, a);
+    }
+  }
+}
+
+// Rows of zeros.
+void launch_zeros(void* out, size_t rows, size_t stride, size_t bytes, hipStream_t s) {
+  for (size_t from = 0; from < rows; from += kMostGroups) {
+    const size_t groups = rows - from < kMostGroups ? rows - from : kMostGroups;
+    hipLaunchKernelGGL(zero_rows_kernel, dim3((unsigned)groups), dim3(kThreads), 0, s, static_cast<char*>(out), stride, bytes, from);
+  }
+}
+
+int check_loss_form(const struct ze_form* f) {
+  const int rc = check_form(f);
+  if (rc != ZC_OK) return rc;
+  return f->cols == 0 ? ZC_ERR_SIZE : ZC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ze_loss_work_bytes(const struct ze_form* form, const void* d_hidden, const void* d_table) {
+  if (check_loss_form(form) != ZC_OK || form->tokens == 0) return 0;
+  return work_bytes_for(*form, false, 0, d_hidden, form->rows ? d_table : d_hidden);
+}
+
+int ze_vocab_loss(const struct ze_form* form, const void* d_hidden, const void* d_table, const void* d_labels, float* d_stats, void* d_work, size_t work_bytes,
+                  void* stream) {
+  const int rc = check_loss_form(form);
+  if (rc != ZC_OK) return rc;
+  if (form->tokens == 0) return ZC_OK;
+  if (!d_hidden || (!d_table && form->rows) || !d_labels || !d_stats || !d_work) return ZC_ERR_NULL;
+  const size_t e = dtype_bytes(form->dtype);
+  if (!aligned(d_hidden, e) || !aligned(d_table, e) || !aligned_ids(d_labels, form->id_dtype) || !aligned(d_stats, 4) || !aligned(d_work, 256)) return ZC_ERR_ALIGN;
+  const Plan p = plan_for(*form, false, 0, d_hidden, form->rows ? d_table : d_hidden);
+  if (work_bytes < p.bytes) return ZC_ERR_CAPACITY;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  char* const work = static_cast<char*>(d_work);
+  const List list = list_in(p, work, false);
+  launch_list(*form, d_labels, nullptr, nullptr, list, s);
+#define CALL(DT) forward<DT>(*form, p, d_hidden, d_table, list, work, d_stats, s)
+  ZE_BY_TYPE(form->dtype, CALL);
+#undef CALL
+  return finish_launch();
+}
+
+int ze_join_loss(size_t tokens, int ranks, int id_dtype, const float* d_stats, const void* d_labels, float* d_loss, float* d_lse, void* stream) {
+  if (id_dtype != ZE_I32 && id_dtype != ZE_I64) return ZC_ERR_ARG;
+  if (ranks < 1) return ZC_ERR_K;
+  if (tokens > ZE_MAX_TOKENS) return ZC_ERR_SIZE;
+  if (tokens == 0) return ZC_OK;
+  if (!d_stats || !d_labels || !d_lse) return ZC_ERR_NULL;
+  if (!aligned(d_stats, 4) || !aligned_ids(d_labels, id_dtype) || !aligned(d_loss, 4) || !aligned(d_lse, 4)) return ZC_ERR_ALIGN;
+  const dim3 grid((unsigned)parts(tokens, kThreads));
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (id_dtype == ZE_I64)
+    hipLaunchKernelGGL(join_kernel<long long>, grid, dim3(kThreads), 0, s, tokens, ranks, d_stats, static_cast<const long long*>(d_labels), d_loss, d_lse);
+  else
+    hipLaunchKernelGGL(join_kernel<int>, grid, dim3(kThreads), 0, s, tokens, ranks, d_stats, static_cast<const int*>(d_labels), d_loss, d_lse);
+  return finish_launch();
+}
+
+size_t ze_loss_backward_work_bytes(const struct ze_form* form, const void* d_hidden, const void* d_table, size_t piece) {
+  if (check_loss_form(form) != ZC_OK || form->tokens == 0 || form->rows == 0) return 0;
+  return work_bytes_for(*form, true, piece, d_hidden, d_table);
+}
+
+int ze_vocab_loss_backward(const struct ze_form* form, const void* d_hidden, const void* d_table, const void* d_labels, const float* d_lse, const float* d_dloss,
+                           void* d_dhidden, void* d_dtable, size_t piece, void* d_work, size_t work_bytes, void* stream) {
+  const int rc = check_loss_form(form);
+  if (rc != ZC_OK) return rc;
+  if (!good_output(form->stride_dtokens, form->cols) || !good_output(form->stride_dtable, form->cols)) return ZC_ERR_ARG;
+  const size_t e = dtype_bytes(form->dtype);
+  if (!aligned(d_dhidden, e) || !aligned(d_dtable, e)) return ZC_ERR_ALIGN;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (form->tokens == 0 || form->rows == 0) {   // sums of nothing
+    if (d_dhidden) launch_zeros(d_dhidden, form->tokens, stride_of(form->stride_dtokens, form->cols) * e, form->cols * e, s);
+    if (d_dtable) launch_zeros(d_dtable, form->rows, stride_of(form->stride_dtable, form->cols) * e, form->cols * e, s);
+    return finish_launch();
+  }
+  if (!d_hidden || !d_table || !d_labels || !d_lse || !d_dloss || !d_work) return ZC_ERR_NULL;
+  if (!aligned(d_hidden, e) || !aligned(d_table, e) || !aligned_ids(d_labels, form->id_dtype) || !aligned(d_lse, 4) || !aligned(d_dloss, 4) || !aligned(d_work, 256))
+    return ZC_ERR_ALIGN;
+  const Plan p = plan_for(*form, true, piece, d_hidden, d_table);
+  if (work_bytes < p.bytes) return ZC_ERR_CAPACITY;
+  char* const work = static_cast<char*>(d_work);
+  const List list = list_in(p, work, true);
+  launch_list(*form, d_labels, d_lse, d_dloss, list, s);
+#define CALL(DT) backward<DT>(*form, p, d_hidden, d_table, list, work, d_dhidden, d_dtable, s)
+  ZE_BY_TYPE(form->dtype, CALL);
+#undef CALL
+  return finish_launch();
+}
+
+}  // extern "C"

@@ -1,0 +1,172 @@
+"""The vocabulary's operators' C ABI (include/ze.h): every declared symbol is there, and whatever a call does not take is refused before
+any launch.  No GPU: every call below returns before it reaches one."""
+import ctypes
+import os
+import re
+import subprocess
+
+import pytest
+import torch
+
+from paper_2409_02423_amd import zc, ze
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+GOOD, ODD, ODD4, ODD16 = 0x10000, 0x10001, 0x10004, 0x10010   # never dereferenced
+MANY = 1 << 60
+NAN, INF = float("nan"), float("inf")
+
+
+def _header():
+    text = open(os.path.join(ROOT, "include", "ze.h")).read()
+    return re.sub(r"/\*.*?\*/", "", text, flags=re.S)
+
+
+def test_library_exports_every_declared_symbol():
+    declared = set(re.findall(r"\b(ze_[a-z_0-9]+)\s*\(", _header()))
+    assert declared == set(ze.EXPORTS)
+    for name in declared:
+        assert hasattr(ze.lib(), name), name
+
+
+def test_binding_has_the_headers_numbers_and_structure(tmp_path):
+    values = {k: eval(v) for k, v in re.findall(r"\b(ZE_[A-Z_0-9]+) = ([0-9 <]+)", _header())}
+    assert set(values) == {"ZE_I32", "ZE_I64", "ZE_MAX_TOKENS", "ZE_MAX_ROWS", "ZE_MAX_COLS"}
+    for k, v in values.items():
+        assert getattr(ze, k) == v, k
+    source = ['#include <stdio.h>', '#include "%s"' % os.path.join(ROOT, "include", "ze.h"), "int main(void) {", 'printf("%zu\\n", sizeof(struct ze_form));']
+    source += ['printf("%%zu\\n", offsetof(struct ze_form, %s));' % f[0] for f in ze.Form._fields_]
+    (tmp_path / "layout.c").write_text("\n".join(source + ["return 0; }"]))
+    subprocess.check_call(["gcc", "-std=c11", "-Wall", "-Werror", str(tmp_path / "layout.c"), "-o", str(tmp_path / "layout")])
+    said = [int(v) for v in subprocess.run([str(tmp_path / "layout")], capture_output=True, text=True, check=True).stdout.split()]
+    assert said == [ctypes.sizeof(ze.Form)] + [getattr(ze.Form, f[0]).offset for f in ze.Form._fields_]
+
+
+def _form(**change):
+    f = ze.Form(tokens=4, rows=10, cols=64, first=0, dtype=zc.ZC_BF16, grad_dtype=zc.ZC_F32, id_dtype=ze.ZE_I64, scale=1.0)
+    for k, v in change.items():
+        setattr(f, k, v)
+    return f
+
+
+LOOKUP = dict(ids=GOOD, table=GOOD, out=GOOD)
+LOOKUP_BACK = dict(ids=GOOD, dout=GOOD, dtable=GOOD)
+LOSS = dict(hidden=GOOD, table=GOOD, labels=GOOD, stats=GOOD, work=GOOD)
+LOSS_BACK = dict(hidden=GOOD, table=GOOD, labels=GOOD, lse=GOOD, dloss=GOOD, dhidden=GOOD, dtable=GOOD)
+
+
+def lookup(form, **change):
+    return ze.lib().ze_embedding(form, *dict(LOOKUP, **change).values(), None)
+
+
+def lookup_back(form, accumulate=0, work=GOOD, size=MANY, **change):
+    return ze.lib().ze_embedding_backward(form, *dict(LOOKUP_BACK, **change).values(), accumulate, work, size, None)
+
+
+def loss(form, size=MANY, **change):
+    return ze.lib().ze_vocab_loss(form, *dict(LOSS, **change).values(), size, None)
+
+
+def loss_back(form, piece=0, work=GOOD, size=MANY, **change):
+    return ze.lib().ze_vocab_loss_backward(form, *dict(LOSS_BACK, **change).values(), piece, work, size, None)
+
+
+CALLS = (lookup, lookup_back, loss, loss_back)
+
+
+@pytest.mark.parametrize("call", CALLS)
+@pytest.mark.parametrize("change, code", [
+    (dict(dtype=3), zc.ZC_ERR_DTYPE), (dict(dtype=-1), zc.ZC_ERR_DTYPE), (dict(id_dtype=2), ze.ZC_ERR_ARG), (dict(id_dtype=-1), ze.ZC_ERR_ARG),
+    (dict(first=-1), ze.ZC_ERR_ARG), (dict(scale=NAN), ze.ZC_ERR_ARG), (dict(scale=INF), ze.ZC_ERR_ARG), (dict(tokens=ze.ZE_MAX_TOKENS + 1), zc.ZC_ERR_SIZE),
+    (dict(rows=ze.ZE_MAX_ROWS + 1), zc.ZC_ERR_SIZE), (dict(cols=ze.ZE_MAX_COLS + 1), zc.ZC_ERR_SIZE), (dict(stride_table=1 << 21), ze.ZC_ERR_ARG),
+    (dict(stride_tokens=1 << 21), ze.ZC_ERR_ARG)])
+def test_forms_that_no_call_takes(call, change, code):
+    assert call(_form(**change)) == code
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_no_form(call):
+    assert call(None) == zc.ZC_ERR_NULL
+
+
+@pytest.mark.parametrize("call, names", [(lookup, ("ids", "table", "out")), (lookup_back, ("ids", "dout", "dtable", "work")), (loss, tuple(LOSS)),
+                                         (loss_back, ("hidden", "table", "labels", "lse", "dloss", "work"))])
+def test_null_and_misaligned_pointers(call, names):
+    for name in names:
+        assert call(_form(), **{name: None}) == zc.ZC_ERR_NULL, name
+        assert call(_form(), **{name: ODD}) == zc.ZC_ERR_ALIGN, name
+    for name in ("ids", "labels"):
+        if name in names:
+            assert call(_form(), **{name: ODD4}) == zc.ZC_ERR_ALIGN
+            assert call(_form(id_dtype=ze.ZE_I32), **{name: 0x10002}) == zc.ZC_ERR_ALIGN
+    if "work" in names:
+        assert call(_form(), work=ODD16) == zc.ZC_ERR_ALIGN
+    for name in ("table", "out", "dout", "hidden"):
+        if name in names:
+            assert call(_form(dtype=zc.ZC_F32), **{name: 0x10002}) == zc.ZC_ERR_ALIGN
+
+
+def test_outputs_whose_rows_overlap_and_other_arguments():
+    assert lookup(_form(stride_dtokens=63)) == lookup(_form(stride_dtokens=1 << 21)) == ze.ZC_ERR_ARG
+    assert lookup_back(_form(stride_dtable=63)) == ze.ZC_ERR_ARG
+    assert lookup_back(_form(), accumulate=2) == lookup_back(_form(), accumulate=-1) == ze.ZC_ERR_ARG
+    assert lookup_back(_form(grad_dtype=zc.ZC_F16)) == lookup_back(_form(grad_dtype=7)) == zc.ZC_ERR_DTYPE
+    assert lookup_back(_form(), dtable=0x10002) == zc.ZC_ERR_ALIGN      # fp32
+    assert loss_back(_form(stride_dtokens=1)) == loss_back(_form(stride_dtable=63)) == ze.ZC_ERR_ARG
+    assert loss_back(_form(), dhidden=ODD) == loss_back(_form(), dtable=ODD) == loss_back(_form(), lse=0x10002) == zc.ZC_ERR_ALIGN
+    assert loss(_form(cols=0)) == loss_back(_form(cols=0)) == zc.ZC_ERR_SIZE
+    assert loss(_form(), stats=0x10002) == zc.ZC_ERR_ALIGN
+
+
+def test_join_refusals():
+    def join(tokens=4, ranks=2, ids=ze.ZE_I64, stats=GOOD, labels=GOOD, loss=GOOD, lse=GOOD):
+        return ze.lib().ze_join_loss(tokens, ranks, ids, stats, labels, loss, lse, None)
+
+    assert join(ids=2) == ze.ZC_ERR_ARG
+    assert join(ranks=0) == join(ranks=-1) == zc.ZC_ERR_K
+    assert join(tokens=ze.ZE_MAX_TOKENS + 1) == zc.ZC_ERR_SIZE
+    assert join(stats=None) == join(labels=None) == join(lse=None) == zc.ZC_ERR_NULL
+    assert join(stats=ODD) == join(labels=ODD4) == join(loss=0x10002) == join(lse=ODD) == zc.ZC_ERR_ALIGN
+    assert join(tokens=0, stats=None, labels=None, lse=None) == zc.ZC_OK
+
+
+def test_calls_of_nothing():
+    assert lookup(_form(tokens=0), ids=None, out=None) == lookup(_form(cols=0), ids=None) == zc.ZC_OK
+    assert lookup_back(_form(rows=0), dtable=None, work=None, size=0) == zc.ZC_OK
+    assert lookup_back(_form(tokens=0), accumulate=1, ids=None, dout=None, work=None, size=0) == zc.ZC_OK
+    assert loss(_form(tokens=0), hidden=None, stats=None, work=None, size=0) == zc.ZC_OK
+
+
+def test_workspaces():
+    L = ze.lib()
+    for sizes in (L.ze_embedding_work_bytes, lambda f: L.ze_loss_work_bytes(f, None, None), lambda f: L.ze_loss_backward_work_bytes(f, None, None, 0)):
+        assert sizes(None) == sizes(_form(tokens=0)) == sizes(_form(dtype=9)) == 0
+    assert L.ze_loss_work_bytes(_form(cols=0), None, None) == 0
+    for tokens in (1, 300, 9000):
+        for rows in (1, 700, 50000):
+            for cols in (1, 64, 1025):
+                for dtype in (zc.ZC_F32, zc.ZC_F16):
+                    f = _form(tokens=tokens, rows=rows, cols=cols, dtype=dtype)
+                    need = L.ze_embedding_work_bytes(f)
+                    assert need >= 8 * tokens and lookup_back(f, size=need - 1) == zc.ZC_ERR_CAPACITY
+                    for at in (GOOD, 0x10008):
+                        need = L.ze_loss_work_bytes(f, at, at)
+                        assert need >= 8 * tokens and L.ze_loss_work_bytes(f, None, None) >= need
+                        assert loss(f, hidden=at, table=at, size=need - 1) == zc.ZC_ERR_CAPACITY
+                        for piece in (0, 1, 256, 1000, MANY):
+                            need = L.ze_loss_backward_work_bytes(f, at, at, piece)
+                            assert L.ze_loss_backward_work_bytes(f, None, None, piece) >= need > 0
+                            assert loss_back(f, hidden=at, table=at, piece=piece, size=need - 1) == zc.ZC_ERR_CAPACITY
+    # pieces bound what is kept of the probabilities
+    f = _form(tokens=8192, rows=1 << 18, cols=4096)
+    assert L.ze_loss_backward_work_bytes(f, GOOD, GOOD, 1024) < 8192 * (1 << 18)
+    assert L.ze_loss_backward_work_bytes(f, GOOD, GOOD, 0) < 8192 * (1 << 18)
+
+
+def test_binding_rejects_host_tensors_and_wrong_combinations():
+    t, ids = torch.zeros(4, 8), torch.zeros(4, dtype=torch.int64)
+    for call in (lambda: ze.ze_embedding(ids, t), lambda: ze.ze_embedding_backward(ids, t, 3), lambda: ze.ze_vocab_loss(t, t, ids), lambda: ze.ze_join_loss(t, ids),
+                 lambda: ze.ze_vocab_loss_backward(t, t, ids, t, t), lambda: ze.ze_embedding(ids, None), lambda: ze.ze_vocab_loss(None, t, ids)):
+        with pytest.raises(TypeError):
+            call()
+    with pytest.raises(ValueError):
+        ze.ze_embedding_backward(ids, t, 3, accumulate=True)
