@@ -210,6 +210,7 @@ __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a) {
   const int x0 = tx * S::BX + wx * (S::BX / S::WX) + lane / 16 * 4, y0 = ty * S::BY + wy * (S::BY / S::WY) + (lane & 15);
 #pragma unroll
   for (int j = 0; j < S::NY; ++j) {
+    rest_of_sums<S>(sum, j);
     const int y = y0 + 16 * j;
     if (y >= there) continue;
     const int label = a.label_of[y] - a.v0;
@@ -317,6 +318,7 @@ __global__ void __launch_bounds__(S::kThreads) gradient_kernel(GradientArgs a) {
   const int x0 = tx * S::BX + wx * (S::BX / S::WX) + lane / 16 * 4, y0 = ty * S::BY + wy * (S::BY / S::WY) + (lane & 15);
 #pragma unroll
   for (int j = 0; j < S::NY; ++j) {
+    rest_of_sums<S>(sum, j);
     const int y = y0 + 16 * j;
     if (y >= padded) continue;
     const int label = a.label_of[y] - a.v0;
@@ -366,6 +368,7 @@ __global__ void __launch_bounds__(S::kThreads) table_gradient_kernel(OutArgs a) 
   const int x0 = tx * S::BX + wx * (S::BX / S::WX) + lane / 16 * 4, y0 = ty * S::BY + wy * (S::BY / S::WY) + (lane & 15);
 #pragma unroll
   for (int j = 0; j < S::NY; ++j) {
+    rest_of_sums<S>(sum, j);
     const int y = y0 + 16 * j;
     if (y >= a.rows) continue;
     char* const row = a.out + (size_t)y * a.out_stride;
@@ -403,6 +406,7 @@ __global__ void __launch_bounds__(S::kThreads) hidden_gradient_kernel(OutArgs a)
   const int x0 = tx * S::BX + wx * (S::BX / S::WX) + lane / 16 * 4, y0 = ty * S::BY + wy * (S::BY / S::WY) + (lane & 15);
 #pragma unroll
   for (int j = 0; j < S::NY; ++j) {
+    rest_of_sums<S>(sum, j);
     const int y = y0 + 16 * j;
     if (y >= there) continue;
     char* const row = a.finish ? a.out + (size_t)a.token_of[y] * a.out_stride : nullptr;
@@ -446,7 +450,7 @@ __global__ void __launch_bounds__(kThreads) hidden_finish_kernel(OutArgs a) {
 
 // ---- host: how a call is laid out ----------------------------------------------------------
 
-using Large = Shape<256, 256, 2, 4, 2>;
+using Large = Shape<256, 256, 2, 2, 2, true>;
 using Medium = Shape<128, 128, 2, 2, 2>;
 using Small = Shape<64, 64, 2, 2, 4>;
 enum { kLarge, kMedium, kSmall };

@@ -8,6 +8,9 @@
 #ifndef ZE_PRODUCT_H
 #define ZE_PRODUCT_H
 
+#include <type_traits>
+#include <utility>
+
 #include "zt_device.h"
 
 namespace {
@@ -63,7 +66,7 @@ struct Operand {
 
   uint32_t from[kLoads];   // bytes from the tile's start
   const char* at;          // the tile's start, at the present step
-  size_t left, step;
+  long long left, step;    // bytes from there to the matrix's end (or less than none), and from step to step
   int lane_at[kAddresses];
 
   static __device__ __forceinline__ int swap_along(int row) { return (row >> 1) & 7; }
@@ -80,7 +83,7 @@ struct Operand {
       const bool listed = m.places != nullptr;
       const size_t skip = listed ? 0 : first * m.stride;
       at = m.at + skip;
-      left = skip < m.bytes ? m.bytes - skip : 0;
+      left = (long long)m.bytes - (long long)skip;
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) {
         const int row = j * (THREADS / 8) + tid / 8, piece = (tid & 7) ^ swap_along(row);
@@ -95,9 +98,9 @@ struct Operand {
 #pragma unroll
       for (int h = 0; h < 2; ++h) lane_at[h] = row * kStepBytes + ((group + 4 * h) ^ swap_along(lane & 15)) * 16;
     } else {
-      step = m.stride * kStep<DT>;
+      step = (long long)m.stride * kStep<DT>;
       at = m.at + first * kE;
-      left = first * kE < m.bytes ? m.bytes - first * kE : 0;
+      left = (long long)m.bytes - (long long)(first * kE);
       constexpr int kUnit = DT == kF32 ? 4 : 2;   // pieces of 16 values
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) {
@@ -112,16 +115,28 @@ struct Operand {
     }
   }
 
-  // The next step's loads into `tile`; zeros where there is none.  (Every wavefront counts on kLoads loads of its own.)
-  __device__ __forceinline__ void load(ZE_LDS char* tile, bool any) {
-    const uint32_t records = !any ? 0u : left > 0xFFFFFE00u ? 0xFFFFFE00u : (uint32_t)left;
-    const auto buffer = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at), 0, (int)records, 0x00027000);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-#pragma unroll
-    for (int j = 0; j < kLoads; ++j)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer, (ZE_LDS void*)(tile + (j * THREADS + wave * 64) * 16), 16, (int)from[j], 0, 0, 0);
+  // The next step's loads into `tile`; zeros where there is none (every wavefront counts on kLoads loads of its own).  One after the other, between
+  // other work, or all at once.
+  struct Step {
+    __amdgpu_buffer_rsrc_t buffer;
+    ZE_LDS char* tile;      // the wavefront's part
+  };
+  __device__ __forceinline__ Step next(ZE_LDS char* tile, bool any) {
+    const int high = (int)(left >> 32);
+    const uint32_t records = !any || high < 0 ? 0u : high > 0 ? 0xFFFFFE00u : (uint32_t)left;
+    const Step s = {__builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(at), 0, (int)records, 0x00027000),
+                    tile + __builtin_amdgcn_readfirstlane(threadIdx.x / 64) * 1024};
     at += step;
-    left -= step < left ? step : left;
+    left -= step;
+    return s;
+  }
+  __device__ __forceinline__ void load_one(const Step& s, int j) const {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(s.buffer, (ZE_LDS void*)(s.tile + j * THREADS * 16), 16, (int)from[j], 0, 0, 0);
+  }
+  __device__ __forceinline__ void load(ZE_LDS char* tile, bool any) {
+    const Step s = next(tile, any);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) load_one(s, j);
   }
 
   // What a lane puts into a product: row 16 t + its number of the wavefront's part, its group's quarter of half h of the step.
@@ -146,8 +161,9 @@ struct Operand {
 };
 
 // How a product is shared out: a tile of BX x BY for each workgroup, of which each of WX x WY wavefronts has a part.
-template <int BX_, int BY_, int WX_, int WY_, int STAGES_>
+template <int BX_, int BY_, int WX_, int WY_, int STAGES_, bool BY_HAND = false>
 struct Shape {
+  static constexpr bool kByHand = BY_HAND;   // half precision alone
   static constexpr int BX = BX_, BY = BY_, WX = WX_, WY = WY_, kStages = STAGES_, kThreads = WX * WY * 64;
   static constexpr int NX = BX / WX / 16, NY = BY / WY / 16;   // 16 x 16 products of a wavefront
 };
@@ -163,64 +179,173 @@ __device__ __forceinline__ void meet() {
   asm volatile("" ::: "memory");
 }
 
+template <int DT, class S, Lies LX, Lies LY>
+struct Operands {
+  Operand<DT, LX, S::BX, S::kThreads> x;
+  Operand<DT, LY, S::BY, S::kThreads> y;
+  static constexpr int kLoads = decltype(x)::kLoads + decltype(y)::kLoads, kTile = (S::BX + S::BY) * kStepBytes, kY = S::BX * kStepBytes;
+
+  __device__ __forceinline__ void start(const Matrix& mx, const Matrix& my, size_t first_x, size_t first_y) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    x.start(mx, first_x, wave % S::WX * (S::BX / S::WX));
+    y.start(my, first_y, wave / S::WX * (S::BY / S::WY));
+  }
+  __device__ __forceinline__ void load(ZE_LDS char* tile, bool any) {
+    x.load(tile, any);
+    y.load(tile + kY, any);
+  }
+  __device__ __forceinline__ i32x4 read_x(const ZE_LDS char* tile, int i, int h) const { return x.read(tile, i, h); }
+  __device__ __forceinline__ i32x4 read_y(const ZE_LDS char* tile, int j, int h) const { return y.read(tile + kY, j, h); }
+};
+
+// Nothing is moved across this by the compiler.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+
+template <class F, int... I>
+__device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+
+// sum = x y + sum, in accumulation registers.  (As an instruction by name: left to itself the compiler moves half of 256 sums to and from other
+// registers in every step.  It knows nothing of the time that it takes, see product_of_four.)
+template <int DT>
+__device__ __forceinline__ void multiply_in_place(i32x4 x, i32x4 y, f32x4& sum) {
+  if constexpr (DT == kBF16) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(sum) : "v"(x), "v"(y));
+  else asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(sum) : "v"(x), "v"(y));
+}
+
+// Four wavefronts with 128 x 128 sums each, one for each SIMD: a value that is read from LDS goes into eight products, which leaves a quarter of LDS's time
+// (eight wavefronts of 128 x 64 fill all of it).  Nothing but the order of instructions hides anything here, so it is written down: of a step's
+// 128 products, two follow each read of the next half step, and five each load.  At kMeet, all of the step has been read; its place takes the loads of the step
+// after the next from there on, spread so that the cache answers them about as fast as they are asked for (all at once behind the meeting, a
+// load took 516 cycles on average; a bf16 product of 8192 x 8192 x 8192 830 us, so 748 to 764).
+template <int DT, class S, Lies LX, Lies LY>
+__device__ __forceinline__ void product_of_four(const Matrix& mx, const Matrix& my, size_t first_x, size_t first_y, int steps, f32x4 (&sum)[S::NX][S::NY]) {
+  using Both = Operands<DT, S, LX, LY>;
+  __shared__ __attribute__((aligned(1024))) char stage0[Both::kTile], stage1[Both::kTile];
+  ZE_LDS char* const stages[2] = {(ZE_LDS char*)stage0, (ZE_LDS char*)stage1};
+  constexpr int NX = S::NX, NY = S::NY, kReads = NX + NY, kHalf = NX * NY, kMeet = 40, kSpread = 5, kReadEvery = 2;
+  static_assert(S::kStages == 2 && kReads * kReadEvery <= kMeet && kMeet + (Both::kLoads - 1) * kSpread < 2 * kHalf && kReads * kReadEvery <= kHalf, "order");
+  Both both;
+  both.start(mx, my, first_x, first_y);
+#pragma unroll
+  for (int i = 0; i < NX; ++i)
+#pragma unroll
+    for (int j = 0; j < NY; ++j) sum[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  i32x4 x[2][NX], y[2][NY];
+  const auto read = [&](auto q, const ZE_LDS char* tile, auto h) __attribute__((always_inline)) {
+    if constexpr (q < NX) x[h][q] = both.read_x(tile, q, h);
+    else y[h][q - NX] = both.read_y(tile, q - NX, h);
+  };
+  using First = std::integral_constant<int, 0>;
+  using Second = std::integral_constant<int, 1>;
+  both.load(stages[0], 0 < steps);
+  both.load(stages[1], 1 < steps);
+  wait_for_loads<Both::kLoads>();
+  meet();
+  each_of([&](auto q) __attribute__((always_inline)) { read(q, stages[0], First{}); }, std::make_integer_sequence<int, kReads>{});
+  const auto step = [&](ZE_LDS char* here, const ZE_LDS char* there, bool any) __attribute__((always_inline)) {
+    const auto from_x = both.x.next(here, any);
+    const auto from_y = both.y.next(here + Both::kY, any);
+    each_of([&](auto p) __attribute__((always_inline)) {
+      constexpr int h = p / kHalf, m = p % kHalf;
+      in_order();
+      if constexpr (p == kMeet) {
+        wait_for_loads<0>();
+        meet();
+        in_order();
+      }
+      if constexpr (h == 0 && m % kReadEvery == 0 && m / kReadEvery < kReads) read(std::integral_constant<int, m / kReadEvery>{}, here, Second{});
+      if constexpr (h == 1 && m % kReadEvery == 1 && m / kReadEvery < kReads) read(std::integral_constant<int, m / kReadEvery>{}, there, First{});
+      if constexpr (p >= kMeet && (p - kMeet) % kSpread == 0 && (p - kMeet) / kSpread < Both::kLoads) {
+        constexpr int q = (p - kMeet) / kSpread;
+        if constexpr (q < both.x.kLoads) both.x.load_one(from_x, q);
+        else both.y.load_one(from_y, q - both.x.kLoads);
+      }
+      in_order();
+      multiply_in_place<DT>(x[h][m % NX], y[h][m / NX], sum[m % NX][m / NX]);
+    }, std::make_integer_sequence<int, 2 * kHalf>{});
+  };
+  for (int t = 0; t < steps; t += 2) {
+    step(stages[0], stages[1], t + 2 < steps);
+    step(stages[1], stages[0], t + 3 < steps);
+    // a sum may be read eleven issues after its product, wherever the compiler reads it behind the loop
+    asm volatile("s_nop 7\n\ts_nop 3");
+    in_order();
+  }
+  wait_for_loads<0>();
+}
+
 // The tile's sums: sum[i][j][r] is that of x = the wavefront's first + 16 i + 4 (lane / 16) + r, y = the wavefront's first + 16 j + lane % 16.
 template <int DT, class S, Lies LX, Lies LY>
 __device__ __forceinline__ void product(const Matrix& mx, const Matrix& my, size_t first_x, size_t first_y, int steps, f32x4 (&sum)[S::NX][S::NY]) {
-  constexpr int kTile = (S::BX + S::BY) * kStepBytes, kMore = S::kStages > 2 ? kTile : 16;
-  // An array for each stage: what is loaded into one is seen to leave the others alone.
-  __shared__ __attribute__((aligned(1024))) char stage0[kTile], stage1[kTile], stage2[kMore], stage3[kMore];
-  ZE_LDS char* const stages[4] = {(ZE_LDS char*)stage0, (ZE_LDS char*)stage1, (ZE_LDS char*)stage2, (ZE_LDS char*)stage3};
-  static_assert(S::kStages == 2 || S::kStages == 4, "arrays");
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  Operand<DT, LX, S::BX, S::kThreads> ox;
-  Operand<DT, LY, S::BY, S::kThreads> oy;
-  constexpr int kLoads = ox.kLoads + oy.kLoads;
-  ox.start(mx, first_x, wave % S::WX * (S::BX / S::WX));
-  oy.start(my, first_y, wave / S::WX * (S::BY / S::WY));
+  if constexpr (S::kByHand) {
+    product_of_four<DT, S, LX, LY>(mx, my, first_x, first_y, steps, sum);
+  } else {
+    using Both = Operands<DT, S, LX, LY>;
+    constexpr int kTile = Both::kTile, kMore = S::kStages > 2 ? kTile : 16;
+    // An array for each stage: what is loaded into one is seen to leave the others alone.
+    __shared__ __attribute__((aligned(1024))) char stage0[kTile], stage1[kTile], stage2[kMore], stage3[kMore];
+    ZE_LDS char* const stages[4] = {(ZE_LDS char*)stage0, (ZE_LDS char*)stage1, (ZE_LDS char*)stage2, (ZE_LDS char*)stage3};
+    static_assert(S::kStages == 2 || S::kStages == 4, "arrays");
+    Both both;
+    both.start(mx, my, first_x, first_y);
 #pragma unroll
-  for (int i = 0; i < S::NX; ++i)
+    for (int i = 0; i < S::NX; ++i)
 #pragma unroll
-    for (int j = 0; j < S::NY; ++j) sum[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
-  const auto load = [&](ZE_LDS char* tile, bool any) {
-    ox.load(tile, any);
-    oy.load(tile + S::BX * kStepBytes, any);
-  };
-  i32x4 x[2][S::NX], y[2][S::NY];
-  const auto read = [&](const ZE_LDS char* tile, int h) {
+      for (int j = 0; j < S::NY; ++j) sum[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    i32x4 x[2][S::NX], y[2][S::NY];
+    const auto read = [&](const ZE_LDS char* tile, int h) {
 #pragma unroll
-    for (int i = 0; i < S::NX; ++i) x[h][i] = ox.read(tile, i, h);
+      for (int i = 0; i < S::NX; ++i) x[h][i] = both.read_x(tile, i, h);
 #pragma unroll
-    for (int j = 0; j < S::NY; ++j) y[h][j] = oy.read(tile + S::BX * kStepBytes, j, h);
-  };
-  const auto add = [&](int h) {
+      for (int j = 0; j < S::NY; ++j) y[h][j] = both.read_y(tile, j, h);
+    };
+    const auto add = [&](int h) {
 #pragma unroll
-    for (int j = 0; j < S::NY; ++j)
+      for (int j = 0; j < S::NY; ++j)
 #pragma unroll
-      for (int i = 0; i < S::NX; ++i) sum[i][j] = multiply<DT>(x[h][i], y[h][j], sum[i][j]);
-  };
+        for (int i = 0; i < S::NX; ++i) sum[i][j] = multiply<DT>(x[h][i], y[h][j], sum[i][j]);
+    };
 
 #pragma unroll
-  for (int s = 0; s < S::kStages; ++s) load(stages[s], s < steps);
-  wait_for_loads<(S::kStages - 1) * kLoads>();
-  meet();
-  read(stages[0], 0);
-  // Half of a step is multiplied while the other half, or the next step's first, is read.  Between the halves all wavefronts have read
-  // the step for good, so that its place takes the loads of the step kStages behind it.  (Steps behind the last are zeros.)
-  for (int t = 0; t < steps; t += S::kStages) {
+    for (int s = 0; s < S::kStages; ++s) both.load(stages[s], s < steps);
+    wait_for_loads<(S::kStages - 1) * Both::kLoads>();
+    meet();
+    read(stages[0], 0);
+    // Half of a step is multiplied while the other half, or the next step's first, is read.  Between the halves all wavefronts have read
+    // the step for good, so that its place takes the loads of the step kStages behind it, before anything else is done: left to the compiler they
+    // came last.  (Steps behind the last are zeros.)
+    for (int t = 0; t < steps; t += S::kStages) {
 #pragma unroll
-    for (int s = 0; s < S::kStages; ++s) {
-      read(stages[s], 1);
-      add(0);
-      wait_for_loads<(S::kStages - 2) * kLoads>();
-      meet();
-      load(stages[s], t + s + S::kStages < steps);
-      read(stages[(s + 1) % S::kStages], 0);
-      add(1);
+      for (int s = 0; s < S::kStages; ++s) {
+        read(stages[s], 1);
+        add(0);
+        wait_for_loads<(S::kStages - 2) * Both::kLoads>();
+        meet();
+        both.load(stages[s], t + s + S::kStages < steps);
+        in_order();
+        read(stages[(s + 1) % S::kStages], 0);
+        add(1);
+      }
     }
+    // nothing may be under way into LDS when the workgroup ends or uses it for something else
+    wait_for_loads<0>();
   }
-  // nothing may be under way into LDS when the workgroup ends or uses it for something else
-  wait_for_loads<0>();
+}
+
+// Before the sums of row j are used: they and those behind them stay where they are until then.  (Where sums fill half of all registers, they cannot all be
+// taken out at once.)
+template <class S>
+__device__ __forceinline__ void rest_of_sums(f32x4 (&sum)[S::NX][S::NY], int j) {
+  if constexpr (S::kByHand) {
+#pragma unroll
+    for (int i = 0; i < S::NX; ++i)
+#pragma unroll
+      for (int k = 0; k < S::NY; ++k)
+        if (k >= j) asm volatile("" : "+a"(sum[i][k]));
+    in_order();
+  }
 }
 
 // Which tile a workgroup has, of nx x ny: neighbours in a band of eight rows of tiles follow one another in an XCD (workgroups go to the
