@@ -8,7 +8,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 SOURCES = [os.path.join(HERE, "csrc", f) for f in ("zc_kernels.hip", "zc2d_kernels.hip", "zl_kernels.hip", "zt_step.hip", "zt_norm.hip", "zt_norm_backward.hip",
                                                   "ze_embedding.hip", "ze_loss.hip")]
-DEPS = SOURCES + [os.path.join(HERE, "csrc", f) for f in ("zc_codec.h", "zc_half.h", "zc2d_codec.h", "zc2d_grid.h", "zl_codec.h", "zt_device.h", "zt_norm.h", "ze_host.h",
+DEPS = SOURCES + [os.path.join(HERE, "csrc", f) for f in ("zc_codec.h", "zc_half.h", "zc2d_codec.h", "zc2d_grid.h", "zl_codec.h", "zt_device.h", "zt_norm.h", "ze_common.h",
                                                               "ze_product.h")] + [
                   os.path.join(HERE, "..", "include", h) for h in ("zc.h", "zt.h", "ze.h")]
 LIB = os.path.join(HERE, "libzc.so")

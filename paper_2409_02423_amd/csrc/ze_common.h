@@ -1,6 +1,6 @@
-// ze_host.h -- what the host sides of the vocabulary's operators share: checks of a form, places in a workspace.
-#ifndef ZE_HOST_H
-#define ZE_HOST_H
+// ze_common.h -- what the vocabulary's operators share: sums over the lanes up to one, checks of a form, places in a workspace.
+#ifndef ZE_COMMON_H
+#define ZE_COMMON_H
 
 #include <math.h>
 
@@ -8,6 +8,20 @@
 #include "zt_device.h"
 
 namespace {
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_count(uint32_t v) {
+  return v + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, true);
+}
+// The sum over the lanes up to each one.  All 64 have to be active.
+__device__ __forceinline__ uint32_t sum_up_to(uint32_t v) {
+  v = dpp_count<0x111, 0xF>(v);   // row_shr 1, 2, 4, 8
+  v = dpp_count<0x112, 0xF>(v);
+  v = dpp_count<0x114, 0xF>(v);
+  v = dpp_count<0x118, 0xF>(v);
+  v = dpp_count<0x142, 0xA>(v);   // each row's last lane to the next row, then the second row's to the last two
+  return dpp_count<0x143, 0xC>(v);
+}
 
 constexpr size_t kMaxStride = (size_t)1 << 20;   // elements: a tile's rows are told apart by 32 bits
 
@@ -38,4 +52,4 @@ struct Places {
 };
 
 }  // namespace
-#endif  // ZE_HOST_H
+#endif  // ZE_COMMON_H

@@ -9,7 +9,7 @@
 #include <stdint.h>
 
 #include "../../include/ze.h"
-#include "ze_host.h"
+#include "ze_common.h"
 
 namespace {
 
@@ -77,59 +77,64 @@ __global__ void __launch_bounds__(kThreads) lookup_kernel(LookupArgs a) {
 
 // ---- tokens sorted by row ------------------------------------------------------------------
 
-constexpr int kSortThreads = 1024, kSortItems = 8, kSortTile = kSortThreads * kSortItems, kWaves = kSortThreads / 64, kBins = 256;
+constexpr int kSortThreads = 1024, kSortItems = 8, kSortTile = kSortThreads * kSortItems, kWaves = kSortThreads / 64, kDigitBits = 8, kBins = 1 << kDigitBits;
 // A digit's numbers of the wavefronts, one behind the other; 17 words from digit to digit, so that digits fall into different banks of LDS.
 constexpr int kCounts = kBins * (kWaves + 1);
 __device__ __forceinline__ int count_at(uint32_t digit, int wave) { return (int)digit * (kWaves + 1) + wave; }
 constexpr int kEach = kBins * kWaves / kSortThreads;
 static_assert(kEach == 4 && kWaves == 16, "four lanes for each digit");
 
-// An item's place among those with its digit in its wavefront's part of a tile (512 items that follow one another, 64 at a time), and at the end the number of
-// each digit in each wavefront's part.
-__device__ __forceinline__ void rank_items(const uint32_t (&digit)[kSortItems], uint32_t (&rank)[kSortItems], uint32_t (&counts)[kCounts]) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-  for (int i = threadIdx.x; i < kCounts; i += kSortThreads) counts[i] = 0;
+// An item's place among those with its digit in its wavefront's part of a tile (items that follow one another, 64 at a time, `rounds` times), and at the end the
+// number of each digit in each wavefront's part.
+template <int ITEMS>
+__device__ __forceinline__ void rank_items(const uint32_t (&digit)[ITEMS], int rounds, int bits, uint32_t (&rank)[ITEMS], uint32_t (&counts)[kCounts]) {
+  const int wave = threadIdx.x / 64;
+  for (int i = threadIdx.x; i < (kWaves + 1) << bits; i += kSortThreads) counts[i] = 0;
+  // the lanes with the same digit: each bit is one comparison, and takes the lanes that differ in it out
+  uint32_t low[ITEMS], high[ITEMS];
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i) {
+    if (i >= rounds) break;
+    low[i] = high[i] = 0xFFFFFFFFu;
+    for (int b = 0; b < bits; ++b) {
+      const uint32_t mine = 0u - (digit[i] >> b & 1u);
+      const uint64_t with = __builtin_amdgcn_ballot_w64(mine != 0);
+      low[i] &= ~((uint32_t)with ^ mine);
+      high[i] &= ~((uint32_t)(with >> 32) ^ mine);
+    }
+  }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kSortItems; ++i) {
-    uint64_t same = ~(uint64_t)0;
-#pragma unroll
-    for (int b = 0; b < 8; ++b) {
-      const bool bit = digit[i] >> b & 1;
-      const uint64_t with = __builtin_amdgcn_ballot_w64(bit);
-      same &= bit ? with : ~with;
-    }
+  for (int i = 0; i < ITEMS; ++i) {
+    if (i >= rounds) break;
     uint32_t* const count = &counts[count_at(digit[i], wave)];
-    const uint32_t before = __builtin_popcountll(same & (((uint64_t)1 << lane) - 1));
+    const uint32_t before = __builtin_amdgcn_mbcnt_hi(high[i], __builtin_amdgcn_mbcnt_lo(low[i], 0));
     rank[i] = *count + before;
     // (a wavefront's reads and writes of LDS happen in order: all lanes have read before one of them writes)
-    if (before == 0) *count = rank[i] + __builtin_popcountll(same);
+    if (before == 0) *count = rank[i] + __builtin_popcount(low[i]) + __builtin_popcount(high[i]);
   }
   __syncthreads();
 }
 
 // Numbers of digits in wavefronts' parts -> how many items come before each: digit by digit, and within one wavefront by wavefront.
-__device__ __forceinline__ void sum_counts(uint32_t (&counts)[kCounts], uint32_t (&buffer)[kWaves]) {
+__device__ __forceinline__ void sum_counts(uint32_t (&counts)[kCounts], int bits, uint32_t (&buffer)[kWaves]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, at = count_at(threadIdx.x / 4, threadIdx.x % 4 * kEach);
+  const bool there = threadIdx.x < 4 << bits;
   uint32_t v[kEach], sum = 0;
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
-    v[i] = counts[at + i];
+    v[i] = there ? counts[at + i] : 0;
     sum += v[i];
   }
-  uint32_t up_to = sum;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const uint32_t other = __shfl_up(up_to, d);
-    if (lane >= d) up_to += other;
-  }
+  const uint32_t up_to = sum_up_to(sum);
   if (lane == 63) buffer[wave] = up_to;
   __syncthreads();
   uint32_t before = up_to - sum;
-  for (int w = 0; w < wave; ++w) before += buffer[w];
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) before += w < wave ? buffer[w] : 0;
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
-    counts[at + i] = before;
+    if (there) counts[at + i] = before;
     before += v[i];
   }
   __syncthreads();
@@ -146,53 +151,89 @@ struct SortArgs {
   const void* ids;
   uint32_t tokens;
   long long first, rows;
-  int passes;                      // of 8 bits
+  int passes, bits;                // bits of the keys that a pass sorts by
   uint32_t *keys, *places;         // sorted: rows of the table, tokens
   uint32_t *other_keys, *other_places;
   uint32_t* table;                 // [256][tiles]
+  uint8_t* named;                  // a byte for each row: whether a token has it (NULL: it is not asked for)
   uint32_t tiles;
 };
 
-// Up to one tile: one workgroup takes all passes in LDS.  (8192 tokens, two passes: see the head of this file.)
-template <class ID>
+// (The same byte, and the same value, from several tokens.)
+__device__ __forceinline__ void name_row(const SortArgs& a, uint32_t row) { a.named[row] = 1; }
+__device__ __forceinline__ void name_none(const SortArgs& a, uint32_t thread, uint32_t threads) {
+  uint32_t* const words = reinterpret_cast<uint32_t*>(a.named);   // (up to whole words)
+  for (uint32_t i = thread; i < ((uint32_t)a.rows + 3) / 4; i += threads) words[i] = 0;
+}
+
+// Up to one tile: one workgroup takes all passes in LDS.  The tokens that have a row are brought together first (on one of four ranks they are
+// a quarter), so that the rest costs what they cost.  What bounds it is the chain of steps that wait for one another.  8192 tokens of which a quarter has a
+// row, 14 bits in two passes: SORT_FULL; 512 tokens, 10 bits in two passes: SORT_SMALL.
+template <class ID, int ITEMS>
 __global__ void __launch_bounds__(kSortThreads) sort_kernel(SortArgs a) {
-  __shared__ uint32_t keys[kSortTile], counts[kCounts], buffer[kWaves];
-  __shared__ uint16_t places[kSortTile];
+  __shared__ uint32_t keys[kSortThreads * ITEMS], counts[kCounts], buffer[kWaves];
+  __shared__ uint16_t places[kSortThreads * ITEMS];
+  static_assert(ITEMS <= 8, "two numbers for each lane of a wavefront");
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-  uint32_t key[kSortItems], place[kSortItems], digit[kSortItems], rank[kSortItems];
+  uint32_t key[ITEMS], place[ITEMS], digit[ITEMS], rank[ITEMS];
 #pragma unroll
-  for (int i = 0; i < kSortItems; ++i) {
-    place[i] = wave * (64 * kSortItems) + i * 64 + lane;
-    // those behind the last token stay behind it: they are the last ones with the greatest of keys
-    key[i] = place[i] < a.tokens ? key_of<ID>(a.ids, place[i], a.first, a.rows) : (uint32_t)a.rows;
+  for (int i = 0; i < ITEMS; ++i) {
+    const uint32_t n = i * kSortThreads + threadIdx.x;
+    key[i] = n < a.tokens ? key_of<ID>(a.ids, n, a.first, a.rows) : (uint32_t)a.rows;
   }
+  if (a.named) name_none(a, threadIdx.x, kSortThreads);   // (the barriers below stand between this and the names)
+  uint64_t has[ITEMS];
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i) {
+    has[i] = __builtin_amdgcn_ballot_w64(key[i] < (uint32_t)a.rows);
+    if (lane == 0) counts[i * kWaves + wave] = __builtin_popcountll(has[i]);
+  }
+  __syncthreads();
+  // each wavefront sums up the numbers for itself
+  const int entry = 2 * lane;
+  const uint32_t first = entry < ITEMS * kWaves ? counts[entry] : 0, second = entry < ITEMS * kWaves ? counts[entry + 1] : 0, up_to = sum_up_to(first + second);
+  const uint32_t there = (uint32_t)__builtin_amdgcn_readlane((int)up_to, 63), below = up_to - first - second;
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i) {
+    const int at = i * kWaves + wave;
+    const uint32_t before = (uint32_t)__builtin_amdgcn_readlane((int)(at & 1 ? below + first : below), at / 2);
+    const uint32_t to = before + __builtin_amdgcn_mbcnt_hi((uint32_t)(has[i] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)has[i], 0));
+    if (key[i] < (uint32_t)a.rows) {
+      keys[to] = key[i];
+      places[to] = (uint16_t)(i * kSortThreads + threadIdx.x);
+      if (a.named) name_row(a, key[i]);
+    }
+  }
+  for (uint32_t i = there + threadIdx.x; i < a.tokens; i += kSortThreads) a.keys[i] = (uint32_t)a.rows;   // tokens without a row come last
+  __syncthreads();
+  const int rounds = (int)((there + kSortThreads - 1) / kSortThreads);
   for (int pass = 0; pass < a.passes; ++pass) {
 #pragma unroll
-    for (int i = 0; i < kSortItems; ++i) digit[i] = key[i] >> (8 * pass) & 255u;
-    rank_items(digit, rank, counts);
-    sum_counts(counts, buffer);
+    for (int i = 0; i < ITEMS; ++i) {
+      if (i >= rounds) break;
+      const uint32_t at = wave * (64 * rounds) + i * 64 + lane;
+      // (those behind the last stay there: they are the last ones with the greatest of digits)
+      key[i] = at < there ? keys[at] : 0xFFFFFFFFu;
+      place[i] = at < there ? places[at] : 0;
+      digit[i] = key[i] >> (a.bits * pass) & ((1u << a.bits) - 1);
+    }
+    rank_items(digit, rounds, a.bits, rank, counts);
+    sum_counts(counts, a.bits, buffer);
+    const bool last = pass + 1 == a.passes;
 #pragma unroll
-    for (int i = 0; i < kSortItems; ++i) {
+    for (int i = 0; i < ITEMS; ++i) {
+      if (i >= rounds) break;
       const uint32_t to = counts[count_at(digit[i], wave)] + rank[i];
-      keys[to] = key[i];
-      places[to] = (uint16_t)place[i];
+      if (to >= there) continue;
+      if (last) {
+        a.keys[to] = key[i];
+        a.places[to] = place[i];
+      } else {
+        keys[to] = key[i];
+        places[to] = (uint16_t)place[i];
+      }
     }
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kSortItems; ++i) {
-      const int at = wave * (64 * kSortItems) + i * 64 + lane;
-      key[i] = keys[at];
-      place[i] = places[at];
-    }
-    __syncthreads();
-  }
-#pragma unroll
-  for (int i = 0; i < kSortItems; ++i) {
-    const uint32_t at = wave * (64 * kSortItems) + i * 64 + lane;
-    if (at < a.tokens) {
-      a.keys[at] = key[i];
-      a.places[at] = place[i];
-    }
   }
 }
 
@@ -211,10 +252,11 @@ __global__ void __launch_bounds__(kSortThreads) count_kernel(SortArgs a, int pas
   for (int i = 0; i < kSortItems; ++i) {
     const uint32_t at = blockIdx.x * kSortTile + i * kSortThreads + threadIdx.x;
     // (numbers alone: the order in which they are counted does not matter)
-    if (at < a.tokens) atomicAdd(&counts[item_key<ID>(a, in, at) >> (8 * pass) & 255u], 1u);
+    if (at < a.tokens) atomicAdd(&counts[item_key<ID>(a, in, at) >> (a.bits * pass) & ((1u << a.bits) - 1)], 1u);
   }
   __syncthreads();
-  if (threadIdx.x < kBins) a.table[(size_t)threadIdx.x * a.tiles + blockIdx.x] = counts[threadIdx.x];
+  if (threadIdx.x < 1u << a.bits) a.table[(size_t)threadIdx.x * a.tiles + blockIdx.x] = counts[threadIdx.x];
+  if (a.named && pass == 0) name_none(a, blockIdx.x * kSortThreads + threadIdx.x, gridDim.x * kSortThreads);
 }
 
 // In one workgroup: each entry of the table becomes the sum of those before it.
@@ -230,12 +272,7 @@ __global__ void __launch_bounds__(kSortThreads) sums_kernel(uint32_t* table, uin
       v[i] = at < entries ? table[at] : 0;
       sum += v[i];
     }
-    uint32_t up_to = sum;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const uint32_t other = __shfl_up(up_to, d);
-      if (lane >= d) up_to += other;
-    }
+    const uint32_t up_to = sum_up_to(sum);
     if (lane == 63) buffer[wave] = up_to;
     __syncthreads();
     uint32_t mine = before + up_to - sum;
@@ -264,15 +301,15 @@ __global__ void __launch_bounds__(kSortThreads) scatter_kernel(SortArgs a, int p
     const bool there = at < a.tokens;
     key[i] = there ? item_key<ID>(a, in, at) : 0xFFFFFFFFu;
     place[i] = there ? (in_places ? in_places[at] : at) : 0;
-    digit[i] = key[i] >> (8 * pass) & 255u;   // those behind the last token: 255, behind all others in the last tile
+    digit[i] = key[i] >> (a.bits * pass) & ((1u << a.bits) - 1);   // those behind the last token: the greatest, behind all others in the last tile
   }
-  rank_items(digit, rank, counts);
+  rank_items(digit, kSortItems, a.bits, rank, counts);
   // sums over the wavefronts of each digit: four lanes have a digit's sixteen numbers
   const int at_digit = count_at(threadIdx.x / 4, threadIdx.x % 4 * kEach);
   uint32_t v[kEach], sum = 0;
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
-    v[i] = counts[at_digit + i];
+    v[i] = counts[at_digit + i];   // (digits past the last have none, but what they hold is not used)
     sum += v[i];
   }
   uint32_t up_to = sum;
@@ -281,11 +318,13 @@ __global__ void __launch_bounds__(kSortThreads) scatter_kernel(SortArgs a, int p
     const uint32_t other = __shfl_up(up_to, d, 4);
     if ((lane & 3) >= d) up_to += other;
   }
-  uint32_t before = a.table[(size_t)(threadIdx.x / 4) * a.tiles + blockIdx.x] + up_to - sum;
+  if (threadIdx.x < 4u << a.bits) {
+    uint32_t before = a.table[(size_t)(threadIdx.x / 4) * a.tiles + blockIdx.x] + up_to - sum;
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    counts[at_digit + i] = before;
-    before += v[i];
+    for (int i = 0; i < kEach; ++i) {
+      counts[at_digit + i] = before;
+      before += v[i];
+    }
   }
   __syncthreads();
 #pragma unroll
@@ -295,6 +334,7 @@ __global__ void __launch_bounds__(kSortThreads) scatter_kernel(SortArgs a, int p
     const uint32_t to = counts[count_at(digit[i], wave)] + rank[i];
     out[to] = key[i];
     out_places[to] = place[i];
+    if (a.named && pass + 1 == a.passes && key[i] < (uint32_t)a.rows) name_row(a, key[i]);
   }
 }
 
@@ -316,19 +356,15 @@ struct SumArgs {
   float scale;
   int accumulate;
   unsigned sum_groups;             // workgroups that add up; those behind them write zeros
+  const uint8_t* named;            // a byte for each row: whether a token has it (NULL: none has)
 };
 
-// A vector of sums into its row of the gradient, or its row plus them.
+// A vector of sums into its row of the gradient, or the row as it was plus them.
 template <int DT, int DO>
-__device__ __forceinline__ void store_sums(const SumArgs& a, uint32_t row, int vector, const float (&sum)[kVec<DT>]) {
+__device__ __forceinline__ void store_sums(const SumArgs& a, uint32_t row, int vector, const float (&sum)[kVec<DT>], const Raw<DO, kVec<DT>>& old) {
   constexpr int kN = kVec<DT>;
-  char* const to = a.dtable + (size_t)row * a.stride_dtable;
-  const int valid = a.cols - vector * kN;
-  const uint32_t at = (uint32_t)vector * kN * kBytes<DO>;
   float v[kN];
   if (a.accumulate) {
-    Raw<DO, kN> old;
-    old.load(to, at, valid);
     old.unpack(v);
 #pragma unroll
     for (int j = 0; j < kN; ++j) v[j] += a.scale * sum[j];
@@ -338,7 +374,12 @@ __device__ __forceinline__ void store_sums(const SumArgs& a, uint32_t row, int v
   }
   Raw<DO, kN> raw;
   raw.pack(v);
-  raw.store(to, at, valid);
+  raw.store(a.dtable + (size_t)row * a.stride_dtable, (uint32_t)vector * kN * kBytes<DO>, a.cols - vector * kN);
+}
+template <int DT, int DO>
+__device__ __forceinline__ void load_old(const SumArgs& a, uint32_t row, int vector, Raw<DO, kVec<DT>>& old) {
+  constexpr int kN = kVec<DT>;
+  old.load(a.dtable + (size_t)row * a.stride_dtable, (uint32_t)vector * kN * kBytes<DO>, a.cols - vector * kN);
 }
 
 template <int DT>
@@ -354,7 +395,8 @@ __device__ __forceinline__ void keep(float* to, const float (&v)[N]) {
 }
 
 // One piece of the sorted list, in 64 vectors of the columns.  A run of tokens with the same row that begins and ends in the piece is stored; the part of one that
-// comes from the piece before is kept as the piece's first, that of one which goes on (and began here) as its second.
+// comes from the piece before is kept as the piece's first, that of one which goes on (and began here) as its second.  What is read of eight tokens is
+// asked for at once: their rows, and with `accumulate` the gradient's rows that are done among them.
 template <int DT, int DO>
 __device__ __forceinline__ void add_piece(const SumArgs& a, uint32_t piece, int vector) {
   constexpr int kN = kVec<DT>, kAhead = 8;
@@ -373,49 +415,41 @@ __device__ __forceinline__ void add_piece(const SumArgs& a, uint32_t piece, int 
   bool began = (uint32_t)__builtin_amdgcn_readlane((int)keys, 0) != before;   // the present run, in this piece
   for (uint32_t i = 0; i < count; i += kAhead) {
     Raw<DT> raw[kAhead];
+    Raw<DO, kN> old[kAhead];
+    uint32_t key[kAhead];
+    bool ends[kAhead], own[kAhead];   // the run at the token, or its part in this piece; and it began here
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const uint32_t q = i + u < count ? i + u : count - 1;
-      const uint32_t key = (uint32_t)__builtin_amdgcn_readlane((int)keys, (int)q);
-      const char* row = a.dout + (size_t)(uint32_t)__builtin_amdgcn_readlane((int)places, (int)q) * a.stride_dout;
-      if (key < a.rows && i + u < count) raw[u].load(row, there ? at : 0, valid);
+      key[u] = i + u < count ? (uint32_t)__builtin_amdgcn_readlane((int)keys, (int)q) : a.rows;
+      const uint32_t next = q + 1 == count ? behind : (uint32_t)__builtin_amdgcn_readlane((int)keys, (int)q + 1);
+      ends[u] = next != key[u] || q + 1 == count;
+      own[u] = began;
+      if (key[u] >= a.rows) continue;   // without a row
+      raw[u].load(a.dout + (size_t)(uint32_t)__builtin_amdgcn_readlane((int)places, (int)q) * a.stride_dout, there ? at : 0, valid);
+      if (a.accumulate && there && began && next != key[u]) load_old<DT, DO>(a, key[u], vector, old[u]);
+      began = began || ends[u];
     }
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      if (i + u >= count) break;
-      const uint32_t key = (uint32_t)__builtin_amdgcn_readlane((int)keys, (int)(i + u));
-      if (key >= a.rows) return;   // tokens without a row come last
+      if (key[u] >= a.rows) return;   // tokens without a row come last
       float v[kN];
       raw[u].unpack(v);
 #pragma unroll
       for (int j = 0; j < kN; ++j) sum[j] += v[j];
-      const bool last = i + u + 1 == count;
-      const uint32_t next = last ? behind : (uint32_t)__builtin_amdgcn_readlane((int)keys, (int)(i + u + 1));
-      if (next == key && !last) continue;
+      if (!ends[u]) continue;
       if (there) {
-        if (!began) keep(kept_at<DT>(a, piece, 0, vector), sum);
-        else if (next == key) keep(kept_at<DT>(a, piece, 1, vector), sum);
-        else store_sums<DT, DO>(a, key, vector, sum);
+        if (!own[u]) keep(kept_at<DT>(a, piece, 0, vector), sum);
+        else if (i + u + 1 == count && behind == key[u]) keep(kept_at<DT>(a, piece, 1, vector), sum);
+        else store_sums<DT, DO>(a, key[u], vector, sum, old[u]);
       }
 #pragma unroll
       for (int j = 0; j < kN; ++j) sum[j] = 0.0f;
-      began = true;
     }
   }
 }
 
-// First row at or behind which the sorted keys are `key` or more.
-__device__ __forceinline__ uint32_t first_of(const uint32_t* keys, uint32_t count, uint32_t key) {
-  uint32_t lo = 0, hi = count;
-  while (lo < hi) {
-    const uint32_t mid = (lo + hi) / 2;
-    if (keys[mid] < key) lo = mid + 1;
-    else hi = mid;
-  }
-  return lo;
-}
-
-constexpr int kZeroRows = 16;   // of a workgroup
+constexpr int kZeroRows = 4;   // of a workgroup
 
 template <int DT, int DO>
 __global__ void __launch_bounds__(kThreads) sum_kernel(SumArgs a) {
@@ -426,27 +460,27 @@ __global__ void __launch_bounds__(kThreads) sum_kernel(SumArgs a) {
     return;
   }
   // zeros for the rows that no token has
-  __shared__ uint32_t ends[kZeroRows + 1];
   constexpr int kN = kVec<DO>;
   Raw<DO> zero;
 #pragma unroll
   for (int i = 0; i < zero.kWords; ++i) zero.w[i] = 0;
   for (uint32_t row0 = (blockIdx.x - a.sum_groups) * kZeroRows; row0 < a.rows; row0 += (gridDim.x - a.sum_groups) * kZeroRows) {
-    if (threadIdx.x <= kZeroRows) ends[threadIdx.x] = first_of(a.keys, a.tokens, row0 + threadIdx.x);
-    __syncthreads();
+    const uint32_t named = a.named ? *reinterpret_cast<const uint32_t*>(a.named + row0) : 0;
     for (int r = 0; r < kZeroRows; ++r) {
-      if (row0 + r >= a.rows || ends[r] != ends[r + 1]) continue;
+      if (row0 + r >= a.rows || named >> 8 * r & 1) continue;
       char* const row = a.dtable + (size_t)(row0 + r) * a.stride_dtable;
-      for (int x = threadIdx.x * kN; x < a.cols; x += kThreads * kN) zero.store(row, (uint32_t)x * kBytes<DO>, a.cols - x);
+      for (int x = threadIdx.x * kN; x < a.cols; x += kThreads * kN) {
+        if (x + kN <= a.cols) zero.template store<true>(row, (uint32_t)x * kBytes<DO>);
+        else zero.store(row, (uint32_t)x * kBytes<DO>, a.cols - x);
+      }
     }
-    __syncthreads();
   }
 }
 
 // The rows whose tokens do not lie within a piece: the sums that were kept of them, from the piece that they begin in.
 template <int DT, int DO>
 __device__ __forceinline__ void join_from(const SumArgs& a, uint32_t piece, int vector) {
-  constexpr int kN = kVec<DT>, kAhead = 4;
+  constexpr int kN = kVec<DT>, kAhead = 8;
   typedef float f4 __attribute__((ext_vector_type(4)));
   const uint32_t from = piece * (uint32_t)a.piece, next = from + (uint32_t)a.piece;
   if (piece + 1 >= a.pieces) return;
@@ -454,13 +488,22 @@ __device__ __forceinline__ void join_from(const SumArgs& a, uint32_t piece, int 
   if (key >= a.rows || a.keys[next] != key) return;
   // a run that fills the piece and comes from the one before it began there
   if (a.keys[from] == key && from > 0 && a.keys[from - 1] == key) return;
+  // the run's last piece: 64 of their first keys are compared at once
+  uint32_t last = piece;
+  for (;;) {
+    const uint32_t q = last + 1 + (threadIdx.x & 63);
+    const uint64_t same = __builtin_amdgcn_ballot_w64(q < a.pieces && a.keys[q * (size_t)a.piece] == key);
+    const int many = ~same ? __builtin_ctzll(~same) : 64;
+    last += many;
+    if (many < 64) break;
+  }
   if (vector >= a.vectors) return;
+  Raw<DO, kN> old;
+  if (a.accumulate) load_old<DT, DO>(a, key, vector, old);
   float sum[kN];
   const float* p = kept_at<DT>(a, piece, 1, vector);
 #pragma unroll
   for (int j = 0; j < kN; ++j) sum[j] = p[j];
-  const uint32_t to = first_of(a.keys, a.tokens, key + 1);               // behind the run's last token
-  const uint32_t last = (to - 1) / (uint32_t)a.piece;                    // its piece
   for (uint32_t q = piece + 1; q <= last; q += kAhead) {
     f4 v[kAhead][kN / 4];
 #pragma unroll
@@ -474,7 +517,7 @@ __device__ __forceinline__ void join_from(const SumArgs& a, uint32_t piece, int 
         for (int j = 0; j < kN; ++j) sum[j] += v[u][j / 4][j % 4];
       }
   }
-  store_sums<DT, DO>(a, key, vector, sum);
+  store_sums<DT, DO>(a, key, vector, sum, old);
 }
 
 template <int DT, int DO>
@@ -488,16 +531,20 @@ __global__ void __launch_bounds__(kThreads) join_kernel(SumArgs a) {
 
 struct Plan {
   uint32_t tiles, pieces;
-  int piece, passes, vectors;
-  size_t keys, places, other_keys, other_places, table, kept, bytes;
+  int piece, passes, bits, vectors;
+  size_t keys, places, other_keys, other_places, table, named, kept, bytes;
 };
 
 Plan plan_for(const struct ze_form& f) {
   Plan p = {};
   p.vectors = (int)parts(f.cols, 16 / dtype_bytes(f.dtype));
   p.tiles = (uint32_t)parts(f.tokens, kSortTile);
-  p.passes = f.rows < 1u << 8 ? 1 : f.rows < 1u << 16 ? 2 : f.rows < 1u << 24 ? 3 : 4;   // keys up to `rows`
-  p.piece = f.tokens <= 16384 ? 16 : f.tokens <= 65536 ? 32 : kMostPiece;
+  int bits = 1;
+  while (f.rows >> bits) ++bits;   // of keys up to `rows`
+  p.passes = (bits + kDigitBits - 1) / kDigitBits;
+  p.bits = (bits + p.passes - 1) / p.passes;
+  // Short pieces where there are few of them, so that none waits for a second load; else longer ones, which keep less.
+  p.piece = parts(f.tokens, 16) * parts((size_t)p.vectors, 64) <= 2048 ? 8 : f.tokens <= 16384 ? 16 : f.tokens <= 65536 ? 32 : kMostPiece;
   p.pieces = (uint32_t)parts(f.tokens, (size_t)p.piece);
   Places places;
   p.keys = places.take(f.tokens * 4);
@@ -507,6 +554,7 @@ Plan plan_for(const struct ze_form& f) {
     p.other_places = places.take(f.tokens * 4);
     p.table = places.take((size_t)p.tiles * kBins * 4);
   }
+  p.named = places.take(up(f.rows, 4));
   p.kept = places.take((size_t)p.pieces * 2 * p.vectors * (16 / dtype_bytes(f.dtype)) * 4);
   p.bytes = places.at;
   return p;
@@ -515,7 +563,10 @@ Plan plan_for(const struct ze_form& f) {
 template <class ID>
 void sort_tokens(const SortArgs& a, const Plan& p, char* work, hipStream_t s) {
   if (p.tiles == 1) {
-    hipLaunchKernelGGL(sort_kernel<ID>, dim3(1), dim3(kSortThreads), 0, s, a);
+    const dim3 one(1), threads(kSortThreads);
+    if (a.tokens <= kSortThreads) hipLaunchKernelGGL((sort_kernel<ID, 1>), one, threads, 0, s, a);
+    else if (a.tokens <= kSortThreads * 4) hipLaunchKernelGGL((sort_kernel<ID, 4>), one, threads, 0, s, a);
+    else hipLaunchKernelGGL((sort_kernel<ID, kSortItems>), one, threads, 0, s, a);
     return;
   }
   const uint32_t *in = nullptr, *in_places = nullptr;
@@ -523,7 +574,7 @@ void sort_tokens(const SortArgs& a, const Plan& p, char* work, hipStream_t s) {
     const bool own = (p.passes - pass) % 2 == 1;   // the last pass writes what is read
     uint32_t *out = own ? a.keys : a.other_keys, *out_places = own ? a.places : a.other_places;
     hipLaunchKernelGGL(count_kernel<ID>, dim3(p.tiles), dim3(kSortThreads), 0, s, a, pass, in);
-    hipLaunchKernelGGL(sums_kernel, dim3(1), dim3(kSortThreads), 0, s, a.table, p.tiles * kBins);
+    hipLaunchKernelGGL(sums_kernel, dim3(1), dim3(kSortThreads), 0, s, a.table, p.tiles << a.bits);
     hipLaunchKernelGGL(scatter_kernel<ID>, dim3(p.tiles), dim3(kSortThreads), 0, s, a, pass, in, in_places, out, out_places);
     in = out;
     in_places = out_places;
@@ -610,12 +661,14 @@ int ze_embedding_backward(const struct ze_form* form, const void* d_ids, const v
     a.first = f.first;
     a.rows = (long long)f.rows;
     a.passes = p.passes;
+    a.bits = p.bits;
     a.keys = in_work(p.keys);
     a.places = in_work(p.places);
     a.other_keys = in_work(p.other_keys);
     a.other_places = in_work(p.other_places);
     a.table = in_work(p.table);
     a.tiles = p.tiles;
+    a.named = accumulate ? nullptr : reinterpret_cast<uint8_t*>(work + p.named);
     if (f.id_dtype == ZE_I64) sort_tokens<long long>(a, p, work, s);
     else sort_tokens<int>(a, p, work, s);
   }
@@ -635,6 +688,7 @@ int ze_embedding_backward(const struct ze_form* form, const void* d_ids, const v
   a.pieces = p.pieces;
   a.scale = f.scale;
   a.accumulate = accumulate;
+  a.named = f.tokens && !accumulate ? reinterpret_cast<const uint8_t*>(work + p.named) : nullptr;
 #define LAUNCH(DT)                                                     \
   do {                                                                 \
     if (f.grad_dtype == ZC_F32) launch_sums<DT, kF32>(a, f.rows, s);   \

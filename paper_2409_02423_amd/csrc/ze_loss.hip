@@ -10,7 +10,7 @@
 #include <stdint.h>
 
 #include "../../include/ze.h"
-#include "ze_host.h"
+#include "ze_common.h"
 #include "ze_product.h"
 
 namespace {
@@ -63,13 +63,7 @@ __global__ void __launch_bounds__(kListThreads) list_kernel(const ID* ids, int t
     }
     __syncthreads();
     if (wave == 0) {
-      const int a = counts[2 * lane], b = counts[2 * lane + 1];
-      int sum = a + b;
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        const int other = __shfl_up(sum, d);
-        if (lane >= d) sum += other;
-      }
+      const int a = counts[2 * lane], b = counts[2 * lane + 1], sum = (int)sum_up_to((uint32_t)(a + b));
       counts[2 * lane] = sum - a - b;
       counts[2 * lane + 1] = sum - b;
       if (lane == 63) counts[kListRounds * 16] = sum;
