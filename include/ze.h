@@ -72,8 +72,8 @@ int ze_embedding_backward(const struct ze_form* form, const void* d_ids, const v
  * without rows), the sum of exp(l - m), and the label's logit (-inf where the label is not one of this rank's). A
  * token without a label gets -inf, 0, 0.  A logit of +inf counts as not a number.
  *
- * How much workspace a call needs depends on whether d_hidden and d_table can be read as they are (rows that start at multiples of 16 bytes
- * and are a multiple of 128 bytes long) or have to be copied; ze_loss_work_bytes and ze_loss_backward_work_bytes look at the pointers'
+ * How much workspace a call needs depends on whether d_hidden and d_table can be read as they are (rows that start at multiples of 4 bytes)
+ * or have to be copied; ze_loss_work_bytes and ze_loss_backward_work_bytes look at the pointers'
  * values for that, and give enough for any place where one is NULL.
  */
 size_t ze_loss_work_bytes(const struct ze_form* form, const void* d_hidden, const void* d_table);

@@ -50,10 +50,15 @@ __global__ void __launch_bounds__(kListThreads) list_kernel(const ID* ids, int t
   float most = 0.0f;
   for (int base = 0; base < tokens; base += kListRounds * kListThreads) {
     long long id[kListRounds];
+    float of_lse[kListRounds], of_dloss[kListRounds];
 #pragma unroll
     for (int i = 0; i < kListRounds; ++i) {
       const int n = base + i * kListThreads + tid;
       id[i] = n < tokens ? (long long)ids[n] : -1;
+      if (lse) {
+        of_lse[i] = n < tokens ? lse[n] : 0.0f;
+        of_dloss[i] = n < tokens ? dloss[n] : 0.0f;
+      }
     }
     uint64_t there[kListRounds];
 #pragma unroll
@@ -82,9 +87,9 @@ __global__ void __launch_bounds__(kListThreads) list_kernel(const ID* ids, int t
       list.label_of[row] = local >= 0 && local < rows ? (int)local : -1;
       if (list.target) list.target[row] = -kInf;
       if (lse) {
-        const float d = dloss[n], size = fabsf(d);
-        list.lse[row] = lse[n];
-        list.dloss[row] = d;
+        const float size = fabsf(of_dloss[i]);
+        list.lse[row] = of_lse[i];
+        list.dloss[row] = of_dloss[i];
         if (size < kInf) most = fmaxf(most, size);
       }
     }
@@ -123,24 +128,35 @@ struct PackArgs {
   int cols;
 };
 
+// Of row r of the copy, 16 bytes at `at`.
+template <int DT>
+__device__ __forceinline__ void pack_piece(const PackArgs& a, size_t r, long long source, uint32_t at) {
+  constexpr int kN = kVec<DT>;
+  Raw<DT> raw;
+  const int valid = source < 0 ? 0 : a.cols - (int)(at / kBytes<DT>);
+  const char* in = a.in + (source < 0 ? 0 : (size_t)source) * a.stride;
+  if (valid >= kN) {
+    raw.load(in, at);
+  } else {
+#pragma unroll
+    for (int i = 0; i < raw.kWords; ++i) raw.w[i] = 0;
+    if (valid > 0) raw.load(in, at, valid);
+  }
+  raw.store(a.out + r * a.out_stride, at);
+}
+__device__ __forceinline__ long long source_of(const PackArgs& a, size_t r) { return a.token_of ? (long long)a.token_of[r] : r < a.rows ? (long long)r : -1; }
+
 template <int DT>
 __device__ __forceinline__ void pack_row(const PackArgs& a, size_t r) {
-  constexpr int kN = kVec<DT>;
-  const long long source = a.token_of ? (long long)a.token_of[r] : r < a.rows ? (long long)r : -1;
-  const char* in = a.in + (source < 0 ? 0 : (size_t)source) * a.stride;
-  char* out = a.out + r * a.out_stride;
-  for (uint32_t at = threadIdx.x * 16; at < a.out_stride; at += kThreads * 16) {
-    Raw<DT> raw;
-    const int valid = source < 0 ? 0 : a.cols - (int)(at / kBytes<DT>);
-    if (valid >= kN) {
-      raw.load(in, at);
-    } else {
-#pragma unroll
-      for (int i = 0; i < raw.kWords; ++i) raw.w[i] = 0;
-      if (valid > 0) raw.load(in, at, valid);
-    }
-    raw.store(out, at);
-  }
+  const long long source = source_of(a, r);
+  for (uint32_t at = threadIdx.x * 16; at < a.out_stride; at += kThreads * 16) pack_piece<DT>(a, r, source, at);
+}
+
+// The same of rows of one step each (a row's ends): eight lanes a row.
+template <int DT>
+__global__ void __launch_bounds__(kThreads) pack_ends_kernel(PackArgs a, size_t rows) {
+  const size_t r = ((size_t)blockIdx.x * kThreads + threadIdx.x) / 8;
+  if (r < rows) pack_piece<DT>(a, r, source_of(a, r), threadIdx.x % 8 * 16);
 }
 
 template <int DT>
@@ -172,6 +188,8 @@ __global__ void __launch_bounds__(kThreads) zero_rows_kernel(char* out, size_t s
   zero_row(out + (from + blockIdx.x) * stride, bytes);
 }
 
+__device__ __forceinline__ bool any_lane(bool b) { return __builtin_amdgcn_ballot_w64(b) != 0; }
+
 // ---- forward -----------------------------------------------------------------------------
 
 struct Part {
@@ -180,6 +198,7 @@ struct Part {
 
 struct LogitsArgs {
   Matrix table, hidden;        // the piece's rows; the rows with a label
+  Ends table_ends, hidden_ends;
   const Head* head;
   const int* label_of;
   int nx, ny, steps;           // tiles, and steps of k
@@ -190,17 +209,33 @@ struct LogitsArgs {
   float* target;
 };
 
+// Products of hidden states and rows of the table, whose ends may be apart.
+template <int DT, class S, class ARGS>
+__device__ __forceinline__ void product_with_ends(const ARGS& a, int tx, int ty, f32x4 (&sum)[S::NX][S::NY]) {
+  using Both = Operands<DT, S, kAlong, kAlong>;
+  const size_t x = (size_t)tx * S::BX, y = (size_t)ty * S::BY;
+  Both both(a.table, a.hidden, x, y);
+  if (a.table_ends.at) {
+    Both ends(Matrix{a.table_ends.at, a.table_ends.bytes, a.table_ends.stride, nullptr}, Matrix{a.hidden_ends.at, a.hidden_ends.bytes, a.hidden_ends.stride, nullptr}, x, y);
+    product(both, &ends, a.steps, sum);
+  } else {
+    product(both, (Both*)nullptr, a.steps, sum);
+  }
+}
+
 // The greatest logit and the sum of exponentials in each wavefront's part of a row.  In a tile that is all there is of them: 4 x 16 columns to
 // a lane group, so a row's maximum takes NX x 4 comparisons in a lane and two across lanes.
 template <int DT, class S>
 __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a) {
-  int tx, ty;
-  tile_of(a.nx, a.ny, tx, ty);
+  // (tiles of rows that have a label: as many for each XCD, however many tokens have none)
   const int there = a.head->rows;
-  if (ty * S::BY >= there) return;
+  int tx, ty;
+  if (!tile_of(a.nx, (there + S::BY - 1) / S::BY, tx, ty)) return;
   f32x4 sum[S::NX][S::NY];
-  product<DT, S, kAlong, kAlong>(a.table, a.hidden, (size_t)tx * S::BX, (size_t)ty * S::BY, a.steps, sum);
+  product_with_ends<DT, S>(a, tx, ty, sum);
   const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, wx = wave % S::WX, wy = wave / S::WX;
+  const int x_wave = __builtin_amdgcn_readfirstlane(tx * S::BX + wx * (S::BX / S::WX));
+  const bool edge = x_wave + S::BX / S::WX > a.rows;
   const int x0 = tx * S::BX + wx * (S::BX / S::WX) + lane / 16 * 4, y0 = ty * S::BY + wy * (S::BY / S::WY) + (lane & 15);
 #pragma unroll
   for (int j = 0; j < S::NY; ++j) {
@@ -208,17 +243,27 @@ __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a) {
     const int y = y0 + 16 * j;
     if (y >= there) continue;
     const int label = a.label_of[y] - a.v0;
+    f32x4 l[S::NX];
+#pragma unroll
+    for (int i = 0; i < S::NX; ++i) l[i] = a.scale * sum[i][j];
+    if (edge) {
+#pragma unroll
+      for (int i = 0; i < S::NX; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) l[i][r] = x0 + 16 * i + r < a.rows ? l[i][r] : -kInf;
+    }
+    if (any_lane((unsigned)(label - x_wave) < (unsigned)(S::BX / S::WX))) {   // few parts of rows have a label
+#pragma unroll
+      for (int i = 0; i < S::NX; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (x0 + 16 * i + r == label && label < a.rows) a.target[y] = l[i][r];
+    }
     float most = -kInf;
 #pragma unroll
     for (int i = 0; i < S::NX; ++i)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int x = x0 + 16 * i + r;
-        const float l = x < a.rows ? a.scale * sum[i][j][r] : -kInf;
-        sum[i][j][r] = l;
-        most = fmaxf(most, l);
-        if (x == label && x < a.rows) a.target[y] = l;
-      }
+      for (int r = 0; r < 4; ++r) most = fmaxf(most, l[i][r]);
     most = fmaxf(most, __shfl_xor(most, 16));
     most = fmaxf(most, __shfl_xor(most, 32));
     const float from = most == -kInf ? 0.0f : most;   // nothing there: exp(-inf) = 0 each
@@ -226,11 +271,18 @@ __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a) {
 #pragma unroll
     for (int i = 0; i < S::NX; ++i)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) total += __builtin_amdgcn_exp2f((sum[i][j][r] - from) * kLog2E);
+      for (int r = 0; r < 4; ++r) total += __builtin_amdgcn_exp2f((l[i][r] - from) * kLog2E);
     total += __shfl_xor(total, 16);
     total += __shfl_xor(total, 32);
     if (lane < 16) a.parts[y * a.parts_stride + tx * S::WX + wx] = Part{most, total};
   }
+}
+
+// Joins parts of a sum of exponentials: the sums are taken to the greater of the two logits.  (Where that is -inf there is nothing in either.)
+__device__ __forceinline__ void join(float& most, float& total, float other_most, float other) {
+  const float to = fmaxf(most, other_most), from = to == -kInf ? 0.0f : to;
+  total = total * __builtin_amdgcn_exp2f((most - from) * kLog2E) + other * __builtin_amdgcn_exp2f((other_most - from) * kLog2E);
+  most = to;
 }
 
 // Joins a row's parts: a wavefront for each token.
@@ -243,13 +295,24 @@ __global__ void __launch_bounds__(kThreads) stats_kernel(const int* row_of, size
   float most = -kInf, total = 0.0f;
   if (row >= 0) {
     const Part* p = parts + (size_t)row * stride;
-    for (size_t i = lane; i < count; i += 64) most = fmaxf(most, p[i].most);
+    constexpr int kAhead = 4;
+    for (size_t i = lane; i < count; i += 64 * kAhead) {
+      Part part[kAhead];
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
-    const float from = most == -kInf ? 0.0f : most;
-    for (size_t i = lane; i < count; i += 64) total += p[i].sum * __builtin_amdgcn_exp2f((p[i].most - from) * kLog2E);
+      for (int u = 0; u < kAhead; ++u) part[u] = i + 64 * u < count ? p[i + 64 * u] : Part{-kInf, 0.0f};
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) total += __shfl_xor(total, d);
+      for (int u = 0; u < kAhead; ++u) join(most, total, part[u].most, part[u].sum);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      // (from one lane to the other and back the same two are joined: the same result in both)
+      const float other_most = __shfl_xor(most, d), other = __shfl_xor(total, d);
+      const bool first = (lane & d) == 0;
+      float m = first ? most : other_most, t = first ? total : other;
+      join(m, t, first ? other_most : most, first ? other : total);
+      most = m;
+      total = t;
+    }
   }
   if (lane == 0) {
     stats[n] = most;
@@ -267,16 +330,14 @@ __global__ void __launch_bounds__(kThreads) join_kernel(size_t tokens, int ranks
     lse[n] = 0.0f;
     return;
   }
-  float most = -kInf, target = -kInf;
+  float most = -kInf, total = 0.0f, target = -kInf;
+#pragma unroll 4
   for (int r = 0; r < ranks; ++r) {
-    most = fmaxf(most, stats[(size_t)r * 3 * tokens + n]);
-    target = fmaxf(target, stats[((size_t)r * 3 + 2) * tokens + n]);
+    const float* of = stats + (size_t)r * 3 * tokens + n;
+    join(most, total, of[0], of[tokens]);
+    target = fmaxf(target, of[2 * tokens]);
   }
-  const float from = most == -kInf ? 0.0f : most;
-  float total = 0.0f;
-  for (int r = 0; r < ranks; ++r)
-    total += stats[((size_t)r * 3 + 1) * tokens + n] * __builtin_amdgcn_exp2f((stats[(size_t)r * 3 * tokens + n] - from) * kLog2E);
-  const float l = from + logf(total);
+  const float l = (most == -kInf ? 0.0f : most) + logf(total);
   lse[n] = l;
   if (loss) loss[n] = l - target;
 }
@@ -288,27 +349,31 @@ template <int DT> constexpr float kLift = DT == kF16 ? 32768.0f : 1.0f;
 
 struct GradientArgs {
   Matrix table, hidden;
+  Ends table_ends, hidden_ends;
   const Head* head;
   const int* label_of;
   const float *lse, *dloss;
   int nx, ny, steps;
   int v0, rows, rows_padded;   // of the piece; padded to whole steps
   float scale;
-  char* g;                     // [rows with a label, to a whole step][rows_padded]
+  char* g;                     // [rows with a label, to a whole step], the piece's first column
+  size_t g_stride;             // bytes
 };
 
 // g of a tile, zeros behind the piece's last row and behind the last row with a label, up to whole steps of the products that read it.
 template <int DT, class S>
 __global__ void __launch_bounds__(S::kThreads) gradient_kernel(GradientArgs a) {
-  int tx, ty;
-  tile_of(a.nx, a.ny, tx, ty);
+  // (tiles of rows that have a label: as many for each XCD, however many tokens have none)
   const int there = a.head->rows;
-  if (ty * S::BY >= there) return;
+  int tx, ty;
+  if (!tile_of(a.nx, (there + S::BY - 1) / S::BY, tx, ty)) return;
   f32x4 sum[S::NX][S::NY];
-  product<DT, S, kAlong, kAlong>(a.table, a.hidden, (size_t)tx * S::BX, (size_t)ty * S::BY, a.steps, sum);
+  product_with_ends<DT, S>(a, tx, ty, sum);
   const float most = a.head->most;
   const int padded = (there + kStep<DT> - 1) / kStep<DT> * kStep<DT>;
   const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, wx = wave % S::WX, wy = wave / S::WX;
+  const int x_wave = __builtin_amdgcn_readfirstlane(tx * S::BX + wx * (S::BX / S::WX));
+  const bool edge = x_wave + S::BX / S::WX > a.rows || (ty + 1) * S::BY > there;
   const int x0 = tx * S::BX + wx * (S::BX / S::WX) + lane / 16 * 4, y0 = ty * S::BY + wy * (S::BY / S::WY) + (lane & 15);
 #pragma unroll
   for (int j = 0; j < S::NY; ++j) {
@@ -317,19 +382,25 @@ __global__ void __launch_bounds__(S::kThreads) gradient_kernel(GradientArgs a) {
     if (y >= padded) continue;
     const int label = a.label_of[y] - a.v0;
     const float lse = a.lse[y], factor = most > 0.0f ? a.dloss[y] / most * kLift<DT> : a.dloss[y];
-    char* const row = a.g + (size_t)y * a.rows_padded * kBytes<DT>;
+    char* const row = a.g + (size_t)y * a.g_stride;
+    const bool has = any_lane((unsigned)(label - x_wave) < (unsigned)(S::BX / S::WX));   // few parts of rows have a label
 #pragma unroll
     for (int i = 0; i < S::NX; ++i) {
       const int x = x0 + 16 * i;
       float v[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float p = __builtin_amdgcn_exp2f((a.scale * sum[i][j][r] - lse) * kLog2E);
-        v[r] = x + r < a.rows && y < there ? factor * (p - (x + r == label ? 1.0f : 0.0f)) : 0.0f;
+      for (int r = 0; r < 4; ++r) v[r] = factor * __builtin_amdgcn_exp2f(fmaf(a.scale, sum[i][j][r], -lse) * kLog2E);
+      if (has) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] -= x + r == label ? factor : 0.0f;
+      }
+      if (edge) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = x + r < a.rows && y < there ? v[r] : 0.0f;
       }
       Raw<DT, 4> raw;
       raw.pack(v);
-      if (x < a.rows_padded) raw.store(row, x * kBytes<DT>);
+      if (!edge || x < a.rows_padded) raw.store(row, x * kBytes<DT>);
     }
   }
 }
@@ -344,19 +415,29 @@ struct OutArgs {
   char* out;                   // of type DT
   size_t out_stride;           // bytes
   const int* token_of;         // of each y: its row of the output
-  float* kept;                 // fp32 sums, [splits][rows][kept_stride], or NULL
-  size_t kept_stride, kept_split;
-  int add, finish, splits;     // whether kept sums are added, whether the output is written
+  float* kept;                 // fp32 sums, [splits][rows with a label, to whole tiles][kept_stride]
+  size_t kept_stride;
+  int add, last;               // whether there are kept sums of pieces before this one, and whether this is the last one
+  int sharers, most_splits;    // see splits_of
 };
+
+// How many workgroups share the steps of a tile: where the rows with a label make few tiles, as many as there are sharers for.
+template <class S>
+__device__ __forceinline__ int splits_of(int rows, int nx, int sharers, int most) {
+  const int tiles = nx * ((rows + S::BY - 1) / S::BY), splits = tiles ? sharers / tiles : 1;
+  return splits < 1 ? 1 : splits < most ? splits : most;
+}
 
 // The matrix's gradient: x along the columns, y the piece's rows, k the rows with a label.
 template <int DT, class S>
 __global__ void __launch_bounds__(S::kThreads) table_gradient_kernel(OutArgs a) {
   int tx, ty;
-  tile_of(a.nx, a.ny, tx, ty);
+  if (!tile_of(a.nx, a.ny, tx, ty)) return;
   f32x4 sum[S::NX][S::NY];
   const int there = a.head->rows;
-  product<DT, S, kAcross, kAcross>(a.mx, a.my, (size_t)tx * S::BX, (size_t)ty * S::BY, (there + kStep<DT> - 1) / kStep<DT>, sum);
+  using Both = Operands<DT, S, kAcross, kAcross>;
+  Both both(a.mx, a.my, (size_t)tx * S::BX, (size_t)ty * S::BY);
+  product(both, (Both*)nullptr, (there + kStep<DT> - 1) / kStep<DT>, sum);
   const float factor = a.scale * (a.head->most / kLift<DT>);
   const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, wx = wave % S::WX, wy = wave / S::WX;
   const int x0 = tx * S::BX + wx * (S::BX / S::WX) + lane / 16 * 4, y0 = ty * S::BY + wy * (S::BY / S::WY) + (lane & 15);
@@ -379,14 +460,14 @@ __global__ void __launch_bounds__(S::kThreads) table_gradient_kernel(OutArgs a) 
   }
 }
 
-// The hidden states' gradient: x along the columns, y the rows with a label, k the piece's rows, which `splits` workgroups share.
+// The hidden states' gradient: x along the columns, y the rows with a label, k the piece's rows, which several workgroups may share.
 template <int DT, class S>
 __global__ void __launch_bounds__(S::kThreads) hidden_gradient_kernel(OutArgs a) {
+  const int there = a.head->rows, splits = splits_of<S>(there, a.nx, a.sharers, a.most_splits), ny = (there + S::BY - 1) / S::BY;
   int tx, ty;
-  tile_of(a.nx, a.ny, tx, ty);
-  const int there = a.head->rows;
-  if (ty * S::BY >= there) return;
-  const int split = blockIdx.y, from = (int)((long long)a.steps * split / a.splits), to = (int)((long long)a.steps * (split + 1) / a.splits);
+  if (!tile_of(a.nx, ny * splits, tx, ty)) return;
+  const int split = ty / ny, from = (int)((long long)a.steps * split / splits), to = (int)((long long)a.steps * (split + 1) / splits);
+  ty -= split * ny;
   Matrix mx = a.mx, my = a.my;
   const size_t skip = (size_t)from * kStep<DT> * mx.stride;
   mx.at += skip < mx.bytes ? skip : mx.bytes;
@@ -394,8 +475,11 @@ __global__ void __launch_bounds__(S::kThreads) hidden_gradient_kernel(OutArgs a)
   my.at += (size_t)from * kStepBytes;
   my.bytes -= (size_t)from * kStepBytes;
   f32x4 sum[S::NX][S::NY];
-  product<DT, S, kAcross, kAlong>(mx, my, (size_t)tx * S::BX, (size_t)ty * S::BY, to - from, sum);
+  using Both = Operands<DT, S, kAcross, kAlong>;
+  Both both(mx, my, (size_t)tx * S::BX, (size_t)ty * S::BY);
+  product(both, (Both*)nullptr, to - from, sum);
   const float factor = a.scale * (a.head->most / kLift<DT>);
+  const bool finish = a.last && splits == 1;
   const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, wx = wave % S::WX, wy = wave / S::WX;
   const int x0 = tx * S::BX + wx * (S::BX / S::WX) + lane / 16 * 4, y0 = ty * S::BY + wy * (S::BY / S::WY) + (lane & 15);
 #pragma unroll
@@ -403,15 +487,15 @@ __global__ void __launch_bounds__(S::kThreads) hidden_gradient_kernel(OutArgs a)
     rest_of_sums<S>(sum, j);
     const int y = y0 + 16 * j;
     if (y >= there) continue;
-    char* const row = a.finish ? a.out + (size_t)a.token_of[y] * a.out_stride : nullptr;
-    float* const kept = a.kept + split * a.kept_split + (size_t)y * a.kept_stride;
+    char* const row = finish ? a.out + (size_t)a.token_of[y] * a.out_stride : nullptr;
+    float* const kept = a.kept + ((size_t)split * ny * S::BY + y) * a.kept_stride;
 #pragma unroll
     for (int i = 0; i < S::NX; ++i) {
       const int x = x0 + 16 * i;
       if (x >= a.cols) continue;   // (kept rows are a multiple of 4 wide)
       f32x4 s = sum[i][j];
       if (a.add) s += *reinterpret_cast<const f32x4*>(kept + x);
-      if (!a.finish) {
+      if (!finish) {
         *reinterpret_cast<f32x4*>(kept + x) = s;
         continue;
       }
@@ -425,21 +509,32 @@ __global__ void __launch_bounds__(S::kThreads) hidden_gradient_kernel(OutArgs a)
   }
 }
 
-// The sums that `splits` workgroups have kept of each place, one after the other.
-template <int DT>
+// The sums that several workgroups have kept of each place, one after the other.
+template <int DT, class S>
 __global__ void __launch_bounds__(kThreads) hidden_finish_kernel(OutArgs a) {
-  const int y = blockIdx.y * 65535 + blockIdx.z, x = (blockIdx.x * kThreads + threadIdx.x) * 4;
-  if (y >= a.head->rows || x >= a.cols) return;
-  const float* kept = a.kept + (size_t)y * a.kept_stride + x;
-  f32x4 s = *reinterpret_cast<const f32x4*>(kept);
-  for (int i = 1; i < a.splits; ++i) s += *reinterpret_cast<const f32x4*>(kept + i * a.kept_split);
+  const int there = a.head->rows, splits = splits_of<S>(there, a.nx, a.sharers, a.most_splits), x = (blockIdx.x * kThreads + threadIdx.x) * 4;
+  if (splits == 1 || x >= a.cols) return;
+  const size_t split = (size_t)((there + S::BY - 1) / S::BY) * S::BY * a.kept_stride;
   const float factor = a.scale * (a.head->most / kLift<DT>);
-  float v[4];
+  for (int y = blockIdx.y; y < there; y += gridDim.y) {
+    const float* kept = a.kept + (size_t)y * a.kept_stride + x;
+    f32x4 s = *reinterpret_cast<const f32x4*>(kept);
+    constexpr int kAhead = 4;
+    for (int i = 1; i < splits; i += kAhead) {
+      f32x4 more[kAhead];
 #pragma unroll
-  for (int r = 0; r < 4; ++r) v[r] = factor * s[r];
-  Raw<DT, 4> raw;
-  raw.pack(v);
-  raw.store(a.out + (size_t)a.token_of[y] * a.out_stride, x * kBytes<DT>, a.cols - x);
+      for (int u = 0; u < kAhead; ++u) more[u] = *reinterpret_cast<const f32x4*>(kept + (i + u < splits ? i + u : i) * split);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (i + u < splits) s += more[u];
+    }
+    float v[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = factor * s[r];
+    Raw<DT, 4> raw;
+    raw.pack(v);
+    raw.store(a.out + (size_t)a.token_of[y] * a.out_stride, x * kBytes<DT>, a.cols - x);
+  }
 }
 
 // ---- host: how a call is laid out ----------------------------------------------------------
@@ -447,7 +542,8 @@ __global__ void __launch_bounds__(kThreads) hidden_finish_kernel(OutArgs a) {
 using Large = Shape<256, 256, 2, 2, 2, true>;
 using Medium = Shape<128, 128, 2, 2, 2>;
 using Small = Shape<64, 64, 2, 2, 4>;
-enum { kLarge, kMedium, kSmall };
+using Thin = Shape<32, 64, 2, 2, 4>;   // logits of few tokens: what counts is how many compute units read the table
+enum { kLarge, kMedium, kSmall, kThin };
 constexpr int kComputeUnits = 256;
 constexpr size_t kMostTiles = (size_t)1 << 22;   // of one launch
 
@@ -466,6 +562,11 @@ int shape_for(int dtype, size_t nx, size_t ny) {
     else if ((SHAPE) == kSmall) LAUNCH(DT, Small);  \
     else if constexpr (DT != kF32) LAUNCH(DT, Large); \
   } while (0)
+#define ZE_BY_SHAPE_OF_LOGITS(SHAPE, DT, LAUNCH)    \
+  do {                                              \
+    if ((SHAPE) == kThin) LAUNCH(DT, Thin);         \
+    else ZE_BY_SHAPE(SHAPE, DT, LAUNCH);            \
+  } while (0)
 #define ZE_BY_TYPE(TYPE, CALL)             \
   do {                                     \
     if ((TYPE) == ZC_F32) CALL(kF32);      \
@@ -477,20 +578,21 @@ int shape_for(int dtype, size_t nx, size_t ny) {
 struct Plan {
   size_t e, padded;                  // bytes of a value; tokens, to whole tiles
   size_t cols_padded;                // to whole steps
+  int steps;                         // whole ones
+  bool ends;                         // whether rows have an end behind them
   size_t stride_hidden, stride_table;   // bytes
   bool pack_hidden, pack_table;
   size_t piece;                      // rows of the table at a time
   int shape;                         // of the logits
   size_t parts;                      // forward: of a row
-  int hidden_shape, splits;          // backward
-  bool keep;                         // backward: sums of the hidden states' gradient are kept from piece to piece
-  size_t list[7], packed_hidden, packed_table, part, g, kept, bytes;
+  int hidden_shape, sharers, most_splits;   // backward
+  size_t list[7], packed_hidden, packed_table, table_ends, hidden_ends, part, g, kept, bytes;
 };
 
 constexpr size_t kMostPacked = (size_t)64 << 20;   // bytes of the table that are copied at a time
 
-bool readable(const void* p, size_t stride_bytes, size_t cols, size_t e) {
-  return aligned(p, 16) && stride_bytes % 16 == 0 && cols * e % kStepBytes == 0;
+bool readable(const void* p, size_t stride_bytes) {
+  return aligned(p, 4) && stride_bytes % 4 == 0;
 }
 
 // Whether the operands are copied to where a product can read them decides what the workspace holds.
@@ -522,24 +624,37 @@ Plan plan_with(const struct ze_form& f, bool backward, size_t piece, bool pack_h
     if (even < p.piece) p.piece = even;
   }
   p.shape = shape_for(f.dtype, p.piece, f.tokens);
+  if (!backward && p.shape == kSmall && f.tokens <= Thin::BY) p.shape = kThin;
+  // (The ends are added first also where a copy has them behind the rest: the sums do not depend on where the tensors lie.)
+  p.steps = (int)(f.cols * p.e / kStepBytes);
+  p.ends = f.cols * p.e % kStepBytes != 0;
   Places places;
   places.take(kHeadBytes);
   for (int i = 0; i < 7; ++i) p.list[i] = places.take(p.padded * 4);
   p.packed_hidden = places.take(backward || pack_hidden ? p.padded * p.cols_padded * p.e : 0);
   p.packed_table = places.take(pack_table ? p.piece * p.cols_padded * p.e : 0);
+  p.table_ends = places.take(p.ends && !pack_table ? p.piece * kStepBytes : 0);
+  p.hidden_ends = places.take(p.ends && !backward && !pack_hidden ? p.padded * kStepBytes : 0);
   if (!backward) {
-    const size_t part = p.shape == kLarge ? Large::BX / Large::WX : p.shape == kMedium ? Medium::BX / Medium::WX : Small::BX / Small::WX;
+    const size_t part = p.shape == kLarge    ? Large::BX / Large::WX
+                        : p.shape == kMedium ? Medium::BX / Medium::WX
+                        : p.shape == kSmall  ? Small::BX / Small::WX
+                                             : Thin::BX / Thin::WX;
     p.parts = p.piece ? parts(f.rows, p.piece) * parts(up(p.piece, 256), part) : 0;
     p.part = places.take(f.tokens * p.parts * sizeof(Part));
   } else {
     const size_t padded = up(p.piece, kStepBytes / p.e);
     p.g = places.take(p.padded * padded * p.e);
     p.hidden_shape = shape_for(f.dtype, f.cols, f.tokens);
-    const size_t n = tiles(p.hidden_shape, f.cols, f.tokens), steps = padded * p.e / kStepBytes, most = steps / 16;
-    const size_t wanted = n ? 2 * kComputeUnits / n : 1;
-    p.splits = (int)(wanted < 1 || p.hidden_shape == kLarge ? 1 : wanted < most ? wanted : most ? most : 1);
-    p.keep = p.piece < f.rows || p.splits > 1;
-    if (p.keep) p.kept = places.take((size_t)p.splits * p.padded * up(f.cols, 4) * 4);
+    const size_t by = p.hidden_shape == kLarge ? Large::BY : p.hidden_shape == kMedium ? Medium::BY : Small::BY;
+    const size_t steps = padded * p.e / kStepBytes;
+    p.sharers = p.hidden_shape == kLarge ? kComputeUnits : 2 * kComputeUnits;   // as many as run at once
+    p.most_splits = (int)(steps < 16 ? 1 : steps / 8);
+    if (p.piece < f.rows || p.most_splits > 1) {
+      // splits x rows is greatest where all sharers have a tile, or all rows one
+      const size_t rows = parts(f.tokens, by) * by, shared = parts((size_t)p.sharers, parts(f.cols, by)) * by;
+      p.kept = places.take((rows > shared ? rows : shared) * up(f.cols, 4) * 4);
+    }
   }
   p.bytes = places.at;
   return p;
@@ -549,8 +664,8 @@ Plan plan_with(const struct ze_form& f, bool backward, size_t piece, bool pack_h
 Plan plan_for(const struct ze_form& f, bool backward, size_t piece, const void* d_hidden, const void* d_table) {
   const size_t e = dtype_bytes(f.dtype), stride = stride_of(f.stride_tokens, f.cols) * e;
   // a list of rows tells places apart by 32 bits
-  const bool pack_hidden = !d_hidden || !readable(d_hidden, stride, f.cols, e) || f.tokens * stride > 0xF0000000u;
-  return plan_with(f, backward, piece, pack_hidden, !d_table || !readable(d_table, stride_of(f.stride_table, f.cols) * e, f.cols, e));
+  const bool pack_hidden = !d_hidden || !readable(d_hidden, stride) || f.tokens * stride > 0xF0000000u;
+  return plan_with(f, backward, piece, pack_hidden, !d_table || !readable(d_table, stride_of(f.stride_table, f.cols) * e));
 }
 size_t work_bytes_for(const struct ze_form& f, bool backward, size_t piece, const void* d_hidden, const void* d_table) {
   const size_t bytes = plan_for(f, backward, piece, d_hidden, d_table).bytes;
@@ -594,7 +709,7 @@ Matrix table_piece(const struct ze_form& f, const Plan& p, const void* d_table, 
   if (!p.pack_table) {
     m.at = at;
     m.stride = p.stride_table;
-    m.bytes = (count - 1) * m.stride + f.cols * p.e;
+    m.bytes = up((count - 1) * m.stride + f.cols * p.e, 4);   // (a word that holds a value may be read)
     return m;
   }
   PackArgs a = {at, p.stride_table, nullptr, count, work + p.packed_table, p.cols_padded * p.e, (int)f.cols};
@@ -608,6 +723,23 @@ Matrix table_piece(const struct ze_form& f, const Plan& p, const void* d_table, 
   return m;
 }
 
+// The ends of `rows` rows, where they are apart.
+template <int DT>
+Ends ends_of(const Plan& p, const char* at, size_t stride, const int* token_of, size_t rows, size_t cols, char* out, hipStream_t s) {
+  if (!p.ends) return Ends{nullptr, 0, 0};
+  const size_t skip = (size_t)p.steps * kStep<DT>;
+  PackArgs a = {at + skip * kBytes<DT>, stride, token_of, rows, out, kStepBytes, (int)(cols - skip)};
+  hipLaunchKernelGGL(pack_ends_kernel<DT>, dim3((unsigned)parts(rows * 8, kThreads)), dim3(kThreads), 0, s, a, rows);
+  return Ends{out, rows * kStepBytes, kStepBytes};
+}
+
+// Those of rows that have been copied, ends and all.
+Ends ends_in(const Plan& p, const Matrix& m) {
+  if (!p.ends) return Ends{nullptr, 0, 0};
+  const size_t skip = (size_t)p.steps * kStepBytes;
+  return Ends{m.at + skip, m.bytes - skip, m.stride};
+}
+
 template <int DT>
 void forward(const struct ze_form& f, const Plan& p, const void* d_hidden, const void* d_table, const List& list, char* work, float* d_stats, hipStream_t s) {
   LogitsArgs a;
@@ -616,7 +748,7 @@ void forward(const struct ze_form& f, const Plan& p, const void* d_hidden, const
   a.scale = f.scale;
   a.target = list.target;
   a.parts_stride = p.parts;
-  a.steps = (int)(p.cols_padded * p.e / kStepBytes);
+  a.steps = p.steps;
   if (p.piece) {
     if (p.pack_hidden) {
       PackArgs pack = {static_cast<const char*>(d_hidden), p.stride_hidden, list.token_of, 0, work + p.packed_hidden, p.cols_padded * p.e, (int)f.cols};
@@ -625,14 +757,17 @@ void forward(const struct ze_form& f, const Plan& p, const void* d_hidden, const
         hipLaunchKernelGGL(pack_kernel<DT>, dim3((unsigned)groups), dim3(kThreads), 0, s, pack, from);
       }
       a.hidden = Matrix{pack.out, p.padded * pack.out_stride, pack.out_stride, nullptr};
+      a.hidden_ends = ends_in(p, a.hidden);
     } else {
-      a.hidden = Matrix{static_cast<const char*>(d_hidden), (f.tokens - 1) * p.stride_hidden + f.cols * p.e, p.stride_hidden, list.token_of};
+      a.hidden = Matrix{static_cast<const char*>(d_hidden), up((f.tokens - 1) * p.stride_hidden + f.cols * p.e, 4), p.stride_hidden, list.token_of};
+      a.hidden_ends = ends_of<DT>(p, static_cast<const char*>(d_hidden), p.stride_hidden, list.token_of, p.padded, f.cols, work + p.hidden_ends, s);
     }
   }
   size_t part = 0;
   for (size_t v0 = 0; v0 < f.rows; v0 += p.piece) {
     const size_t count = f.rows - v0 < p.piece ? f.rows - v0 : p.piece;
     a.table = table_piece<DT>(f, p, d_table, v0, count, work, s);
+    a.table_ends = p.pack_table ? ends_in(p, a.table) : ends_of<DT>(p, a.table.at, a.table.stride, nullptr, count, f.cols, work + p.table_ends, s);
     a.v0 = (int)v0;
     a.rows = (int)count;
     a.parts = reinterpret_cast<Part*>(work + p.part) + part;
@@ -643,7 +778,7 @@ void forward(const struct ze_form& f, const Plan& p, const void* d_hidden, const
     part += (size_t)a.nx * S::WX;                                                                                                     \
     hipLaunchKernelGGL((logits_kernel<D, S>), dim3((unsigned)(a.nx * a.ny)), dim3(S::kThreads), 0, s, a);                             \
   } while (0)
-    ZE_BY_SHAPE(p.shape, DT, LAUNCH);
+    ZE_BY_SHAPE_OF_LOGITS(p.shape, DT, LAUNCH);
 #undef LAUNCH
   }
   const size_t groups = parts(f.tokens, kThreads / 64);
@@ -669,16 +804,19 @@ void backward(const struct ze_form& f, const Plan& p, const void* d_hidden, cons
     GradientArgs g;
     g.table = table;
     g.hidden = hidden;
+    g.table_ends = p.pack_table ? ends_in(p, table) : ends_of<DT>(p, table.at, table.stride, nullptr, count, f.cols, work + p.table_ends, s);
+    g.hidden_ends = ends_in(p, hidden);
     g.head = list.head;
     g.label_of = list.label_of;
     g.lse = list.lse;
     g.dloss = list.dloss;
-    g.steps = (int)(p.cols_padded * p.e / kStepBytes);
+    g.steps = p.steps;
     g.v0 = (int)v0;
     g.rows = (int)count;
     g.rows_padded = (int)padded;
     g.scale = f.scale;
     g.g = work + p.g;
+    g.g_stride = padded * p.e;
 #define LAUNCH(D, S)                                                                                           \
   do {                                                                                                         \
     g.nx = (int)parts(count, S::BX);                                                                           \
@@ -714,23 +852,23 @@ void backward(const struct ze_form& f, const Plan& p, const void* d_hidden, cons
       a.out = static_cast<char*>(d_dhidden);
       a.out_stride = dhidden_stride;
       a.token_of = list.token_of;
-      a.kept = p.keep ? reinterpret_cast<float*>(work + p.kept) : nullptr;
+      a.kept = reinterpret_cast<float*>(work + p.kept);
       a.kept_stride = up(f.cols, 4);
-      a.kept_split = p.padded * a.kept_stride;
-      a.splits = p.splits;
+      a.sharers = p.sharers;
+      a.most_splits = p.most_splits;
       a.add = v0 > 0;
-      a.finish = p.splits == 1 && v0 + count == f.rows;
-#define LAUNCH(D, S)                                                                                                                             \
-  do {                                                                                                                                           \
-    a.nx = (int)parts(f.cols, S::BX);                                                                                                            \
-    a.ny = (int)parts(f.tokens, S::BY);                                                                                                          \
-    hipLaunchKernelGGL((hidden_gradient_kernel<D, S>), dim3((unsigned)(a.nx * a.ny), (unsigned)a.splits), dim3(S::kThreads), 0, s, a);           \
+      a.last = v0 + count == f.rows;
+#define LAUNCH(D, S)                                                                                                                       \
+  do {                                                                                                                                     \
+    a.nx = (int)parts(f.cols, S::BX);                                                                                                      \
+    const size_t all = a.nx * parts(f.tokens, S::BY), groups = p.most_splits > 1 && all < (size_t)p.sharers ? (size_t)p.sharers : all;     \
+    hipLaunchKernelGGL((hidden_gradient_kernel<D, S>), dim3((unsigned)groups), dim3(S::kThreads), 0, s, a);                                \
+    if (a.last && p.most_splits > 1)                                                                                                       \
+      hipLaunchKernelGGL((hidden_finish_kernel<D, S>), dim3((unsigned)parts(f.cols, kThreads * 4), (unsigned)(f.tokens < 2048 ? f.tokens : 2048)), \
+                         dim3(kThreads), 0, s, a);                                                                                         \
   } while (0)
       ZE_BY_SHAPE(p.hidden_shape, DT, LAUNCH);
 #undef LAUNCH
-      if (!a.finish && v0 + count == f.rows)
-        hipLaunchKernelGGL(hidden_finish_kernel<DT>, dim3((unsigned)parts(f.cols, kThreads * 4), (unsigned)parts(f.tokens, 65535), (unsigned)(f.tokens < 65535 ? f.tokens : 65535)),
-                           dim3(kThreads), 0, s, a);
     }
   }
 }

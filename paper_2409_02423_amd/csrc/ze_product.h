@@ -42,11 +42,17 @@ __device__ __forceinline__ f32x4 multiply(i32x4 x, i32x4 y, f32x4 sum) {
   }
 }
 
-// An operand in memory: every row starts at a multiple of 16 bytes.  Nothing is read at or behind `bytes`: what would be is zero.
+// An operand in memory: every row starts at a multiple of 4 bytes.  Nothing is read at or behind `bytes`, a multiple of 4: what would be is zero.
 struct Matrix {
   const char* at;
   size_t bytes, stride;   // stride in bytes
   const int* places;      // kAlong: NULL, or the row that stands for each row (the matrix then has less than 2^32 bytes)
+};
+
+// A row's end behind its last whole step: one step more, which ends in zeros, of rows of its own (kAlong).  at = NULL where there is none.
+struct Ends {
+  const char* at;
+  size_t bytes, stride;
 };
 
 constexpr uint32_t kNowhere = 0xFFFFFF00u;   // behind the end of every buffer
@@ -62,7 +68,7 @@ struct Operand {
   static_assert(kLoads * THREADS * 16 == kTileBytes, "whole loads");
   static constexpr int kParts = SIZE / 16 < 8 ? SIZE / 16 : 8;   // kAcross, half precision: 16 values of a row, places that are exchanged
   static constexpr int kAddresses = LIES == kAlong ? 2 : DT == kF32 ? 4 : kParts;
-  static_assert(DT != kF32 || SIZE >= 64, "exchanged places");
+  static_assert(LIES == kAlong || DT != kF32 || SIZE >= 64, "exchanged places");
 
   uint32_t from[kLoads];   // bytes from the tile's start
   const char* at;          // the tile's start, at the present step
@@ -179,13 +185,15 @@ __device__ __forceinline__ void meet() {
   asm volatile("" ::: "memory");
 }
 
-template <int DT, class S, Lies LX, Lies LY>
+template <int DT_, class S_, Lies LX, Lies LY>
 struct Operands {
+  static constexpr int DT = DT_;
+  using S = S_;
   Operand<DT, LX, S::BX, S::kThreads> x;
   Operand<DT, LY, S::BY, S::kThreads> y;
-  static constexpr int kLoads = decltype(x)::kLoads + decltype(y)::kLoads, kTile = (S::BX + S::BY) * kStepBytes, kY = S::BX * kStepBytes;
+  static constexpr int kLoadsX = decltype(x)::kLoads, kLoads = kLoadsX + decltype(y)::kLoads, kTile = (S::BX + S::BY) * kStepBytes, kY = S::BX * kStepBytes;
 
-  __device__ __forceinline__ void start(const Matrix& mx, const Matrix& my, size_t first_x, size_t first_y) {
+  __device__ __forceinline__ Operands(const Matrix& mx, const Matrix& my, size_t first_x, size_t first_y) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     x.start(mx, first_x, wave % S::WX * (S::BX / S::WX));
     y.start(my, first_y, wave / S::WX * (S::BY / S::WY));
@@ -207,7 +215,7 @@ __device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>)
 }
 
 // sum = x y + sum, in accumulation registers.  (As an instruction by name: left to itself the compiler moves half of 256 sums to and from other
-// registers in every step.  It knows nothing of the time that it takes, see product_of_four.)
+// registers in every step.  It knows nothing of the time that it takes, see the end of product_of_four.)
 template <int DT>
 __device__ __forceinline__ void multiply_in_place(i32x4 x, i32x4 y, f32x4& sum) {
   if constexpr (DT == kBF16) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(sum) : "v"(x), "v"(y));
@@ -219,15 +227,13 @@ __device__ __forceinline__ void multiply_in_place(i32x4 x, i32x4 y, f32x4& sum) 
 // 128 products, two follow each read of the next half step, and five each load.  At kMeet, all of the step has been read; its place takes the loads of the step
 // after the next from there on, spread so that the cache answers them about as fast as they are asked for (all at once behind the meeting, a
 // load took 516 cycles on average; a bf16 product of 8192 x 8192 x 8192 830 us, so 748 to 764).
-template <int DT, class S, Lies LX, Lies LY>
-__device__ __forceinline__ void product_of_four(const Matrix& mx, const Matrix& my, size_t first_x, size_t first_y, int steps, f32x4 (&sum)[S::NX][S::NY]) {
-  using Both = Operands<DT, S, LX, LY>;
+template <class Both, class S = typename Both::S>
+__device__ __forceinline__ void product_of_four(Both& both, Both* ends, int steps, f32x4 (&sum)[S::NX][S::NY]) {
+  constexpr int DT = Both::DT;
   __shared__ __attribute__((aligned(1024))) char stage0[Both::kTile], stage1[Both::kTile];
   ZE_LDS char* const stages[2] = {(ZE_LDS char*)stage0, (ZE_LDS char*)stage1};
-  constexpr int NX = S::NX, NY = S::NY, kReads = NX + NY, kHalf = NX * NY, kMeet = 40, kSpread = 5, kReadEvery = 2;
+  constexpr int NX = S::NX, NY = S::NY, kReads = NX + NY, kHalf = NX * NY, kReadEvery = 2, kMeet = kReads * kReadEvery + NX, kSpread = (2 * kHalf - kMeet) / Both::kLoads;
   static_assert(S::kStages == 2 && kReads * kReadEvery <= kMeet && kMeet + (Both::kLoads - 1) * kSpread < 2 * kHalf && kReads * kReadEvery <= kHalf, "order");
-  Both both;
-  both.start(mx, my, first_x, first_y);
 #pragma unroll
   for (int i = 0; i < NX; ++i)
 #pragma unroll
@@ -239,6 +245,17 @@ __device__ __forceinline__ void product_of_four(const Matrix& mx, const Matrix& 
   };
   using First = std::integral_constant<int, 0>;
   using Second = std::integral_constant<int, 1>;
+  if (ends) {
+    ends->load(stages[0], true);
+    wait_for_loads<0>();
+    meet();
+    each_of([&](auto h) __attribute__((always_inline)) {
+      each_of([&](auto q) __attribute__((always_inline)) { read(q, stages[0], h); }, std::make_integer_sequence<int, kReads>{});
+      each_of([&](auto m) __attribute__((always_inline)) { multiply_in_place<DT>(x[h][m % NX], y[h][m / NX], sum[m % NX][m / NX]); },
+              std::make_integer_sequence<int, kHalf>{});
+    }, std::make_integer_sequence<int, 2>{});
+    meet();
+  }
   both.load(stages[0], 0 < steps);
   both.load(stages[1], 1 < steps);
   wait_for_loads<Both::kLoads>();
@@ -259,8 +276,8 @@ __device__ __forceinline__ void product_of_four(const Matrix& mx, const Matrix& 
       if constexpr (h == 1 && m % kReadEvery == 1 && m / kReadEvery < kReads) read(std::integral_constant<int, m / kReadEvery>{}, there, First{});
       if constexpr (p >= kMeet && (p - kMeet) % kSpread == 0 && (p - kMeet) / kSpread < Both::kLoads) {
         constexpr int q = (p - kMeet) / kSpread;
-        if constexpr (q < both.x.kLoads) both.x.load_one(from_x, q);
-        else both.y.load_one(from_y, q - both.x.kLoads);
+        if constexpr (q < Both::kLoadsX) both.x.load_one(from_x, q);
+        else both.y.load_one(from_y, q - Both::kLoadsX);
       }
       in_order();
       multiply_in_place<DT>(x[h][m % NX], y[h][m / NX], sum[m % NX][m / NX]);
@@ -276,20 +293,18 @@ __device__ __forceinline__ void product_of_four(const Matrix& mx, const Matrix& 
   wait_for_loads<0>();
 }
 
-// The tile's sums: sum[i][j][r] is that of x = the wavefront's first + 16 i + 4 (lane / 16) + r, y = the wavefront's first + 16 j + lane % 16.
-template <int DT, class S, Lies LX, Lies LY>
-__device__ __forceinline__ void product(const Matrix& mx, const Matrix& my, size_t first_x, size_t first_y, int steps, f32x4 (&sum)[S::NX][S::NY]) {
+// The tile's sums: sum[i][j][r] is that of x = the wavefront's first + 16 i + 4 (lane / 16) + r, y = the wavefront's first + 16 j + lane % 16.  `ends`: NULL, or the operands
+// of a step that is added first (a row's end).
+template <class Both, class S = typename Both::S>
+__device__ __forceinline__ void product(Both& both, Both* ends, int steps, f32x4 (&sum)[S::NX][S::NY]) {
   if constexpr (S::kByHand) {
-    product_of_four<DT, S, LX, LY>(mx, my, first_x, first_y, steps, sum);
+    product_of_four(both, ends, steps, sum);
   } else {
-    using Both = Operands<DT, S, LX, LY>;
-    constexpr int kTile = Both::kTile, kMore = S::kStages > 2 ? kTile : 16;
+    constexpr int DT = Both::DT, kTile = Both::kTile, kMore = S::kStages > 2 ? kTile : 16;
     // An array for each stage: what is loaded into one is seen to leave the others alone.
     __shared__ __attribute__((aligned(1024))) char stage0[kTile], stage1[kTile], stage2[kMore], stage3[kMore];
     ZE_LDS char* const stages[4] = {(ZE_LDS char*)stage0, (ZE_LDS char*)stage1, (ZE_LDS char*)stage2, (ZE_LDS char*)stage3};
     static_assert(S::kStages == 2 || S::kStages == 4, "arrays");
-    Both both;
-    both.start(mx, my, first_x, first_y);
 #pragma unroll
     for (int i = 0; i < S::NX; ++i)
 #pragma unroll
@@ -308,6 +323,18 @@ __device__ __forceinline__ void product(const Matrix& mx, const Matrix& my, size
         for (int i = 0; i < S::NX; ++i) sum[i][j] = multiply<DT>(x[h][i], y[h][j], sum[i][j]);
     };
 
+    if (ends) {
+      ends->load(stages[0], true);
+      wait_for_loads<0>();
+      meet();
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        read(stages[0], h);
+        add(h);
+      }
+      wait_for_loads<0>();
+      meet();
+    }
 #pragma unroll
     for (int s = 0; s < S::kStages; ++s) both.load(stages[s], s < steps);
     wait_for_loads<(S::kStages - 1) * Both::kLoads>();
@@ -348,15 +375,17 @@ __device__ __forceinline__ void rest_of_sums(f32x4 (&sum)[S::NX][S::NY], int j) 
   }
 }
 
-// Which tile a workgroup has, of nx x ny: neighbours in a band of eight rows of tiles follow one another in an XCD (workgroups go to the
+// Which tile a workgroup has, of nx x ny, or none: neighbours in a band of eight rows of tiles follow one another in an XCD (workgroups go to the
 // eight of them in turn), so that what they share is read into its cache once.
-__device__ __forceinline__ void tile_of(int nx, int ny, int& x, int& y) {
-  const int total = nx * ny, each = total / 8, more = total % 8, xcd = blockIdx.x & 7;
-  const int at = xcd * each + (xcd < more ? xcd : more) + (blockIdx.x >> 3);
+__device__ __forceinline__ bool tile_of(int nx, int ny, int& x, int& y) {
+  const int total = nx * ny, each = total / 8, more = total % 8, xcd = blockIdx.x & 7, n = blockIdx.x >> 3;
+  if (n >= each + (xcd < more)) return false;
+  const int at = xcd * each + (xcd < more ? xcd : more) + n;
   constexpr int kBand = 8;
   const int band = at / (kBand * nx), in = at - band * (kBand * nx), rows = ny - band * kBand < kBand ? ny - band * kBand : kBand;
   y = band * kBand + in % rows;
   x = in / rows;
+  return true;
 }
 
 }  // namespace
