@@ -542,7 +542,7 @@ __global__ void __launch_bounds__(kThreads) hidden_finish_kernel(OutArgs a) {
 using Large = Shape<256, 256, 2, 2, 2, true>;
 using Medium = Shape<128, 128, 2, 2, 2>;
 using Small = Shape<64, 64, 2, 2, 4>;
-using Thin = Shape<32, 64, 2, 2, 4>;   // logits of few tokens: what counts is how many compute units read the table
+using Thin = Shape<32, 16, 2, 1, 8>;   // logits of few tokens: what counts is how many compute units read the table
 enum { kLarge, kMedium, kSmall, kThin };
 constexpr int kComputeUnits = 256;
 constexpr size_t kMostTiles = (size_t)1 << 22;   // of one launch

@@ -300,11 +300,12 @@ __device__ __forceinline__ void product(Both& both, Both* ends, int steps, f32x4
   if constexpr (S::kByHand) {
     product_of_four(both, ends, steps, sum);
   } else {
-    constexpr int DT = Both::DT, kTile = Both::kTile, kMore = S::kStages > 2 ? kTile : 16;
+    constexpr int DT = Both::DT, kTile = Both::kTile, kMore = S::kStages > 2 ? kTile : 16, kMost = S::kStages > 4 ? kTile : 16;
     // An array for each stage: what is loaded into one is seen to leave the others alone.
-    __shared__ __attribute__((aligned(1024))) char stage0[kTile], stage1[kTile], stage2[kMore], stage3[kMore];
-    ZE_LDS char* const stages[4] = {(ZE_LDS char*)stage0, (ZE_LDS char*)stage1, (ZE_LDS char*)stage2, (ZE_LDS char*)stage3};
-    static_assert(S::kStages == 2 || S::kStages == 4, "arrays");
+    __shared__ __attribute__((aligned(1024))) char stage0[kTile], stage1[kTile], stage2[kMore], stage3[kMore], stage4[kMost], stage5[kMost], stage6[kMost], stage7[kMost];
+    ZE_LDS char* const stages[8] = {(ZE_LDS char*)stage0, (ZE_LDS char*)stage1, (ZE_LDS char*)stage2, (ZE_LDS char*)stage3,
+                                    (ZE_LDS char*)stage4, (ZE_LDS char*)stage5, (ZE_LDS char*)stage6, (ZE_LDS char*)stage7};
+    static_assert(S::kStages == 2 || S::kStages == 4 || S::kStages == 8, "arrays");
 #pragma unroll
     for (int i = 0; i < S::NX; ++i)
 #pragma unroll
