@@ -209,30 +209,24 @@ struct LogitsArgs {
   float* target;
 };
 
-// Products of hidden states and rows of the table, whose ends may be apart.
-template <int DT, class S, class ARGS>
-__device__ __forceinline__ void product_with_ends(const ARGS& a, int tx, int ty, f32x4 (&sum)[S::NX][S::NY]) {
+// The tiles of the products of hidden states and rows of the table, whose ends may be apart: of the rows that have a label, as many for each XCD, however many
+// tokens have none.
+template <int DT, class S, class ARGS, class Use>
+__device__ __forceinline__ void logits_of_tiles(const ARGS& a, int there, const Use& use) {
   using Both = Operands<DT, S, kAlong, kAlong>;
-  const size_t x = (size_t)tx * S::BX, y = (size_t)ty * S::BY;
-  Both both(a.table, a.hidden, x, y);
-  if (a.table_ends.at) {
-    Both ends(Matrix{a.table_ends.at, a.table_ends.bytes, a.table_ends.stride, nullptr}, Matrix{a.hidden_ends.at, a.hidden_ends.bytes, a.hidden_ends.stride, nullptr}, x, y);
-    product(both, &ends, a.steps, sum);
-  } else {
-    product(both, (Both*)nullptr, a.steps, sum);
-  }
+  products<Both>(
+      Tiles(a.nx, (there + S::BY - 1) / S::BY), a.steps, a.table_ends.at != nullptr, [&](Both& both, int tx, int ty) { both.start(a.table, a.hidden, tx, ty); },
+      [&](Both& both, int tx, int ty) {
+        both.start(Matrix{a.table_ends.at, a.table_ends.bytes, a.table_ends.stride, nullptr}, Matrix{a.hidden_ends.at, a.hidden_ends.bytes, a.hidden_ends.stride, nullptr},
+                   tx, ty);
+      },
+      use);
 }
 
 // The greatest logit and the sum of exponentials in each wavefront's part of a row.  In a tile that is all there is of them: 4 x 16 columns to
 // a lane group, so a row's maximum takes NX x 4 comparisons in a lane and two across lanes.
 template <int DT, class S>
-__global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a) {
-  // (tiles of rows that have a label: as many for each XCD, however many tokens have none)
-  const int there = a.head->rows;
-  int tx, ty;
-  if (!tile_of(a.nx, (there + S::BY - 1) / S::BY, tx, ty)) return;
-  f32x4 sum[S::NX][S::NY];
-  product_with_ends<DT, S>(a, tx, ty, sum);
+__device__ __forceinline__ void use_logits(const LogitsArgs& a, int there, f32x4 (&sum)[S::NX][S::NY], int tx, int ty) {
   const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, wx = wave % S::WX, wy = wave / S::WX;
   const int x_wave = __builtin_amdgcn_readfirstlane(tx * S::BX + wx * (S::BX / S::WX));
   const bool edge = x_wave + S::BX / S::WX > a.rows;
@@ -276,6 +270,11 @@ __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a) {
     total += __shfl_xor(total, 32);
     if (lane < 16) a.parts[y * a.parts_stride + tx * S::WX + wx] = Part{most, total};
   }
+}
+template <int DT, class S>
+__global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a) {
+  const int there = a.head->rows;
+  logits_of_tiles<DT, S>(a, there, [&](f32x4 (&sum)[S::NX][S::NY], int tx, int ty) { use_logits<DT, S>(a, there, sum, tx, ty); });
 }
 
 // Joins parts of a sum of exponentials: the sums are taken to the greater of the two logits.  (Where that is -inf there is nothing in either.)
@@ -362,14 +361,7 @@ struct GradientArgs {
 
 // g of a tile, zeros behind the piece's last row and behind the last row with a label, up to whole steps of the products that read it.
 template <int DT, class S>
-__global__ void __launch_bounds__(S::kThreads) gradient_kernel(GradientArgs a) {
-  // (tiles of rows that have a label: as many for each XCD, however many tokens have none)
-  const int there = a.head->rows;
-  int tx, ty;
-  if (!tile_of(a.nx, (there + S::BY - 1) / S::BY, tx, ty)) return;
-  f32x4 sum[S::NX][S::NY];
-  product_with_ends<DT, S>(a, tx, ty, sum);
-  const float most = a.head->most;
+__device__ __forceinline__ void use_gradient(const GradientArgs& a, int there, float most, f32x4 (&sum)[S::NX][S::NY], int tx, int ty) {
   const int padded = (there + kStep<DT> - 1) / kStep<DT> * kStep<DT>;
   const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, wx = wave % S::WX, wy = wave / S::WX;
   const int x_wave = __builtin_amdgcn_readfirstlane(tx * S::BX + wx * (S::BX / S::WX));
@@ -404,6 +396,12 @@ __global__ void __launch_bounds__(S::kThreads) gradient_kernel(GradientArgs a) {
     }
   }
 }
+template <int DT, class S>
+__global__ void __launch_bounds__(S::kThreads) gradient_kernel(GradientArgs a) {
+  const int there = a.head->rows;
+  const float most = a.head->most;
+  logits_of_tiles<DT, S>(a, there, [&](f32x4 (&sum)[S::NX][S::NY], int tx, int ty) { use_gradient<DT, S>(a, there, most, sum, tx, ty); });
+}
 
 // out[y][x] from a tile's sums.
 struct OutArgs {
@@ -430,15 +428,7 @@ __device__ __forceinline__ int splits_of(int rows, int nx, int sharers, int most
 
 // The matrix's gradient: x along the columns, y the piece's rows, k the rows with a label.
 template <int DT, class S>
-__global__ void __launch_bounds__(S::kThreads) table_gradient_kernel(OutArgs a) {
-  int tx, ty;
-  if (!tile_of(a.nx, a.ny, tx, ty)) return;
-  f32x4 sum[S::NX][S::NY];
-  const int there = a.head->rows;
-  using Both = Operands<DT, S, kAcross, kAcross>;
-  Both both(a.mx, a.my, (size_t)tx * S::BX, (size_t)ty * S::BY);
-  product(both, (Both*)nullptr, (there + kStep<DT> - 1) / kStep<DT>, sum);
-  const float factor = a.scale * (a.head->most / kLift<DT>);
+__device__ __forceinline__ void use_table_gradient(const OutArgs& a, float factor, f32x4 (&sum)[S::NX][S::NY], int tx, int ty) {
   const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, wx = wave % S::WX, wy = wave / S::WX;
   const int x0 = tx * S::BX + wx * (S::BX / S::WX) + lane / 16 * 4, y0 = ty * S::BY + wy * (S::BY / S::WY) + (lane & 15);
 #pragma unroll
@@ -459,27 +449,19 @@ __global__ void __launch_bounds__(S::kThreads) table_gradient_kernel(OutArgs a) 
     }
   }
 }
+template <int DT, class S>
+__global__ void __launch_bounds__(S::kThreads) table_gradient_kernel(OutArgs a) {
+  using Both = Operands<DT, S, kAcross, kAcross>;
+  const int there = a.head->rows;
+  const float factor = a.scale * (a.head->most / kLift<DT>);
+  const auto start = [&](Both& both, int tx, int ty) { both.start(a.mx, a.my, tx, ty); };
+  products<Both>(Tiles(a.nx, a.ny), (there + kStep<DT> - 1) / kStep<DT>, false, start, start,
+                 [&](f32x4 (&sum)[S::NX][S::NY], int tx, int ty) { use_table_gradient<DT, S>(a, factor, sum, tx, ty); });
+}
 
 // The hidden states' gradient: x along the columns, y the rows with a label, k the piece's rows, which several workgroups may share.
 template <int DT, class S>
-__global__ void __launch_bounds__(S::kThreads) hidden_gradient_kernel(OutArgs a) {
-  const int there = a.head->rows, splits = splits_of<S>(there, a.nx, a.sharers, a.most_splits), ny = (there + S::BY - 1) / S::BY;
-  int tx, ty;
-  if (!tile_of(a.nx, ny * splits, tx, ty)) return;
-  const int split = ty / ny, from = (int)((long long)a.steps * split / splits), to = (int)((long long)a.steps * (split + 1) / splits);
-  ty -= split * ny;
-  Matrix mx = a.mx, my = a.my;
-  const size_t skip = (size_t)from * kStep<DT> * mx.stride;
-  mx.at += skip < mx.bytes ? skip : mx.bytes;
-  mx.bytes -= skip < mx.bytes ? skip : mx.bytes;
-  my.at += (size_t)from * kStepBytes;
-  my.bytes -= (size_t)from * kStepBytes;
-  f32x4 sum[S::NX][S::NY];
-  using Both = Operands<DT, S, kAcross, kAlong>;
-  Both both(mx, my, (size_t)tx * S::BX, (size_t)ty * S::BY);
-  product(both, (Both*)nullptr, to - from, sum);
-  const float factor = a.scale * (a.head->most / kLift<DT>);
-  const bool finish = a.last && splits == 1;
+__device__ __forceinline__ void use_hidden_gradient(const OutArgs& a, int there, int ny, int split, bool finish, float factor, f32x4 (&sum)[S::NX][S::NY], int tx, int ty) {
   const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, wx = wave % S::WX, wy = wave / S::WX;
   const int x0 = tx * S::BX + wx * (S::BX / S::WX) + lane / 16 * 4, y0 = ty * S::BY + wy * (S::BY / S::WY) + (lane & 15);
 #pragma unroll
@@ -507,6 +489,30 @@ __global__ void __launch_bounds__(S::kThreads) hidden_gradient_kernel(OutArgs a)
       raw.store(row, x * kBytes<DT>, a.cols - x);
     }
   }
+}
+template <int DT, class S>
+__global__ void __launch_bounds__(S::kThreads) hidden_gradient_kernel(OutArgs a) {
+  using Both = Operands<DT, S, kAcross, kAlong>;
+  const int there = a.head->rows, splits = splits_of<S>(there, a.nx, a.sharers, a.most_splits), ny = (there + S::BY - 1) / S::BY;
+  const float factor = a.scale * (a.head->most / kLift<DT>);
+  const bool finish = a.last && splits == 1;
+  // the steps, shared out: where there are several parts of them a workgroup has one tile, and so one part
+  const Tiles tiles(a.nx, ny * splits);
+  if (tiles.count == 0) return;
+  int tx, ty;
+  tiles.at(0, tx, ty);
+  const int split = splits == 1 ? 0 : ty / ny;
+  const int from = (int)((long long)a.steps * split / splits), to = (int)((long long)a.steps * (split + 1) / splits);
+  Matrix mx = a.mx, my = a.my;
+  const size_t skip = (size_t)from * kStep<DT> * mx.stride;
+  mx.at += skip < mx.bytes ? skip : mx.bytes;
+  mx.bytes -= skip < mx.bytes ? skip : mx.bytes;
+  my.at += (size_t)from * kStepBytes;
+  my.bytes -= (size_t)from * kStepBytes;
+  const auto start = [&](Both& both, int tx, int ty) { both.start(mx, my, tx, ty - split * ny); };
+  products<Both>(tiles, to - from, false, start, start, [&](f32x4 (&sum)[S::NX][S::NY], int tx, int ty) {
+    use_hidden_gradient<DT, S>(a, there, ny, split, finish, factor, sum, tx, ty - split * ny);
+  });
 }
 
 // The sums that several workgroups have kept of each place, one after the other.
@@ -550,6 +556,11 @@ constexpr size_t kMostTiles = (size_t)1 << 22;   // of one launch
 size_t tiles(int shape, size_t nx, size_t ny) {
   const size_t b = shape == kLarge ? Large::BX : shape == kMedium ? Medium::BX : Small::BX;
   return parts(nx, b) * parts(ny, b);
+}
+// Workgroups of a launch: one for each tile, or, where a workgroup goes on from tile to tile, for each compute unit.
+template <class S>
+unsigned groups_for(size_t tiles) {
+  return (unsigned)(S::kByHand && tiles > kComputeUnits ? kComputeUnits : tiles);
 }
 int shape_for(int dtype, size_t nx, size_t ny) {
   if (dtype != ZC_F32 && tiles(kLarge, nx, ny) >= kComputeUnits * 3 / 4) return kLarge;
@@ -776,7 +787,7 @@ void forward(const struct ze_form& f, const Plan& p, const void* d_hidden, const
     a.nx = (int)parts(count, S::BX);                                                                                                  \
     a.ny = (int)parts(f.tokens, S::BY);                                                                                               \
     part += (size_t)a.nx * S::WX;                                                                                                     \
-    hipLaunchKernelGGL((logits_kernel<D, S>), dim3((unsigned)(a.nx * a.ny)), dim3(S::kThreads), 0, s, a);                             \
+    hipLaunchKernelGGL((logits_kernel<D, S>), dim3(groups_for<S>((size_t)a.nx * a.ny)), dim3(S::kThreads), 0, s, a);                             \
   } while (0)
     ZE_BY_SHAPE_OF_LOGITS(p.shape, DT, LAUNCH);
 #undef LAUNCH
@@ -821,7 +832,7 @@ void backward(const struct ze_form& f, const Plan& p, const void* d_hidden, cons
   do {                                                                                                         \
     g.nx = (int)parts(count, S::BX);                                                                           \
     g.ny = (int)parts(f.tokens, S::BY);                                                                        \
-    hipLaunchKernelGGL((gradient_kernel<D, S>), dim3((unsigned)(g.nx * g.ny)), dim3(S::kThreads), 0, s, g);    \
+    hipLaunchKernelGGL((gradient_kernel<D, S>), dim3(groups_for<S>((size_t)g.nx * g.ny)), dim3(S::kThreads), 0, s, g);    \
   } while (0)
     ZE_BY_SHAPE(p.shape, DT, LAUNCH);
 #undef LAUNCH
@@ -840,7 +851,7 @@ void backward(const struct ze_form& f, const Plan& p, const void* d_hidden, cons
   do {                                                                                                             \
     a.nx = (int)parts(f.cols, S::BX);                                                                              \
     a.ny = (int)parts(count, S::BY);                                                                               \
-    hipLaunchKernelGGL((table_gradient_kernel<D, S>), dim3((unsigned)(a.nx * a.ny)), dim3(S::kThreads), 0, s, a);  \
+    hipLaunchKernelGGL((table_gradient_kernel<D, S>), dim3(groups_for<S>((size_t)a.nx * a.ny)), dim3(S::kThreads), 0, s, a);  \
   } while (0)
       ZE_BY_SHAPE(shape_for(f.dtype, f.cols, count), DT, LAUNCH);
 #undef LAUNCH
@@ -862,7 +873,7 @@ void backward(const struct ze_form& f, const Plan& p, const void* d_hidden, cons
   do {                                                                                                                                     \
     a.nx = (int)parts(f.cols, S::BX);                                                                                                      \
     const size_t all = a.nx * parts(f.tokens, S::BY), groups = p.most_splits > 1 && all < (size_t)p.sharers ? (size_t)p.sharers : all;     \
-    hipLaunchKernelGGL((hidden_gradient_kernel<D, S>), dim3((unsigned)groups), dim3(S::kThreads), 0, s, a);                                \
+    hipLaunchKernelGGL((hidden_gradient_kernel<D, S>), dim3(groups_for<S>(groups)), dim3(S::kThreads), 0, s, a);                                \
     if (a.last && p.most_splits > 1)                                                                                                       \
       hipLaunchKernelGGL((hidden_finish_kernel<D, S>), dim3((unsigned)parts(f.cols, kThreads * 4), (unsigned)(f.tokens < 2048 ? f.tokens : 2048)), \
                          dim3(kThreads), 0, s, a);                                                                                         \

@@ -193,10 +193,10 @@ struct Operands {
   Operand<DT, LY, S::BY, S::kThreads> y;
   static constexpr int kLoadsX = decltype(x)::kLoads, kLoads = kLoadsX + decltype(y)::kLoads, kTile = (S::BX + S::BY) * kStepBytes, kY = S::BX * kStepBytes;
 
-  __device__ __forceinline__ Operands(const Matrix& mx, const Matrix& my, size_t first_x, size_t first_y) {
+  __device__ __forceinline__ void start(const Matrix& mx, const Matrix& my, int tx, int ty) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    x.start(mx, first_x, wave % S::WX * (S::BX / S::WX));
-    y.start(my, first_y, wave / S::WX * (S::BY / S::WY));
+    x.start(mx, (size_t)tx * S::BX, wave % S::WX * (S::BX / S::WX));
+    y.start(my, (size_t)ty * S::BY, wave / S::WX * (S::BY / S::WY));
   }
   __device__ __forceinline__ void load(ZE_LDS char* tile, bool any) {
     x.load(tile, any);
@@ -215,29 +215,47 @@ __device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>)
 }
 
 // sum = x y + sum, in accumulation registers.  (As an instruction by name: left to itself the compiler moves half of 256 sums to and from other
-// registers in every step.  It knows nothing of the time that it takes, see the end of product_of_four.)
+// registers in every step.  It knows nothing of the time that it takes, see products_of_four.)
 template <int DT>
 __device__ __forceinline__ void multiply_in_place(i32x4 x, i32x4 y, f32x4& sum) {
   if constexpr (DT == kBF16) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(sum) : "v"(x), "v"(y));
   else asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(sum) : "v"(x), "v"(y));
 }
 
+// The tiles of a workgroup, of nx x ny: neighbours in a band of eight rows of tiles follow one another in an XCD (workgroups go to the
+// eight of them in turn), so that what they share is read into its cache once.
+struct Tiles {
+  int nx, ny, first, stride, count;
+  __device__ __forceinline__ Tiles(int nx, int ny) : nx(nx), ny(ny) {
+    const int total = nx * ny, each = total / 8, more = total % 8, xcd = blockIdx.x & 7, n = blockIdx.x >> 3;
+    const int mine = each + (xcd < more);                  // the XCD's
+    stride = ((int)gridDim.x - xcd + 7) >> 3;              // its workgroups
+    count = n < mine ? (mine - n + stride - 1) / stride : 0;
+    first = xcd * each + (xcd < more ? xcd : more) + n;
+  }
+  __device__ __forceinline__ void at(int k, int& x, int& y) const {
+    constexpr int kBand = 8;
+    const int at = first + k * stride, band = at / (kBand * nx), in = at - band * (kBand * nx), rows = ny - band * kBand < kBand ? ny - band * kBand : kBand;
+    y = band * kBand + in % rows;
+    x = in / rows;
+  }
+};
+
 // Four wavefronts with 128 x 128 sums each, one for each SIMD: a value that is read from LDS goes into eight products, which leaves a quarter of LDS's time
 // (eight wavefronts of 128 x 64 fill all of it).  Nothing but the order of instructions hides anything here, so it is written down: of a step's
 // 128 products, two follow each read of the next half step, and five each load.  At kMeet, all of the step has been read; its place takes the loads of the step
 // after the next from there on, spread so that the cache answers them about as fast as they are asked for (all at once behind the meeting, a
-// load took 516 cycles on average; a bf16 product of 8192 x 8192 x 8192 830 us, so 748 to 764).
-template <class Both, class S = typename Both::S>
-__device__ __forceinline__ void product_of_four(Both& both, Both* ends, int steps, f32x4 (&sum)[S::NX][S::NY]) {
+// load took 516 cycles on average; a bf16 product of 8192 x 8192 x 8192 830 us, so 748 to 764).  Behind a tile's last step come the next tile's first: they are
+// under way while `use` has the tile's sums.
+template <class Both, class Start, class StartEnds, class Use, class S = typename Both::S>
+__device__ __forceinline__ void products_of_four(const Tiles& tiles, int steps, bool has_ends, const Start& start, const StartEnds& start_ends, const Use& use) {
   constexpr int DT = Both::DT;
   __shared__ __attribute__((aligned(1024))) char stage0[Both::kTile], stage1[Both::kTile];
   ZE_LDS char* const stages[2] = {(ZE_LDS char*)stage0, (ZE_LDS char*)stage1};
   constexpr int NX = S::NX, NY = S::NY, kReads = NX + NY, kHalf = NX * NY, kReadEvery = 2, kMeet = kReads * kReadEvery + NX, kSpread = (2 * kHalf - kMeet) / Both::kLoads;
   static_assert(S::kStages == 2 && kReads * kReadEvery <= kMeet && kMeet + (Both::kLoads - 1) * kSpread < 2 * kHalf && kReads * kReadEvery <= kHalf, "order");
-#pragma unroll
-  for (int i = 0; i < NX; ++i)
-#pragma unroll
-    for (int j = 0; j < NY; ++j) sum[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  Both both;
+  f32x4 sum[NX][NY];
   i32x4 x[2][NX], y[2][NY];
   const auto read = [&](auto q, const ZE_LDS char* tile, auto h) __attribute__((always_inline)) {
     if constexpr (q < NX) x[h][q] = both.read_x(tile, q, h);
@@ -245,22 +263,9 @@ __device__ __forceinline__ void product_of_four(Both& both, Both* ends, int step
   };
   using First = std::integral_constant<int, 0>;
   using Second = std::integral_constant<int, 1>;
-  if (ends) {
-    ends->load(stages[0], true);
-    wait_for_loads<0>();
-    meet();
-    each_of([&](auto h) __attribute__((always_inline)) {
-      each_of([&](auto q) __attribute__((always_inline)) { read(q, stages[0], h); }, std::make_integer_sequence<int, kReads>{});
-      each_of([&](auto m) __attribute__((always_inline)) { multiply_in_place<DT>(x[h][m % NX], y[h][m / NX], sum[m % NX][m / NX]); },
-              std::make_integer_sequence<int, kHalf>{});
-    }, std::make_integer_sequence<int, 2>{});
-    meet();
-  }
-  both.load(stages[0], 0 < steps);
-  both.load(stages[1], 1 < steps);
-  wait_for_loads<Both::kLoads>();
-  meet();
-  each_of([&](auto q) __attribute__((always_inline)) { read(q, stages[0], First{}); }, std::make_integer_sequence<int, kReads>{});
+  const auto read_all = [&](const ZE_LDS char* tile, auto h) __attribute__((always_inline)) {
+    each_of([&](auto q) __attribute__((always_inline)) { read(q, tile, h); }, std::make_integer_sequence<int, kReads>{});
+  };
   const auto step = [&](ZE_LDS char* here, const ZE_LDS char* there, bool any) __attribute__((always_inline)) {
     const auto from_x = both.x.next(here, any);
     const auto from_y = both.y.next(here + Both::kY, any);
@@ -283,29 +288,75 @@ __device__ __forceinline__ void product_of_four(Both& both, Both* ends, int step
       multiply_in_place<DT>(x[h][m % NX], y[h][m / NX], sum[m % NX][m / NX]);
     }, std::make_integer_sequence<int, 2 * kHalf>{});
   };
-  for (int t = 0; t < steps; t += 2) {
-    step(stages[0], stages[1], t + 2 < steps);
-    step(stages[1], stages[0], t + 3 < steps);
-    // a sum may be read eleven issues after its product, wherever the compiler reads it behind the loop
-    asm volatile("s_nop 7\n\ts_nop 3");
-    in_order();
+
+  for (int k = 0; k < tiles.count; ++k) {
+    int tx, ty;
+    tiles.at(k, tx, ty);
+#pragma unroll
+    for (int i = 0; i < NX; ++i)
+#pragma unroll
+      for (int j = 0; j < NY; ++j) sum[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (k == 0 || has_ends || steps == 0) {   // nothing of this tile is under way
+      if (has_ends) {
+        start_ends(both, tx, ty);
+        both.load(stages[0], true);
+        wait_for_loads<0>();
+        meet();
+        each_of([&](auto h) __attribute__((always_inline)) {
+          read_all(stages[0], h);
+          each_of([&](auto m) __attribute__((always_inline)) { multiply_in_place<DT>(x[h][m % NX], y[h][m / NX], sum[m % NX][m / NX]); },
+                  std::make_integer_sequence<int, kHalf>{});
+        }, std::make_integer_sequence<int, 2>{});
+        meet();
+      }
+      start(both, tx, ty);
+      both.load(stages[0], 0 < steps);
+      both.load(stages[1], 1 < steps);
+      wait_for_loads<Both::kLoads>();
+      meet();
+      read_all(stages[0], First{});
+    }
+    for (int t = 0; t < steps; t += 2) {
+      const bool last = t + 2 >= steps, next = last && k + 1 < tiles.count && !has_ends;
+      if (next) {
+        int nx, ny;
+        tiles.at(k + 1, nx, ny);
+        start(both, nx, ny);
+      }
+      step(stages[0], stages[1], last ? next : true);
+      step(stages[1], stages[0], last ? next && 1 < steps : t + 3 < steps);
+      // a sum may be read eleven issues after its product, wherever the compiler reads it behind the loop
+      asm volatile("s_nop 7\n\ts_nop 3");
+      in_order();
+    }
+    use(sum, tx, ty);
+    if (has_ends || steps == 0) {   // LDS is free for another beginning
+      wait_for_loads<0>();
+      meet();
+    }
   }
   wait_for_loads<0>();
 }
 
-// The tile's sums: sum[i][j][r] is that of x = the wavefront's first + 16 i + 4 (lane / 16) + r, y = the wavefront's first + 16 j + lane % 16.  `ends`: NULL, or the operands
-// of a step that is added first (a row's end).
-template <class Both, class S = typename Both::S>
-__device__ __forceinline__ void product(Both& both, Both* ends, int steps, f32x4 (&sum)[S::NX][S::NY]) {
+// The sums of a workgroup's tiles, one tile after the other: use(sum, tx, ty), where sum[i][j][r] is that of x = the wavefront's first + 16 i + 4 (lane / 16) + r,
+// y = the wavefront's first + 16 j + lane % 16.  start(both, tx, ty) puts the operands to a tile's start; start_ends, if there are any, to a step that is added first
+// (the rows' ends).
+template <class Both, class Start, class StartEnds, class Use, class S = typename Both::S>
+__device__ __forceinline__ void products(const Tiles& tiles, int steps, bool has_ends, const Start& start, const StartEnds& start_ends, const Use& use) {
   if constexpr (S::kByHand) {
-    product_of_four(both, ends, steps, sum);
+    products_of_four<Both>(tiles, steps, has_ends, start, start_ends, use);
   } else {
+    if (tiles.count == 0) return;   // (as many workgroups as tiles, or more)
+    int tx, ty;
+    tiles.at(0, tx, ty);
     constexpr int DT = Both::DT, kTile = Both::kTile, kMore = S::kStages > 2 ? kTile : 16, kMost = S::kStages > 4 ? kTile : 16;
     // An array for each stage: what is loaded into one is seen to leave the others alone.
     __shared__ __attribute__((aligned(1024))) char stage0[kTile], stage1[kTile], stage2[kMore], stage3[kMore], stage4[kMost], stage5[kMost], stage6[kMost], stage7[kMost];
     ZE_LDS char* const stages[8] = {(ZE_LDS char*)stage0, (ZE_LDS char*)stage1, (ZE_LDS char*)stage2, (ZE_LDS char*)stage3,
                                     (ZE_LDS char*)stage4, (ZE_LDS char*)stage5, (ZE_LDS char*)stage6, (ZE_LDS char*)stage7};
     static_assert(S::kStages == 2 || S::kStages == 4 || S::kStages == 8, "arrays");
+    Both both;
+    f32x4 sum[S::NX][S::NY];
 #pragma unroll
     for (int i = 0; i < S::NX; ++i)
 #pragma unroll
@@ -324,8 +375,9 @@ __device__ __forceinline__ void product(Both& both, Both* ends, int steps, f32x4
         for (int i = 0; i < S::NX; ++i) sum[i][j] = multiply<DT>(x[h][i], y[h][j], sum[i][j]);
     };
 
-    if (ends) {
-      ends->load(stages[0], true);
+    if (has_ends) {
+      start_ends(both, tx, ty);
+      both.load(stages[0], true);
       wait_for_loads<0>();
       meet();
 #pragma unroll
@@ -336,6 +388,7 @@ __device__ __forceinline__ void product(Both& both, Both* ends, int steps, f32x4
       wait_for_loads<0>();
       meet();
     }
+    start(both, tx, ty);
 #pragma unroll
     for (int s = 0; s < S::kStages; ++s) both.load(stages[s], s < steps);
     wait_for_loads<(S::kStages - 1) * Both::kLoads>();
@@ -357,8 +410,9 @@ __device__ __forceinline__ void product(Both& both, Both* ends, int steps, f32x4
         add(1);
       }
     }
-    // nothing may be under way into LDS when the workgroup ends or uses it for something else
+    // nothing may be under way into LDS when the workgroup ends
     wait_for_loads<0>();
+    use(sum, tx, ty);
   }
 }
 
@@ -374,19 +428,6 @@ __device__ __forceinline__ void rest_of_sums(f32x4 (&sum)[S::NX][S::NY], int j) 
         if (k >= j) asm volatile("" : "+a"(sum[i][k]));
     in_order();
   }
-}
-
-// Which tile a workgroup has, of nx x ny, or none: neighbours in a band of eight rows of tiles follow one another in an XCD (workgroups go to the
-// eight of them in turn), so that what they share is read into its cache once.
-__device__ __forceinline__ bool tile_of(int nx, int ny, int& x, int& y) {
-  const int total = nx * ny, each = total / 8, more = total % 8, xcd = blockIdx.x & 7, n = blockIdx.x >> 3;
-  if (n >= each + (xcd < more)) return false;
-  const int at = xcd * each + (xcd < more ? xcd : more) + n;
-  constexpr int kBand = 8;
-  const int band = at / (kBand * nx), in = at - band * (kBand * nx), rows = ny - band * kBand < kBand ? ny - band * kBand : kBand;
-  y = band * kBand + in % rows;
-  x = in / rows;
-  return true;
 }
 
 }  // namespace
