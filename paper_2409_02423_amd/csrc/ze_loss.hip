@@ -188,6 +188,29 @@ __global__ void __launch_bounds__(kThreads) zero_rows_kernel(char* out, size_t s
   zero_row(out + (from + blockIdx.x) * stride, bytes);
 }
 
+// Values of a row in two 16 x 16 products beside one another: a lane has v at x and w at x + 16, four of each.  Half precision: lanes of
+// neighbouring groups exchange theirs, so that each has eight that follow one another and a row's 64 bytes go out at once (as four times eight bytes for each
+// of the two they took the caches twice as many requests).  Values at `cols` and behind it are left out.
+template <int DT>
+__device__ __forceinline__ void store_pair(char* row, int x, int cols, const float (&v)[4], const float (&w)[4]) {
+  Raw<DT, 4> a, b;
+  a.pack(v);
+  b.pack(w);
+  if constexpr (DT == kF32) {
+    a.store(row, x * 4, cols - x);
+    b.store(row, (x + 16) * 4, cols - x - 16);
+  } else {
+    const auto low = __builtin_amdgcn_permlane16_swap(a.w[0], b.w[0], false, false), high = __builtin_amdgcn_permlane16_swap(a.w[1], b.w[1], false, false);
+    Raw<DT> both;
+    both.w[0] = low[0];
+    both.w[1] = high[0];
+    both.w[2] = low[1];
+    both.w[3] = high[1];
+    const int group = (threadIdx.x & 63) / 16, to = x - 4 * group + 16 * (group & 1) + 8 * (group / 2);
+    both.store(row, to * 2, cols - to);
+  }
+}
+
 __device__ __forceinline__ bool any_lane(bool b) { return __builtin_amdgcn_ballot_w64(b) != 0; }
 
 // ---- forward -----------------------------------------------------------------------------
@@ -377,22 +400,23 @@ __device__ __forceinline__ void use_gradient(const GradientArgs& a, int there, f
     char* const row = a.g + (size_t)y * a.g_stride;
     const bool has = any_lane((unsigned)(label - x_wave) < (unsigned)(S::BX / S::WX));   // few parts of rows have a label
 #pragma unroll
-    for (int i = 0; i < S::NX; ++i) {
-      const int x = x0 + 16 * i;
-      float v[4];
+    for (int i = 0; i < S::NX; i += 2) {
+      float v[2][4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] = factor * __builtin_amdgcn_exp2f(fmaf(a.scale, sum[i][j][r], -lse) * kLog2E);
-      if (has) {
+      for (int k = 0; k < 2; ++k) {
+        const int x = x0 + 16 * (i + k);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] -= x + r == label ? factor : 0.0f;
+        for (int r = 0; r < 4; ++r) v[k][r] = factor * __builtin_amdgcn_exp2f(fmaf(a.scale, sum[i + k][j][r], -lse) * kLog2E);
+        if (has) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[k][r] -= x + r == label ? factor : 0.0f;
+        }
+        if (edge) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[k][r] = x + r < a.rows && y < there ? v[k][r] : 0.0f;
+        }
       }
-      if (edge) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = x + r < a.rows && y < there ? v[r] : 0.0f;
-      }
-      Raw<DT, 4> raw;
-      raw.pack(v);
-      if (!edge || x < a.rows_padded) raw.store(row, x * kBytes<DT>);
+      store_pair<DT>(row, x0 + 16 * i, a.rows_padded, v[0], v[1]);
     }
   }
 }
@@ -438,14 +462,13 @@ __device__ __forceinline__ void use_table_gradient(const OutArgs& a, float facto
     if (y >= a.rows) continue;
     char* const row = a.out + (size_t)y * a.out_stride;
 #pragma unroll
-    for (int i = 0; i < S::NX; ++i) {
-      const int x = x0 + 16 * i;
-      float v[4];
+    for (int i = 0; i < S::NX; i += 2) {
+      float v[2][4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] = factor * sum[i][j][r];
-      Raw<DT, 4> raw;
-      raw.pack(v);
-      raw.store(row, x * kBytes<DT>, a.cols - x);
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[k][r] = factor * sum[i + k][j][r];
+      store_pair<DT>(row, x0 + 16 * i, a.cols, v[0], v[1]);
     }
   }
 }
@@ -472,21 +495,18 @@ __device__ __forceinline__ void use_hidden_gradient(const OutArgs& a, int there,
     char* const row = finish ? a.out + (size_t)a.token_of[y] * a.out_stride : nullptr;
     float* const kept = a.kept + ((size_t)split * ny * S::BY + y) * a.kept_stride;
 #pragma unroll
-    for (int i = 0; i < S::NX; ++i) {
-      const int x = x0 + 16 * i;
-      if (x >= a.cols) continue;   // (kept rows are a multiple of 4 wide)
-      f32x4 s = sum[i][j];
-      if (a.add) s += *reinterpret_cast<const f32x4*>(kept + x);
-      if (!finish) {
-        *reinterpret_cast<f32x4*>(kept + x) = s;
-        continue;
-      }
-      float v[4];
+    for (int i = 0; i < S::NX; i += 2) {
+      float v[2][4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] = factor * s[r];
-      Raw<DT, 4> raw;
-      raw.pack(v);
-      raw.store(row, x * kBytes<DT>, a.cols - x);
+      for (int k = 0; k < 2; ++k) {
+        const int x = x0 + 16 * (i + k);
+        f32x4 s = sum[i + k][j];
+        if (a.add && x < a.cols) s += *reinterpret_cast<const f32x4*>(kept + x);   // (kept rows are a multiple of 4 wide)
+        if (!finish && x < a.cols) *reinterpret_cast<f32x4*>(kept + x) = s;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[k][r] = factor * s[r];
+      }
+      if (finish) store_pair<DT>(row, x0 + 16 * i, a.cols, v[0], v[1]);
     }
   }
 }
