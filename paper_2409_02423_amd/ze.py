@@ -53,43 +53,51 @@ def lib():
     return _lib
 
 
+# A call's checks take as long as a small kernel does, so what is right is seen with few questions, and what is wrong is asked again for its name.
+
+
 class _Call:
     """What the tensors of a call have in common, and the form that the library is given."""
+    __slots__ = ("device", "dtype", "shape", "table_shape", "tokens_shape", "ids", "form")
 
     def __init__(self, d_ids, what, like, like_what, rows, first, scale):
-        self.device = _current(like, like_what)
-        self.dtype = like.dtype
-        code = _DTYPES.get(self.dtype)
-        if code is None or like.dim() == 0:
+        device = self.device = _current(like, like_what)
+        dtype = self.dtype = like.dtype
+        code, of = _DTYPES.get(dtype), like.shape
+        if code is None or not of:
             raise TypeError("%s must be a float32, bfloat16 or float16 tensor of [..., cols]" % like_what)
-        self.cols = like.shape[-1]
-        self.shape = d_ids.shape if isinstance(d_ids, torch.Tensor) else None
-        ids = _IDS.get(d_ids.dtype) if self.shape is not None else None
+        cols = of[-1]
+        ids = _IDS.get(d_ids.dtype) if isinstance(d_ids, torch.Tensor) else None
         if ids is None:
             raise TypeError("%s must be a CUDA tensor of dtype int32 or int64" % what)
-        self.ids = _flat(d_ids, what, d_ids.dtype, self.device, d_ids.numel())
-        self.form = Form(d_ids.numel(), rows, self.cols, first, code, code, ids, scale)
+        count = d_ids.numel()
+        if not (d_ids.get_device() == device and d_ids.is_contiguous()):
+            _flat(d_ids, what, d_ids.dtype, device, count)
+        self.ids = d_ids.data_ptr()
+        shape = self.shape = d_ids.shape
+        self.table_shape, self.tokens_shape = (rows, cols), (count, cols) if len(shape) == 1 else (*shape, cols)
+        self.form = Form(count, rows, cols, first, code, code, ids, scale)
 
     def table(self, t, what, name, dtype=None):
         """Pointer of a [rows, cols] tensor whose rows are apart by a stride, which the form is told."""
         dtype = dtype or self.dtype
-        if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == self.device):
-            _refuse(t, what, dtype, self.device)
-        if t.dim() != 2 or t.shape[0] != self.form.rows or t.shape[1] != self.cols:
-            raise ValueError("%s must have shape %s" % (what, (self.form.rows, self.cols)))
+        if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == self.device and t.is_contiguous() and t.shape == self.table_shape:
+            return t.data_ptr()      # stride 0 in the form: cols
+        _refuse(t, what, dtype, self.device)
+        if t.shape != self.table_shape:
+            raise ValueError("%s must have shape %s" % (what, self.table_shape))
         return self._rows(t, what, name)
 
     def tokens(self, t, what, name):
         """Pointer of a tensor with a row for each id."""
-        if not (isinstance(t, torch.Tensor) and t.dtype is self.dtype and t.get_device() == self.device):
-            _refuse(t, what, self.dtype, self.device)
-        if t.shape[:-1] != self.shape or t.shape[-1] != self.cols:
-            raise ValueError("%s must have shape %s" % (what, (*self.shape, self.cols)))
-        if t.is_contiguous():
-            return t.data_ptr()      # stride 0 in the form: cols
+        if isinstance(t, torch.Tensor) and t.dtype is self.dtype and t.get_device() == self.device and t.is_contiguous() and t.shape == self.tokens_shape:
+            return t.data_ptr()
+        _refuse(t, what, self.dtype, self.device)
+        if t.shape != self.tokens_shape:
+            raise ValueError("%s must have shape %s" % (what, self.tokens_shape))
         if t.dim() != 2:
             try:
-                t = t.view(-1, self.cols)
+                t = t.view(-1, self.form.cols)
             except RuntimeError:
                 raise TypeError("%s: the distance from row to row must be the same everywhere" % what) from None
         return self._rows(t, what, name)
@@ -108,9 +116,19 @@ class _Call:
     def floats(self, t, what, count=None):
         return _flat(t, what, torch.float32, self.device, self.form.tokens if count is None else count)
 
+    def empty(self, shape, dtype, stream):
+        return _empty(shape, dtype, self.device, stream)
+
     def work(self, size, stream):
-        work = _empty(size, torch.uint8, self.device, stream) if size else None
-        return work, None if work is None else work.data_ptr()
+        """Workspace of a call, and its pointer."""
+        if not size:
+            return None, None
+        work = _empty(size, torch.uint8, self.device, stream)
+        return work, work.data_ptr()
+
+
+def _rows_of(d_table):
+    return d_table.shape[0] if isinstance(d_table, torch.Tensor) and d_table.dim() else 0
 
 
 # ---- embedding -----------------------------------------------------------------------
@@ -118,12 +136,14 @@ class _Call:
 
 def ze_embedding(d_ids, d_table, first=0, scale=1.0, d_out=None, stream=None):
     """scale * d_table[id - first] for each id, zeros for ids that are not this rank's; returns d_out, [..., cols] for ids of [...]."""
-    c = _Call(d_ids, "d_ids", d_table, "d_table", d_table.shape[0] if isinstance(d_table, torch.Tensor) and d_table.dim() else 0, first, scale)
+    c = _Call(d_ids, "d_ids", d_table, "d_table", _rows_of(d_table), first, scale)
     table = c.table(d_table, "d_table", "table")
     if d_out is None:
-        d_out = _empty((*c.shape, c.cols), c.dtype, c.device, stream)
+        d_out = c.empty(c.tokens_shape, c.dtype, stream)
     out = c.tokens(d_out, "d_out", "dtokens")
-    _check(lib().ze_embedding(c.form, c.ids, table, out, zc._stream_handle(stream)), "ze_embedding")
+    rc = lib().ze_embedding(c.form, c.ids, table, out, zc._stream_handle(stream))
+    if rc:
+        _check(rc, "ze_embedding")
     return d_out
 
 
@@ -135,7 +155,7 @@ def ze_embedding_backward(d_ids, d_dout, rows, first=0, scale=1.0, d_dtable=None
     c = _Call(d_ids, "d_ids", d_dout, "d_dout", rows, first, scale)
     dout = c.tokens(d_dout, "d_dout", "tokens")
     if d_dtable is None:
-        d_dtable = _empty((rows, c.cols), torch.float32, c.device, stream)
+        d_dtable = c.empty(c.table_shape, torch.float32, stream)
     dtype = c.dtype if isinstance(d_dtable, torch.Tensor) and d_dtable.dtype is c.dtype else torch.float32
     dtable = c.table(d_dtable, "d_dtable", "dtable", dtype)
     c.form.grad_dtype = _DTYPES[dtype]
@@ -150,7 +170,7 @@ def ze_embedding_backward(d_ids, d_dout, rows, first=0, scale=1.0, d_dtable=None
 
 
 def _loss_call(d_hidden, d_table, d_labels, first, scale):
-    c = _Call(d_labels, "d_labels", d_hidden, "d_hidden", d_table.shape[0] if isinstance(d_table, torch.Tensor) and d_table.dim() else 0, first, scale)
+    c = _Call(d_labels, "d_labels", d_hidden, "d_hidden", _rows_of(d_table), first, scale)
     return c, c.tokens(d_hidden, "d_hidden", "tokens"), c.table(d_table, "d_table", "table")
 
 
@@ -159,7 +179,7 @@ def ze_vocab_loss(d_hidden, d_table, d_labels, first=0, scale=1.0, d_stats=None,
     token the greatest logit, the sum of exponentials, the label's logit.  A negative label leaves its token out."""
     c, hidden, table = _loss_call(d_hidden, d_table, d_labels, first, scale)
     if d_stats is None:
-        d_stats = _empty((3, c.form.tokens), torch.float32, c.device, stream)
+        d_stats = c.empty((3, c.form.tokens), torch.float32, stream)
     stats = c.floats(d_stats, "d_stats", 3 * c.form.tokens)
     L = lib()
     size = L.ze_loss_work_bytes(c.form, hidden, table)
@@ -198,9 +218,9 @@ def ze_vocab_loss_backward(d_hidden, d_table, d_labels, d_lse, d_dloss, first=0,
     if (d_dhidden is not None and not want_hidden) or (d_dtable is not None and not want_table):
         raise ValueError("an output that is not wanted")
     if d_dhidden is None and want_hidden:
-        d_dhidden = _empty(d_hidden.shape, c.dtype, c.device, stream)
+        d_dhidden = c.empty(d_hidden.shape, c.dtype, stream)
     if d_dtable is None and want_table:
-        d_dtable = _empty(d_table.shape, c.dtype, c.device, stream)
+        d_dtable = c.empty(d_table.shape, c.dtype, stream)
     dhidden = c.tokens(d_dhidden, "d_dhidden", "dtokens") if want_hidden else None
     dtable = c.table(d_dtable, "d_dtable", "dtable") if want_table else None
     lse, dloss = c.floats(d_lse, "d_lse"), c.floats(d_dloss, "d_dloss")
