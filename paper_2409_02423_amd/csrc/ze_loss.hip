@@ -565,33 +565,60 @@ __global__ void __launch_bounds__(kThreads) hidden_finish_kernel(OutArgs a) {
 
 // ---- host: how a call is laid out ----------------------------------------------------------
 
-using Large = Shape<256, 256, 2, 2, 2, true>;
+using Large = Shape<256, 256, 2, 2, 2, true>;   // half precision
+using Half = Shape<256, 128, 2, 2, 2, true>;    // the same
 using Medium = Shape<128, 128, 2, 2, 2>;
 using Small = Shape<64, 64, 2, 2, 4>;
-using Thin = Shape<32, 16, 2, 1, 8>;   // logits of few tokens: what counts is how many compute units read the table
-enum { kLarge, kMedium, kSmall, kThin };
+using Thin = Shape<32, 16, 2, 1, 8>;            // logits of few tokens: what counts is how many compute units read the table
+enum { kLarge, kHalf, kMedium, kSmall, kThin, kShapes };
+struct Size {
+  int x, y;         // of a tile
+  int part;         // columns of a wavefront
+  int at_once;      // workgroups of a compute unit
+  int cost;         // of a value, in hundredths of that in a large tile where there are many tiles
+};
+template <class S>
+constexpr Size size_of(int at_once, int cost) {
+  return Size{S::BX, S::BY, S::BX / S::WX, at_once, cost};
+}
+constexpr Size kSizes[kShapes] = {size_of<Large>(1, 100), size_of<Half>(1, 115), size_of<Medium>(2, 145), size_of<Small>(2, 220), size_of<Thin>(3, 0)};
 constexpr int kComputeUnits = 256;
 constexpr size_t kMostTiles = (size_t)1 << 22;   // of one launch
 
-size_t tiles(int shape, size_t nx, size_t ny) {
-  const size_t b = shape == kLarge ? Large::BX : shape == kMedium ? Medium::BX : Small::BX;
-  return parts(nx, b) * parts(ny, b);
-}
+size_t tiles(int shape, size_t nx, size_t ny) { return parts(nx, kSizes[shape].x) * parts(ny, kSizes[shape].y); }
+
 // Workgroups of a launch: one for each tile, or, where a workgroup goes on from tile to tile, for each compute unit.
 template <class S>
 unsigned groups_for(size_t tiles) {
   return (unsigned)(S::kByHand && tiles > kComputeUnits ? kComputeUnits : tiles);
 }
+
+// The shape that takes the least time: as many tiles one after the other as the busiest compute unit has, times what one costs.  Small tiles where a y is
+// no longer than one of them: then x is read, and little else.
 int shape_for(int dtype, size_t nx, size_t ny) {
-  if (dtype != ZC_F32 && tiles(kLarge, nx, ny) >= kComputeUnits * 3 / 4) return kLarge;
-  return tiles(kMedium, nx, ny) >= kComputeUnits * 3 / 4 ? kMedium : kSmall;
+  if (ny <= (size_t)kSizes[kSmall].y) return kSmall;
+  int best = kSmall;
+  size_t least = ~(size_t)0;
+  for (int s = dtype == ZC_F32 ? kMedium : kLarge; s <= kSmall; ++s) {
+    // (fp32 products are bound by the matrix instructions in every shape, by those alone in the larger one)
+    const size_t cost = dtype != ZC_F32 ? kSizes[s].cost : s == kMedium ? 100 : 115;
+    const size_t time = parts(tiles(s, nx, ny), kComputeUnits) * kSizes[s].x * kSizes[s].y * cost;
+    if (time < least) {
+      least = time;
+      best = s;
+    }
+  }
+  return best;
 }
 
 #define ZE_BY_SHAPE(SHAPE, DT, LAUNCH)              \
   do {                                              \
     if ((SHAPE) == kMedium) LAUNCH(DT, Medium);     \
     else if ((SHAPE) == kSmall) LAUNCH(DT, Small);  \
-    else if constexpr (DT != kF32) LAUNCH(DT, Large); \
+    else if constexpr (DT != kF32) {                \
+      if ((SHAPE) == kHalf) LAUNCH(DT, Half);       \
+      else LAUNCH(DT, Large);                       \
+    }                                               \
   } while (0)
 #define ZE_BY_SHAPE_OF_LOGITS(SHAPE, DT, LAUNCH)    \
   do {                                              \
@@ -655,7 +682,7 @@ Plan plan_with(const struct ze_form& f, bool backward, size_t piece, bool pack_h
     if (even < p.piece) p.piece = even;
   }
   p.shape = shape_for(f.dtype, p.piece, f.tokens);
-  if (!backward && p.shape == kSmall && f.tokens <= Thin::BY) p.shape = kThin;
+  if (!backward && f.tokens <= Thin::BY) p.shape = kThin;
   // (The ends are added first also where a copy has them behind the rest: the sums do not depend on where the tensors lie.)
   p.steps = (int)(f.cols * p.e / kStepBytes);
   p.ends = f.cols * p.e % kStepBytes != 0;
@@ -667,23 +694,23 @@ Plan plan_with(const struct ze_form& f, bool backward, size_t piece, bool pack_h
   p.table_ends = places.take(p.ends && !pack_table ? p.piece * kStepBytes : 0);
   p.hidden_ends = places.take(p.ends && !backward && !pack_hidden ? p.padded * kStepBytes : 0);
   if (!backward) {
-    const size_t part = p.shape == kLarge    ? Large::BX / Large::WX
-                        : p.shape == kMedium ? Medium::BX / Medium::WX
-                        : p.shape == kSmall  ? Small::BX / Small::WX
-                                             : Thin::BX / Thin::WX;
+    const size_t part = kSizes[p.shape].part;
     p.parts = p.piece ? parts(f.rows, p.piece) * parts(up(p.piece, 256), part) : 0;
     p.part = places.take(f.tokens * p.parts * sizeof(Part));
   } else {
     const size_t padded = up(p.piece, kStepBytes / p.e);
     p.g = places.take(p.padded * padded * p.e);
-    p.hidden_shape = shape_for(f.dtype, f.cols, f.tokens);
-    const size_t by = p.hidden_shape == kLarge ? Large::BY : p.hidden_shape == kMedium ? Medium::BY : Small::BY;
     const size_t steps = padded * p.e / kStepBytes;
-    p.sharers = p.hidden_shape == kLarge ? kComputeUnits : 2 * kComputeUnits;   // as many as run at once
+    p.hidden_shape = shape_for(f.dtype, f.cols, f.tokens);
+    // Where a tile's steps are shared out, few tiles are as good as many: the better of the shapes of which not every row of tiles keeps sums of its own.
+    if (f.dtype != ZC_F32 && f.tokens > (size_t)kSizes[kSmall].y && p.hidden_shape != kLarge && tiles(kHalf, f.cols, f.tokens) * (steps / 8) >= kComputeUnits)
+      p.hidden_shape = kHalf;
+    const Size& size = kSizes[p.hidden_shape];
+    p.sharers = size.at_once * kComputeUnits;   // as many as run at once
     p.most_splits = (int)(steps < 16 ? 1 : steps / 8);
     if (p.piece < f.rows || p.most_splits > 1) {
       // splits x rows is greatest where all sharers have a tile, or all rows one
-      const size_t rows = parts(f.tokens, by) * by, shared = parts((size_t)p.sharers, parts(f.cols, by)) * by;
+      const size_t rows = up(f.tokens, size.y), shared = parts((size_t)p.sharers, parts(f.cols, size.x)) * size.y;
       p.kept = places.take((rows > shared ? rows : shared) * up(f.cols, 4) * 4);
     }
   }

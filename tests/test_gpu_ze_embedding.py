@@ -155,6 +155,21 @@ def test_gradient_against_differences():
         assert abs(float(value(more) - value(table)) - float(got[v, x])) < 1e-4
 
 
+@pytest.mark.parametrize("tokens, rows, cols", [(1, 5, 3), (15, 40, 100), (512, 1000, 256), (4097, 3, 64), (8192, 500, 72), (8193, 500, 72), (30000, 70001, 9)])
+def test_a_workspace_as_large_as_it_has_to_be(tokens, rows, cols):
+    """What lies behind a workspace of just the bytes that a call asks for stays as it was."""
+    g = _generator(tokens)
+    at = _ids(tokens, -1, min(rows, 30), g)
+    dout = torch.randn((tokens, cols), generator=g, device="cuda").bfloat16()
+    out = torch.empty((rows, cols), device="cuda")
+    L, f = ze.lib(), ze.Form(tokens, rows, cols, 0, 1, 0, ze.ZE_I64, 1.0)
+    size = L.ze_embedding_work_bytes(f)
+    work = torch.full((size + (16 << 20),), 0x5A, dtype=torch.uint8, device="cuda")
+    assert L.ze_embedding_backward(f, at.data_ptr(), dout.data_ptr(), out.data_ptr(), 0, work.data_ptr(), size, torch.cuda.current_stream().cuda_stream) == 0
+    _close(out, *ze_ref.embedding_backward(at, dout, rows))
+    assert (work[size:] == 0x5A).all()
+
+
 def test_nothing_to_do():
     empty = torch.empty(0, dtype=torch.int64, device="cuda")
     table = torch.ones((3, 4), device="cuda")

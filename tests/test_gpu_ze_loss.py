@@ -244,6 +244,35 @@ def test_gradients_against_differences():
         assert abs(got - float(want)) < 1e-5 + 1e-4 * float(want)
 
 
+def _form(hidden, table, labels):
+    types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    return ze.Form(labels.numel(), table.shape[0], table.shape[1], 0, types[hidden.dtype], types[hidden.dtype], ze.ZE_I64, 1.0)
+
+
+@pytest.mark.parametrize("tokens, rows, cols, dtype, absent", [
+    (1700, 2049, 1030, "bf16", 0.2), (1700, 2049, 1030, "bf16", 0.9), (300, 9000, 520, "f16", 0.5), (2047, 3001, 2050, "f16", 0.5), (130, 5000, 260, "bf16", 0.0),
+    (70, 3000, 64, "bf16", 0.3), (65, 4000, 200, "f32", 0.0), (513, 1200, 1025, "f32", 0.5), (1, 3000, 77, "bf16", 0.0), (2100, 2600, 4104, "bf16", 0.1)])
+def test_a_workspace_as_large_as_it_has_to_be(tokens, rows, cols, dtype, absent):
+    """What lies behind a workspace of just the bytes that a call asks for stays as it was."""
+    hidden, table, labels, dloss = _inputs(tokens, rows, cols, TYPES[dtype], 13, absent=absent)
+    L, f, behind = ze.lib(), _form(hidden, table, labels), 96 << 20
+    stats, lse = torch.empty((3, tokens), device="cuda"), None
+    dh, dw = torch.empty_like(hidden), torch.empty_like(table)
+    at = (hidden.data_ptr(), table.data_ptr(), labels.data_ptr())
+    for piece in (None, 0, 512):
+        size = L.ze_loss_work_bytes(f, *at[:2]) if piece is None else L.ze_loss_backward_work_bytes(f, *at[:2], piece)
+        work = torch.full((size + behind,), 0x5A, dtype=torch.uint8, device="cuda")
+        if piece is None:
+            assert L.ze_vocab_loss(f, *at, stats.data_ptr(), work.data_ptr(), size, torch.cuda.current_stream().cuda_stream) == 0
+            lse = ze.ze_join_loss(stats, labels)[1]
+        else:
+            assert L.ze_vocab_loss_backward(f, *at, lse.data_ptr(), dloss.data_ptr(), dh.data_ptr(), dw.data_ptr(), piece, work.data_ptr(), size,
+                                            torch.cuda.current_stream().cuda_stream) == 0
+            for a, b, c in zip((dh, dw), *ze_ref.vocab_loss_backward(hidden, table, labels, lse, dloss)):
+                _close(a, b, c)
+        assert (work[size:] == 0x5A).all()
+
+
 def test_nothing_to_do():
     hidden, table, labels, dloss = _inputs(3, 20, 32, torch.bfloat16, 91, absent=0.0)
     none = labels[:0]
