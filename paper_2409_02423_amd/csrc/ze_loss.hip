@@ -567,6 +567,7 @@ __global__ void __launch_bounds__(kThreads) hidden_finish_kernel(OutArgs a) {
 
 using Large = Shape<256, 256, 2, 2, 2, true>;   // half precision
 using Half = Shape<256, 128, 2, 2, 2, true>;    // the same
+using Deep = Shape<256, 128, 2, 2, 3, true>;    // a half one for many steps: three under way
 using Medium = Shape<128, 128, 2, 2, 2>;
 using Small = Shape<64, 64, 2, 2, 4>;
 using Thin = Shape<32, 16, 2, 1, 8>;            // logits of few tokens: what counts is how many compute units read the table
@@ -619,6 +620,11 @@ int shape_for(int dtype, size_t nx, size_t ny) {
       if ((SHAPE) == kHalf) LAUNCH(DT, Half);       \
       else LAUNCH(DT, Large);                       \
     }                                               \
+  } while (0)
+#define ZE_BY_SHAPE_OF_HIDDEN(SHAPE, DT, LAUNCH)    \
+  do {                                              \
+    if ((SHAPE) != kHalf) ZE_BY_SHAPE(SHAPE, DT, LAUNCH); \
+    else if constexpr (DT != kF32) LAUNCH(DT, Deep); \
   } while (0)
 #define ZE_BY_SHAPE_OF_LOGITS(SHAPE, DT, LAUNCH)    \
   do {                                              \
@@ -702,9 +708,10 @@ Plan plan_with(const struct ze_form& f, bool backward, size_t piece, bool pack_h
     p.g = places.take(p.padded * padded * p.e);
     const size_t steps = padded * p.e / kStepBytes;
     p.hidden_shape = shape_for(f.dtype, f.cols, f.tokens);
-    // Where a tile's steps are shared out, few tiles are as good as many: the better of the shapes of which not every row of tiles keeps sums of its own.
+    // Where a tile's steps are shared out, few tiles are as good as many.  Large ones then keep twice the sums that half ones do, and take two thirds of
+    // the time for a product (1024 tokens, 32003 x 2048 fp16 values: HIDDEN_LARGE and HIDDEN_HALF us with joining).
     if (f.dtype != ZC_F32 && f.tokens > (size_t)kSizes[kSmall].y && p.hidden_shape != kLarge && tiles(kHalf, f.cols, f.tokens) * (steps / 8) >= kComputeUnits)
-      p.hidden_shape = kHalf;
+      p.hidden_shape = tiles(kLarge, f.cols, f.tokens) * steps >= 16 * kComputeUnits ? kLarge : kHalf;
     const Size& size = kSizes[p.hidden_shape];
     p.sharers = size.at_once * kComputeUnits;   // as many as run at once
     p.most_splits = (int)(steps < 16 ? 1 : steps / 8);
@@ -925,7 +932,7 @@ void backward(const struct ze_form& f, const Plan& p, const void* d_hidden, cons
       hipLaunchKernelGGL((hidden_finish_kernel<D, S>), dim3((unsigned)parts(f.cols, kThreads * 4), (unsigned)(f.tokens < 2048 ? f.tokens : 2048)), \
                          dim3(kThreads), 0, s, a);                                                                                         \
   } while (0)
-      ZE_BY_SHAPE(p.hidden_shape, DT, LAUNCH);
+      ZE_BY_SHAPE_OF_HIDDEN(p.hidden_shape, DT, LAUNCH);
 #undef LAUNCH
     }
   }

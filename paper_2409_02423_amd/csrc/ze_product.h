@@ -250,10 +250,11 @@ struct Tiles {
 template <class Both, class Start, class StartEnds, class Use, class S = typename Both::S>
 __device__ __forceinline__ void products_of_four(const Tiles& tiles, int steps, bool has_ends, const Start& start, const StartEnds& start_ends, const Use& use) {
   constexpr int DT = Both::DT;
-  __shared__ __attribute__((aligned(1024))) char stage0[Both::kTile], stage1[Both::kTile];
-  ZE_LDS char* const stages[2] = {(ZE_LDS char*)stage0, (ZE_LDS char*)stage1};
+  constexpr int kStages = S::kStages;
+  __shared__ __attribute__((aligned(1024))) char stage0[Both::kTile], stage1[Both::kTile], stage2[kStages > 2 ? Both::kTile : 16];
+  ZE_LDS char* const stages[3] = {(ZE_LDS char*)stage0, (ZE_LDS char*)stage1, (ZE_LDS char*)stage2};
   constexpr int NX = S::NX, NY = S::NY, kReads = NX + NY, kHalf = NX * NY, kReadEvery = 2, kMeet = kReads * kReadEvery + NX, kSpread = (2 * kHalf - kMeet) / Both::kLoads;
-  static_assert(S::kStages == 2 && kReads * kReadEvery <= kMeet && kMeet + (Both::kLoads - 1) * kSpread < 2 * kHalf && kReads * kReadEvery <= kHalf, "order");
+  static_assert((kStages == 2 || kStages == 3) && kReads * kReadEvery <= kMeet && kMeet + (Both::kLoads - 1) * kSpread < 2 * kHalf && kReads * kReadEvery <= kHalf, "order");
   Both both;
   f32x4 sum[NX][NY];
   i32x4 x[2][NX], y[2][NY];
@@ -273,7 +274,7 @@ __device__ __forceinline__ void products_of_four(const Tiles& tiles, int steps, 
       constexpr int h = p / kHalf, m = p % kHalf;
       in_order();
       if constexpr (p == kMeet) {
-        wait_for_loads<0>();
+        wait_for_loads<(kStages - 2) * Both::kLoads>();
         meet();
         in_order();
       }
@@ -310,21 +311,21 @@ __device__ __forceinline__ void products_of_four(const Tiles& tiles, int steps, 
         meet();
       }
       start(both, tx, ty);
-      both.load(stages[0], 0 < steps);
-      both.load(stages[1], 1 < steps);
-      wait_for_loads<Both::kLoads>();
+      each_of([&](auto s) __attribute__((always_inline)) { both.load(stages[s], s < steps); }, std::make_integer_sequence<int, kStages>{});
+      wait_for_loads<(kStages - 1) * Both::kLoads>();
       meet();
       read_all(stages[0], First{});
     }
-    for (int t = 0; t < steps; t += 2) {
-      const bool last = t + 2 >= steps, next = last && k + 1 < tiles.count && !has_ends;
+    for (int t = 0; t < steps; t += kStages) {
+      const bool last = t + kStages >= steps, next = last && k + 1 < tiles.count && !has_ends;
       if (next) {
         int nx, ny;
         tiles.at(k + 1, nx, ny);
         start(both, nx, ny);
       }
-      step(stages[0], stages[1], last ? next : true);
-      step(stages[1], stages[0], last ? next && 1 < steps : t + 3 < steps);
+      each_of([&](auto s) __attribute__((always_inline)) {
+        step(stages[s], stages[(s + 1) % kStages], last ? next && s < steps : t + kStages + s < steps);
+      }, std::make_integer_sequence<int, kStages>{});
       // a sum may be read eleven issues after its product, wherever the compiler reads it behind the loop
       asm volatile("s_nop 7\n\ts_nop 3");
       in_order();
