@@ -300,6 +300,19 @@ __global__ void __launch_bounds__(S::kThreads) logits_kernel(LogitsArgs a) {
   logits_of_tiles<DT, S>(a, there, [&](f32x4 (&sum)[S::NX][S::NY], int tx, int ty) { use_logits<DT, S>(a, there, sum, tx, ty); });
 }
 
+template <int CTRL>
+__device__ __forceinline__ float dpp_max(float v) {
+  return fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true)));
+}
+// The greatest of the 64 lanes' values, in every lane.  All 64 have to be active.
+__device__ __forceinline__ float wave_max(float v) {
+  v = dpp_max<0xB1>(v);    // quad_perm 1 0 3 2
+  v = dpp_max<0x4E>(v);    // quad_perm 2 3 0 1
+  v = dpp_max<0x141>(v);   // row_half_mirror
+  v = dpp_max<0x140>(v);   // row_mirror
+  return fmaxf(fmaxf(read_lane(v, 0), read_lane(v, 16)), fmaxf(read_lane(v, 32), read_lane(v, 48)));
+}
+
 // Joins parts of a sum of exponentials: the sums are taken to the greater of the two logits.  (Where that is -inf there is nothing in either.)
 __device__ __forceinline__ void join(float& most, float& total, float other_most, float other) {
   const float to = fmaxf(most, other_most), from = to == -kInf ? 0.0f : to;
@@ -314,32 +327,32 @@ __global__ void __launch_bounds__(kThreads) stats_kernel(const int* row_of, size
   const int lane = threadIdx.x & 63;
   if (n >= tokens) return;
   const int row = row_of[n];
-  float most = -kInf, total = 0.0f;
+  float most = -kInf, total = 0.0f, label = 0.0f;
   if (row >= 0) {
+    label = target[row];
     const Part* p = parts + (size_t)row * stride;
-    constexpr int kAhead = 4;
+    constexpr int kAhead = 8;
     for (size_t i = lane; i < count; i += 64 * kAhead) {
       Part part[kAhead];
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) part[u] = i + 64 * u < count ? p[i + 64 * u] : Part{-kInf, 0.0f};
+      float to = most;
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) join(most, total, part[u].most, part[u].sum);
-    }
+      for (int u = 0; u < kAhead; ++u) to = fmaxf(to, part[u].most);
+      const float from = to == -kInf ? 0.0f : to;
+      total *= __builtin_amdgcn_exp2f((most - from) * kLog2E);
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      // (from one lane to the other and back the same two are joined: the same result in both)
-      const float other_most = __shfl_xor(most, d), other = __shfl_xor(total, d);
-      const bool first = (lane & d) == 0;
-      float m = first ? most : other_most, t = first ? total : other;
-      join(m, t, first ? other_most : most, first ? other : total);
-      most = m;
-      total = t;
+      for (int u = 0; u < kAhead; ++u) total += part[u].sum * __builtin_amdgcn_exp2f((part[u].most - from) * kLog2E);
+      most = to;
     }
+    const float to = wave_max(most), from = to == -kInf ? 0.0f : to;
+    total = wave_sum(total * __builtin_amdgcn_exp2f((most - from) * kLog2E));
+    most = to;
   }
   if (lane == 0) {
     stats[n] = most;
     stats[tokens + n] = total;
-    stats[2 * tokens + n] = row < 0 ? 0.0f : target[row];
+    stats[2 * tokens + n] = label;
   }
 }
 
@@ -929,7 +942,7 @@ void backward(const struct ze_form& f, const Plan& p, const void* d_hidden, cons
     const size_t all = a.nx * parts(f.tokens, S::BY), groups = p.most_splits > 1 && all < (size_t)p.sharers ? (size_t)p.sharers : all;     \
     hipLaunchKernelGGL((hidden_gradient_kernel<D, S>), dim3(groups_for<S>(groups)), dim3(S::kThreads), 0, s, a);                                \
     if (a.last && p.most_splits > 1)                                                                                                       \
-      hipLaunchKernelGGL((hidden_finish_kernel<D, S>), dim3((unsigned)parts(f.cols, kThreads * 4), (unsigned)(f.tokens < 2048 ? f.tokens : 2048)), \
+      hipLaunchKernelGGL((hidden_finish_kernel<D, S>), dim3((unsigned)parts(f.cols, kThreads * 4), (unsigned)(f.tokens < 512 ? f.tokens : 512)), \
                          dim3(kThreads), 0, s, a);                                                                                         \
   } while (0)
       ZE_BY_SHAPE_OF_HIDDEN(p.hidden_shape, DT, LAUNCH);
