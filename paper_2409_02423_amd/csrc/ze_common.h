@@ -23,6 +23,12 @@ __device__ __forceinline__ uint32_t sum_up_to(uint32_t v) {
   return dpp_count<0x143, 0xC>(v);
 }
 
+// Which of this rank's rows an id names, of `rows` from `first` on, or -1.
+__device__ __forceinline__ long long row_of_id(long long id, long long first, long long rows) {
+  const unsigned long long at = (unsigned long long)id - (unsigned long long)first;   // (below `first`, and negative: more than any number of rows)
+  return at < (unsigned long long)rows ? (long long)at : -1;
+}
+
 constexpr size_t kMaxStride = (size_t)1 << 20;   // elements: a tile's rows are told apart by 32 bits
 
 size_t up(size_t n, size_t to) { return (n + to - 1) / to * to; }

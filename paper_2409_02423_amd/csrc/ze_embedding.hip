@@ -36,8 +36,8 @@ __global__ void __launch_bounds__(kThreads) lookup_kernel(LookupArgs a) {
   const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
   const size_t n = (size_t)blockIdx.x * (kThreads >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
   if (n >= a.tokens) return;
-  const long long local = (long long)static_cast<const ID*>(a.ids)[n] - a.first;
-  const bool here = local >= 0 && local < a.rows;
+  const long long local = row_of_id(static_cast<const ID*>(a.ids)[n], a.first, a.rows);
+  const bool here = local >= 0;
   const char* row = a.table + (here ? (size_t)local : 0) * a.stride_table;
   char* out = a.out + n * a.stride_out;
   const int from = (int)blockIdx.y * kLookupSteps * lanes + lane;
@@ -143,8 +143,8 @@ __device__ __forceinline__ void sum_counts(uint32_t (&counts)[kCounts], int bits
 // A token's key: its row of the table, or `rows` where it has none.
 template <class ID>
 __device__ __forceinline__ uint32_t key_of(const void* ids, size_t n, long long first, long long rows) {
-  const long long local = (long long)static_cast<const ID*>(ids)[n] - first;
-  return local >= 0 && local < rows ? (uint32_t)local : (uint32_t)rows;
+  const long long row = row_of_id(static_cast<const ID*>(ids)[n], first, rows);
+  return row >= 0 ? (uint32_t)row : (uint32_t)rows;
 }
 
 struct SortArgs {

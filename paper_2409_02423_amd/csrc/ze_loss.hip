@@ -82,9 +82,8 @@ __global__ void __launch_bounds__(kListThreads) list_kernel(const ID* ids, int t
       const bool has = id[i] >= 0;
       list.row_of[n] = has ? row : -1;
       if (!has) continue;
-      const long long local = id[i] - first;
       list.token_of[row] = n;
-      list.label_of[row] = local >= 0 && local < rows ? (int)local : -1;
+      list.label_of[row] = (int)row_of_id(id[i], first, rows);
       if (list.target) list.target[row] = -kInf;
       if (lse) {
         const float size = fabsf(of_dloss[i]);

@@ -296,7 +296,11 @@ __device__ __forceinline__ void products_of_four(const Tiles& tiles, int steps, 
 #pragma unroll
     for (int i = 0; i < NX; ++i)
 #pragma unroll
-      for (int j = 0; j < NY; ++j) sum[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int j = 0; j < NY; ++j) {
+        sum[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        asm volatile("" : "+a"(sum[i][j]));
+      }
+    asm volatile("s_nop 1");   // (a register that has just been written is not yet a product's)
     if (k == 0 || has_ends || steps == 0) {   // nothing of this tile is under way
       if (has_ends) {
         start_ends(both, tx, ty);

@@ -50,3 +50,27 @@ def test_loads_into_lds_are_waited_for_before_the_end(assembly):
         seen += 1
         assert re.search(r"s_waitcnt vmcnt\(0\)", body[last:]), name
     assert seen >= 30
+
+
+def test_large_products_keep_their_sums_in_place(assembly):
+    """Where the order of instructions is written down, a step holds its products, its reads and its loads, and moves no sum; and between a step's last product and
+    the first use of a sum there are eleven issues (two s_nop), which the compiler does not see to in instructions by name."""
+    text = assembly["ze_loss.hip"]
+    seen = 0
+    for name in re.findall(r"\.amdhsa_kernel (\S*Lb1E\S*)", text):
+        if "finish" in name:
+            continue
+        nx, ny, stages = (int(v) for v in re.search(r"ShapeILi(\d+)ELi(\d+)ELi2ELi2ELi(\d)E", name).groups())
+        body = re.search(r"^%s:.*?^\.Lfunc_end" % re.escape(name), text, flags=re.S | re.M).group(0)
+        each = 2 * (nx // 32) * (ny // 32)
+        steps = [b for b in re.split(r"^\.LBB\S+:", body, flags=re.M) if b.count("v_mfma") >= each]
+        assert sum(b.count("v_mfma") for b in steps) >= stages * each, name
+        for b in steps:
+            inside = b[b.index("v_mfma"):b.rindex("v_mfma")]
+            assert "v_accvgpr" not in inside and "scratch" not in inside and "v_mov_b32" not in inside, name
+        waits = [m.start() for m in re.finditer(r"s_nop 7\n\ts_nop 3", body)]
+        assert waits, name
+        for at in waits:
+            assert "v_accvgpr" not in body[body.rindex("v_mfma", 0, at):at], name
+        seen += 1
+    assert seen >= 14
