@@ -37,12 +37,87 @@ struct List {
   size_t padded;
 };
 
+constexpr int kThreads = 256;
+
+// A copy of rows of `cols` values whose rows start at multiples of 128 bytes and end in zeros.  Row r of the copy is row token_of[r] of `in`, or of
+// zeros where that is negative; without a list row r, of `rows`.
+struct PackArgs {
+  const char* in;
+  size_t stride;        // bytes
+  const int* token_of;
+  size_t rows;          // of `in`, without a list
+  char* out;
+  size_t out_stride;    // bytes, a multiple of 128
+  int cols;
+};
+
+// Of row r of the copy, 16 bytes at `at`.
+template <int DT>
+__device__ __forceinline__ void pack_piece(const PackArgs& a, size_t r, long long source, uint32_t at) {
+  constexpr int kN = kVec<DT>;
+  Raw<DT> raw;
+  const int valid = source < 0 ? 0 : a.cols - (int)(at / kBytes<DT>);
+  const char* in = a.in + (source < 0 ? 0 : (size_t)source) * a.stride;
+  if (valid >= kN) {
+    raw.load(in, at);
+  } else {
+#pragma unroll
+    for (int i = 0; i < raw.kWords; ++i) raw.w[i] = 0;
+    if (valid > 0) raw.load(in, at, valid);
+  }
+  raw.store(a.out + r * a.out_stride, at);
+}
+__device__ __forceinline__ long long source_of(const PackArgs& a, size_t r) { return a.token_of ? (long long)a.token_of[r] : r < a.rows ? (long long)r : -1; }
+
+template <int DT>
+__device__ __forceinline__ void pack_row(const PackArgs& a, size_t r) {
+  const long long source = source_of(a, r);
+  for (uint32_t at = threadIdx.x * 16; at < a.out_stride; at += kThreads * 16) pack_piece<DT>(a, r, source, at);
+}
+
+// The same of rows of one step each (a row's ends), `many` rows from `first` on: eight lanes a row.
+template <int DT>
+__device__ __forceinline__ void pack_ends(const PackArgs& a, size_t first, size_t many) {
+  const size_t r = first + threadIdx.x / 8;
+  if (r < many) pack_piece<DT>(a, r, source_of(a, r), threadIdx.x % 8 * 16);
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kThreads) pack_kernel(PackArgs a, size_t from) {
+  pack_row<DT>(a, from + blockIdx.x);
+}
+
+__device__ __forceinline__ void zero_row(char* row, size_t bytes) {
+  const size_t head = (16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15;
+  if (bytes <= head) {
+    for (size_t i = threadIdx.x * 2; i < bytes; i += kThreads * 2) *reinterpret_cast<uint16_t*>(row + i) = 0;
+    return;
+  }
+  const size_t body = (bytes - head) / 16;
+  for (size_t i = threadIdx.x; i < body; i += kThreads) reinterpret_cast<i32x4*>(row + head)[i] = i32x4{0, 0, 0, 0};
+  for (size_t i = threadIdx.x * 2; i < head; i += kThreads * 2) *reinterpret_cast<uint16_t*>(row + i) = 0;
+  for (size_t i = head + body * 16 + threadIdx.x * 2; i < bytes; i += kThreads * 2) *reinterpret_cast<uint16_t*>(row + i) = 0;
+}
+
 constexpr int kListThreads = 1024, kListRounds = 8;
 
-// One workgroup.  A token's row is the number of those before it: counted in the lanes before its own, the wavefronts before its own, and
-// the rounds before its own, 8 x 1024 tokens at a time.
-template <class ID>
-__global__ void __launch_bounds__(kListThreads) list_kernel(const ID* ids, int tokens, long long first, long long rows, const float* lse, const float* dloss, List list) {
+// The rows' ends that the products need beside the list, of the table and of the hidden states (none where out is NULL).
+struct EndsArgs {
+  PackArgs of[2];
+  unsigned groups;     // of the first, kListThreads / 8 rows each
+};
+
+// One workgroup makes the list.  A token's row is the number of those before it: counted in the lanes before its own, the wavefronts before its own, and
+// the rounds before its own, 8 x 1024 tokens at a time.  The others copy the rows' ends meanwhile.
+template <class ID, int DT>
+__global__ void __launch_bounds__(kListThreads) list_kernel(const ID* ids, int tokens, long long first, long long rows, const float* lse, const float* dloss, List list,
+                                                            EndsArgs ends) {
+  if (blockIdx.x > 0) {
+    const unsigned group = blockIdx.x - 1;
+    const PackArgs& a = ends.of[group < ends.groups ? 0 : 1];
+    pack_ends<DT>(a, (size_t)(group < ends.groups ? group : group - ends.groups) * (kListThreads / 8), a.rows);
+    return;
+  }
   __shared__ int counts[kListRounds * 16 + 1];
   __shared__ float greatest[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid / 64;
@@ -113,68 +188,6 @@ __global__ void __launch_bounds__(kListThreads) list_kernel(const ID* ids, int t
 
 // ---- rows where the products can read them -----------------------------------------------
 
-constexpr int kThreads = 256;
-
-// A copy of rows of `cols` values whose rows start at multiples of 128 bytes and end in zeros.  Row r of the copy is row token_of[r] of `in`, or of
-// zeros where that is negative; without a list row r, of `rows`.
-struct PackArgs {
-  const char* in;
-  size_t stride;        // bytes
-  const int* token_of;
-  size_t rows;          // of `in`, without a list
-  char* out;
-  size_t out_stride;    // bytes, a multiple of 128
-  int cols;
-};
-
-// Of row r of the copy, 16 bytes at `at`.
-template <int DT>
-__device__ __forceinline__ void pack_piece(const PackArgs& a, size_t r, long long source, uint32_t at) {
-  constexpr int kN = kVec<DT>;
-  Raw<DT> raw;
-  const int valid = source < 0 ? 0 : a.cols - (int)(at / kBytes<DT>);
-  const char* in = a.in + (source < 0 ? 0 : (size_t)source) * a.stride;
-  if (valid >= kN) {
-    raw.load(in, at);
-  } else {
-#pragma unroll
-    for (int i = 0; i < raw.kWords; ++i) raw.w[i] = 0;
-    if (valid > 0) raw.load(in, at, valid);
-  }
-  raw.store(a.out + r * a.out_stride, at);
-}
-__device__ __forceinline__ long long source_of(const PackArgs& a, size_t r) { return a.token_of ? (long long)a.token_of[r] : r < a.rows ? (long long)r : -1; }
-
-template <int DT>
-__device__ __forceinline__ void pack_row(const PackArgs& a, size_t r) {
-  const long long source = source_of(a, r);
-  for (uint32_t at = threadIdx.x * 16; at < a.out_stride; at += kThreads * 16) pack_piece<DT>(a, r, source, at);
-}
-
-// The same of rows of one step each (a row's ends): eight lanes a row.
-template <int DT>
-__global__ void __launch_bounds__(kThreads) pack_ends_kernel(PackArgs a, size_t rows) {
-  const size_t r = ((size_t)blockIdx.x * kThreads + threadIdx.x) / 8;
-  if (r < rows) pack_piece<DT>(a, r, source_of(a, r), threadIdx.x % 8 * 16);
-}
-
-template <int DT>
-__global__ void __launch_bounds__(kThreads) pack_kernel(PackArgs a, size_t from) {
-  pack_row<DT>(a, from + blockIdx.x);
-}
-
-__device__ __forceinline__ void zero_row(char* row, size_t bytes) {
-  const size_t head = (16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15;
-  if (bytes <= head) {
-    for (size_t i = threadIdx.x * 2; i < bytes; i += kThreads * 2) *reinterpret_cast<uint16_t*>(row + i) = 0;
-    return;
-  }
-  const size_t body = (bytes - head) / 16;
-  for (size_t i = threadIdx.x; i < body; i += kThreads) reinterpret_cast<i32x4*>(row + head)[i] = i32x4{0, 0, 0, 0};
-  for (size_t i = threadIdx.x * 2; i < head; i += kThreads * 2) *reinterpret_cast<uint16_t*>(row + i) = 0;
-  for (size_t i = head + body * 16 + threadIdx.x * 2; i < bytes; i += kThreads * 2) *reinterpret_cast<uint16_t*>(row + i) = 0;
-}
-
 // The rows with a label, packed; and zeros for the gradients of the hidden states of tokens without one.
 template <int DT>
 __global__ void __launch_bounds__(kThreads) pack_hidden_kernel(PackArgs a, size_t from, const int* row_of, size_t tokens, char* dhidden, size_t dhidden_stride) {
@@ -239,7 +252,8 @@ __device__ __forceinline__ void logits_of_tiles(const ARGS& a, int there, const 
   products<Both>(
       Tiles(a.nx, (there + S::BY - 1) / S::BY), a.steps, a.table_ends.at != nullptr, [&](Both& both, int tx, int ty) { both.start(a.table, a.hidden, tx, ty); },
       [&](Both& both, int tx, int ty) {
-        both.start(Matrix{a.table_ends.at, a.table_ends.bytes, a.table_ends.stride, nullptr}, Matrix{a.hidden_ends.at, a.hidden_ends.bytes, a.hidden_ends.stride, nullptr},
+        both.start(Matrix{a.table_ends.at, a.table_ends.bytes, a.table_ends.stride, nullptr},
+                   Matrix{a.hidden_ends.at, a.hidden_ends.bytes, a.hidden_ends.stride, a.hidden_ends.places},
                    tx, ty);
       },
       use);
@@ -709,8 +723,8 @@ Plan plan_with(const struct ze_form& f, bool backward, size_t piece, bool pack_h
   for (int i = 0; i < 7; ++i) p.list[i] = places.take(p.padded * 4);
   p.packed_hidden = places.take(backward || pack_hidden ? p.padded * p.cols_padded * p.e : 0);
   p.packed_table = places.take(pack_table ? p.piece * p.cols_padded * p.e : 0);
-  p.table_ends = places.take(p.ends && !pack_table ? p.piece * kStepBytes : 0);
-  p.hidden_ends = places.take(p.ends && !backward && !pack_hidden ? p.padded * kStepBytes : 0);
+  p.table_ends = places.take(p.ends ? f.rows * kStepBytes : 0);
+  p.hidden_ends = places.take(p.ends && !backward && !pack_hidden ? f.tokens * kStepBytes : 0);
   if (!backward) {
     const size_t part = kSizes[p.shape].part;
     p.parts = p.piece ? parts(f.rows, p.piece) * parts(up(p.piece, 256), part) : 0;
@@ -741,7 +755,7 @@ Plan plan_with(const struct ze_form& f, bool backward, size_t piece, bool pack_h
 Plan plan_for(const struct ze_form& f, bool backward, size_t piece, const void* d_hidden, const void* d_table) {
   const size_t e = dtype_bytes(f.dtype), stride = stride_of(f.stride_tokens, f.cols) * e;
   // a list of rows tells places apart by 32 bits
-  const bool pack_hidden = !d_hidden || !readable(d_hidden, stride) || f.tokens * stride > 0xF0000000u;
+  const bool pack_hidden = !d_hidden || !readable(d_hidden, stride) || f.tokens * (stride > kStepBytes ? stride : kStepBytes) > 0xF0000000u;
   return plan_with(f, backward, piece, pack_hidden, !d_table || !readable(d_table, stride_of(f.stride_table, f.cols) * e));
 }
 size_t work_bytes_for(const struct ze_form& f, bool backward, size_t piece, const void* d_hidden, const void* d_table) {
@@ -766,13 +780,15 @@ List list_in(const Plan& p, char* work, bool backward) {
   return l;
 }
 
-void launch_list(const struct ze_form& f, const void* d_labels, const float* d_lse, const float* d_dloss, const List& list, hipStream_t s) {
+template <int DT>
+void launch_list(const struct ze_form& f, const void* d_labels, const float* d_lse, const float* d_dloss, const List& list, const EndsArgs& ends, hipStream_t s) {
+  const unsigned groups = 1 + ends.groups + (ends.of[1].out ? (unsigned)parts(ends.of[1].rows, kListThreads / 8) : 0);
   if (f.id_dtype == ZE_I64)
-    hipLaunchKernelGGL(list_kernel<long long>, dim3(1), dim3(kListThreads), 0, s, static_cast<const long long*>(d_labels), (int)f.tokens, f.first, (long long)f.rows,
-                       d_lse, d_dloss, list);
+    hipLaunchKernelGGL((list_kernel<long long, DT>), dim3(groups), dim3(kListThreads), 0, s, static_cast<const long long*>(d_labels), (int)f.tokens, f.first,
+                       (long long)f.rows, d_lse, d_dloss, list, ends);
   else
-    hipLaunchKernelGGL(list_kernel<int>, dim3(1), dim3(kListThreads), 0, s, static_cast<const int*>(d_labels), (int)f.tokens, f.first, (long long)f.rows, d_lse,
-                       d_dloss, list);
+    hipLaunchKernelGGL((list_kernel<int, DT>), dim3(groups), dim3(kListThreads), 0, s, static_cast<const int*>(d_labels), (int)f.tokens, f.first, (long long)f.rows,
+                       d_lse, d_dloss, list, ends);
 }
 
 constexpr size_t kMostGroups = (size_t)1 << 23;   // of one launch: a grid has fewer than 2^32 lanes
@@ -800,21 +816,27 @@ Matrix table_piece(const struct ze_form& f, const Plan& p, const void* d_table, 
   return m;
 }
 
-// The ends of `rows` rows, where they are apart.
-template <int DT>
-Ends ends_of(const Plan& p, const char* at, size_t stride, const int* token_of, size_t rows, size_t cols, char* out, hipStream_t s) {
-  if (!p.ends) return Ends{nullptr, 0, 0};
-  const size_t skip = (size_t)p.steps * kStep<DT>;
-  PackArgs a = {at + skip * kBytes<DT>, stride, token_of, rows, out, kStepBytes, (int)(cols - skip)};
-  hipLaunchKernelGGL(pack_ends_kernel<DT>, dim3((unsigned)parts(rows * 8, kThreads)), dim3(kThreads), 0, s, a, rows);
-  return Ends{out, rows * kStepBytes, kStepBytes};
+// The copies of rows' ends that a call makes.
+EndsArgs ends_to_copy(const struct ze_form& f, const Plan& p, const void* d_hidden, const void* d_table, char* work, bool hidden) {
+  EndsArgs a = {};
+  if (!p.ends || f.rows == 0) return a;
+  const size_t skip = (size_t)p.steps * kStepBytes;
+  const int cols = (int)(f.cols - skip / p.e);
+  a.of[0] = PackArgs{static_cast<const char*>(d_table) + skip, p.stride_table, nullptr, f.rows, work + p.table_ends, kStepBytes, cols};
+  a.groups = (unsigned)parts(f.rows, kListThreads / 8);
+  if (hidden) a.of[1] = PackArgs{static_cast<const char*>(d_hidden) + skip, p.stride_hidden, nullptr, f.tokens, work + p.hidden_ends, kStepBytes, cols};
+  return a;
 }
-
+// Those of the table's rows from v0 on.
+Ends table_ends(const Plan& p, size_t v0, size_t count, const char* work) {
+  if (!p.ends) return Ends{nullptr, 0, 0, nullptr};
+  return Ends{work + p.table_ends + v0 * kStepBytes, count * kStepBytes, kStepBytes, nullptr};
+}
 // Those of rows that have been copied, ends and all.
 Ends ends_in(const Plan& p, const Matrix& m) {
-  if (!p.ends) return Ends{nullptr, 0, 0};
+  if (!p.ends) return Ends{nullptr, 0, 0, nullptr};
   const size_t skip = (size_t)p.steps * kStepBytes;
-  return Ends{m.at + skip, m.bytes - skip, m.stride};
+  return Ends{m.at + skip, m.bytes - skip, m.stride, nullptr};
 }
 
 template <int DT>
@@ -837,14 +859,14 @@ void forward(const struct ze_form& f, const Plan& p, const void* d_hidden, const
       a.hidden_ends = ends_in(p, a.hidden);
     } else {
       a.hidden = Matrix{static_cast<const char*>(d_hidden), up((f.tokens - 1) * p.stride_hidden + f.cols * p.e, 4), p.stride_hidden, list.token_of};
-      a.hidden_ends = ends_of<DT>(p, static_cast<const char*>(d_hidden), p.stride_hidden, list.token_of, p.padded, f.cols, work + p.hidden_ends, s);
+      a.hidden_ends = Ends{p.ends ? work + p.hidden_ends : nullptr, f.tokens * kStepBytes, kStepBytes, list.token_of};
     }
   }
   size_t part = 0;
   for (size_t v0 = 0; v0 < f.rows; v0 += p.piece) {
     const size_t count = f.rows - v0 < p.piece ? f.rows - v0 : p.piece;
     a.table = table_piece<DT>(f, p, d_table, v0, count, work, s);
-    a.table_ends = p.pack_table ? ends_in(p, a.table) : ends_of<DT>(p, a.table.at, a.table.stride, nullptr, count, f.cols, work + p.table_ends, s);
+    a.table_ends = table_ends(p, v0, count, work);
     a.v0 = (int)v0;
     a.rows = (int)count;
     a.parts = reinterpret_cast<Part*>(work + p.part) + part;
@@ -881,7 +903,7 @@ void backward(const struct ze_form& f, const Plan& p, const void* d_hidden, cons
     GradientArgs g;
     g.table = table;
     g.hidden = hidden;
-    g.table_ends = p.pack_table ? ends_in(p, table) : ends_of<DT>(p, table.at, table.stride, nullptr, count, f.cols, work + p.table_ends, s);
+    g.table_ends = table_ends(p, v0, count, work);
     g.hidden_ends = ends_in(p, hidden);
     g.head = list.head;
     g.label_of = list.label_of;
@@ -986,8 +1008,12 @@ int ze_vocab_loss(const struct ze_form* form, const void* d_hidden, const void* 
   const hipStream_t s = static_cast<hipStream_t>(stream);
   char* const work = static_cast<char*>(d_work);
   const List list = list_in(p, work, false);
-  launch_list(*form, d_labels, nullptr, nullptr, list, s);
-#define CALL(DT) forward<DT>(*form, p, d_hidden, d_table, list, work, d_stats, s)
+  const EndsArgs ends = ends_to_copy(*form, p, d_hidden, d_table, work, !p.pack_hidden);
+#define CALL(DT)                                                             \
+  do {                                                                       \
+    launch_list<DT>(*form, d_labels, nullptr, nullptr, list, ends, s);       \
+    forward<DT>(*form, p, d_hidden, d_table, list, work, d_stats, s);        \
+  } while (0)
   ZE_BY_TYPE(form->dtype, CALL);
 #undef CALL
   return finish_launch();
@@ -1034,8 +1060,12 @@ int ze_vocab_loss_backward(const struct ze_form* form, const void* d_hidden, con
   if (work_bytes < p.bytes) return ZC_ERR_CAPACITY;
   char* const work = static_cast<char*>(d_work);
   const List list = list_in(p, work, true);
-  launch_list(*form, d_labels, d_lse, d_dloss, list, s);
-#define CALL(DT) backward<DT>(*form, p, d_hidden, d_table, list, work, d_dhidden, d_dtable, s)
+  const EndsArgs ends = ends_to_copy(*form, p, d_hidden, d_table, work, false);
+#define CALL(DT)                                                                           \
+  do {                                                                                     \
+    launch_list<DT>(*form, d_labels, d_lse, d_dloss, list, ends, s);                       \
+    backward<DT>(*form, p, d_hidden, d_table, list, work, d_dhidden, d_dtable, s);         \
+  } while (0)
   ZE_BY_TYPE(form->dtype, CALL);
 #undef CALL
   return finish_launch();

@@ -25,9 +25,10 @@ template <int DT> constexpr int kStep = kStepBytes / kBytes<DT>;   // values of 
 
 enum Lies { kAlong, kAcross };
 
-// Sums of 16 x 16 products over half a step: 32 half-precision values of k in one instruction, 16 fp32 values in four.
+// Sums of 16 x 16 products over half a step: 32 half-precision values of k in one instruction, 16 fp32 values in four, of which this is one.
+template <int DT> constexpr int kInstructions = DT == kF32 ? 4 : 1;
 template <int DT>
-__device__ __forceinline__ f32x4 multiply(i32x4 x, i32x4 y, f32x4 sum) {
+__device__ __forceinline__ f32x4 multiply(i32x4 x, i32x4 y, int part, f32x4 sum) {
   if constexpr (DT == kBF16) {
     typedef __bf16 v8 __attribute__((ext_vector_type(8)));
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, x), __builtin_bit_cast(v8, y), sum, 0, 0, 0);
@@ -35,10 +36,7 @@ __device__ __forceinline__ f32x4 multiply(i32x4 x, i32x4 y, f32x4 sum) {
     typedef _Float16 v8 __attribute__((ext_vector_type(8)));
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, x), __builtin_bit_cast(v8, y), sum, 0, 0, 0);
   } else {
-    const f32x4 fx = __builtin_bit_cast(f32x4, x), fy = __builtin_bit_cast(f32x4, y);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(fx[j], fy[j], sum, 0, 0, 0);
-    return sum;
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(f32x4, x)[part], __builtin_bit_cast(f32x4, y)[part], sum, 0, 0, 0);
   }
 }
 
@@ -53,6 +51,7 @@ struct Matrix {
 struct Ends {
   const char* at;
   size_t bytes, stride;
+  const int* places;
 };
 
 constexpr uint32_t kNowhere = 0xFFFFFF00u;   // behind the end of every buffer
@@ -67,8 +66,7 @@ struct Operand {
   static constexpr int kE = kBytes<DT>, kTileBytes = SIZE * kStepBytes, kLoads = kTileBytes / (THREADS * 16), kRow = SIZE * kE;
   static_assert(kLoads * THREADS * 16 == kTileBytes, "whole loads");
   static constexpr int kParts = SIZE / 16 < 8 ? SIZE / 16 : 8;   // kAcross, half precision: 16 values of a row, places that are exchanged
-  static constexpr int kAddresses = LIES == kAlong ? 2 : DT == kF32 ? 4 : kParts;
-  static_assert(LIES == kAlong || DT != kF32 || SIZE >= 64, "exchanged places");
+  static constexpr int kAddresses = LIES == kAlong ? 2 : DT == kF32 && kParts > 4 ? 4 : kParts;
 
   uint32_t from[kLoads];   // bytes from the tile's start
   const char* at;          // the tile's start, at the present step
@@ -77,7 +75,7 @@ struct Operand {
 
   static __device__ __forceinline__ int swap_along(int row) { return (row >> 1) & 7; }
   static __device__ __forceinline__ int swap_across(int k) {
-    if constexpr (DT == kF32) return (k >> 2) & 3;
+    if constexpr (DT == kF32) return (k >> 2) & 3 & (SIZE / 16 - 1);
     else return ((k & 3) | ((k >> 3) & 3) << 2) & (SIZE / 16 - 1);
   }
 
@@ -373,11 +371,13 @@ __device__ __forceinline__ void products(const Tiles& tiles, int steps, bool has
 #pragma unroll
       for (int j = 0; j < S::NY; ++j) y[h][j] = both.read_y(tile, j, h);
     };
-    const auto add = [&](int h) {
+    const auto add = [&](int h) {   // (a sum's next product does not follow at once, where there are others)
 #pragma unroll
-      for (int j = 0; j < S::NY; ++j)
+      for (int part = 0; part < kInstructions<DT>; ++part)
 #pragma unroll
-        for (int i = 0; i < S::NX; ++i) sum[i][j] = multiply<DT>(x[h][i], y[h][j], sum[i][j]);
+        for (int j = 0; j < S::NY; ++j)
+#pragma unroll
+          for (int i = 0; i < S::NX; ++i) sum[i][j] = multiply<DT>(x[h][i], y[h][j], part, sum[i][j]);
     };
 
     if (has_ends) {
