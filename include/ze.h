@@ -40,7 +40,7 @@ enum { ZE_MAX_TOKENS = 1 << 25, ZE_MAX_ROWS = 1 << 28, ZE_MAX_COLS = 65536 };
  * `cols` values.  A stride is the number of elements from one row to the next, 0 for cols. */
 struct ze_form {
   size_t tokens, rows, cols;
-  long long first;                       /* >= 0: the id of the table's first row */
+  long long first;                       /* the id of the table's first row: from 0 to 2^63 - 1 - ZE_MAX_ROWS */
   int dtype;                             /* enum zc_dtype: of the table and of the tokens' rows */
   int grad_dtype;                        /* of ze_embedding_backward's d_dtable: dtype or ZC_F32; the others do not read it */
   int id_dtype;                          /* enum ze_id_dtype */
@@ -72,9 +72,9 @@ int ze_embedding_backward(const struct ze_form* form, const void* d_ids, const v
  * without rows), the sum of exp(l - m), and the label's logit (-inf where the label is not one of this rank's). A
  * token without a label gets -inf, 0, 0.  A logit of +inf counts as not a number.
  *
- * How much workspace a call needs depends on whether d_hidden and d_table can be read as they are (rows that start at multiples of 4 bytes)
- * or have to be copied; ze_loss_work_bytes and ze_loss_backward_work_bytes look at the pointers'
- * values for that, and give enough for any place where one is NULL.
+ * How much workspace a call needs depends on whether d_hidden and d_table can be read as they are (rows that start at multiples of 4 bytes; the
+ * table's, that do not overlap) or have to be copied; ze_loss_work_bytes and ze_loss_backward_work_bytes look at the pointers'
+ * values for that, and give enough for any place where one is NULL.  The forward call keeps 8 bytes for each token and 16 to 128 rows.
  */
 size_t ze_loss_work_bytes(const struct ze_form* form, const void* d_hidden, const void* d_table);
 int ze_vocab_loss(const struct ze_form* form, const void* d_hidden, const void* d_table, const void* d_labels, float* d_stats,

@@ -2,6 +2,7 @@
 #ifndef ZE_COMMON_H
 #define ZE_COMMON_H
 
+#include <limits.h>
 #include <math.h>
 
 #include "../../include/ze.h"
@@ -23,7 +24,7 @@ __device__ __forceinline__ uint32_t sum_up_to(uint32_t v) {
   return dpp_count<0x143, 0xC>(v);
 }
 
-// Which of this rank's rows an id names, of `rows` from `first` on, or -1.
+// Which of this rank's rows an id names, of `rows` from `first` on, or -1.  (first is at most 2^63 - 1 - ZE_MAX_ROWS: then the least of ids is no row either.)
 __device__ __forceinline__ long long row_of_id(long long id, long long first, long long rows) {
   const unsigned long long at = (unsigned long long)id - (unsigned long long)first;   // (below `first`, and negative: more than any number of rows)
   return at < (unsigned long long)rows ? (long long)at : -1;
@@ -37,7 +38,7 @@ size_t parts(size_t n, size_t of) { return (n + of - 1) / of; }
 int check_form(const struct ze_form* f) {
   if (!f) return ZC_ERR_NULL;
   if (!known_dtype(f->dtype)) return ZC_ERR_DTYPE;
-  if ((f->id_dtype != ZE_I32 && f->id_dtype != ZE_I64) || f->first < 0 || !isfinite(f->scale)) return ZC_ERR_ARG;
+  if ((f->id_dtype != ZE_I32 && f->id_dtype != ZE_I64) || f->first < 0 || f->first > LLONG_MAX - ZE_MAX_ROWS || !isfinite(f->scale)) return ZC_ERR_ARG;
   if (f->tokens > ZE_MAX_TOKENS || f->rows > ZE_MAX_ROWS || f->cols > ZE_MAX_COLS) return ZC_ERR_SIZE;
   if (f->stride_table > kMaxStride || f->stride_tokens > kMaxStride) return ZC_ERR_ARG;
   return ZC_OK;

@@ -756,7 +756,9 @@ Plan plan_for(const struct ze_form& f, bool backward, size_t piece, const void* 
   const size_t e = dtype_bytes(f.dtype), stride = stride_of(f.stride_tokens, f.cols) * e;
   // a list of rows tells places apart by 32 bits
   const bool pack_hidden = !d_hidden || !readable(d_hidden, stride) || f.tokens * (stride > kStepBytes ? stride : kStepBytes) > 0xF0000000u;
-  return plan_with(f, backward, piece, pack_hidden, !d_table || !readable(d_table, stride_of(f.stride_table, f.cols) * e));
+  // Rows that overlap reach behind the piece's last row, where the products over it count on zeros.
+  const size_t apart = stride_of(f.stride_table, f.cols);
+  return plan_with(f, backward, piece, pack_hidden, !d_table || !readable(d_table, apart * e) || apart < f.cols);
 }
 size_t work_bytes_for(const struct ze_form& f, bool backward, size_t piece, const void* d_hidden, const void* d_table) {
   const size_t bytes = plan_for(f, backward, piece, d_hidden, d_table).bytes;

@@ -217,6 +217,8 @@ def ze_vocab_loss_backward(d_hidden, d_table, d_labels, d_lse, d_dloss, first=0,
     c, hidden, table = _loss_call(d_hidden, d_table, d_labels, first, scale)
     if (d_dhidden is not None and not want_hidden) or (d_dtable is not None and not want_table):
         raise ValueError("an output that is not wanted")
+    if piece < 0:
+        raise ValueError("piece must not be negative")
     if d_dhidden is None and want_hidden:
         d_dhidden = c.empty(d_hidden.shape, c.dtype, stream)
     if d_dtable is None and want_table:

@@ -289,3 +289,24 @@ def test_nothing_to_do():
     assert (dh == 0).all() and (dw == 0).all()
     stats = ze.ze_vocab_loss(hidden.view(3, 1, 32), table, labels.view(3, 1))
     assert ze.ze_join_loss(stats, labels.view(3, 1))[0].shape == (3, 1)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+def test_rows_of_the_matrix_that_overlap(dtype):
+    """An input's rows may overlap.  -inf where the last row alone has it, and the rows behind it would, were there any: the columns in which they would
+    stay finite."""
+    t, cols, stride = TYPES[dtype], 128, 64
+    for rows in (65, 301):
+        hidden, _, labels, dloss = _inputs(70, rows, cols, t, 71)
+        flat = (torch.randn((rows - 1) * stride + cols, generator=torch.Generator(device="cuda").manual_seed(72), device="cuda") / 8).to(t)
+        flat[-1] = -INF
+        hidden[:, -1] = 1.0          # the last row's logits are -inf, and no token's label
+        labels[labels == rows - 1] = 0
+        table = flat.as_strided((rows, cols), (stride, 1))
+        clean = table.clone()
+        stats = ze.ze_vocab_loss(hidden, table, labels)
+        assert torch.equal(stats, ze.ze_vocab_loss(hidden, clean, labels))
+        lse = ze.ze_join_loss(stats, labels)[1]
+        got, want = (ze.ze_vocab_loss_backward(hidden, m, labels, lse, dloss) for m in (table, clean))
+        assert torch.equal(got[1], want[1]) and got[0][:, :-1].isfinite().all()
+        assert torch.equal(got[0][:, :-1], want[0][:, :-1])

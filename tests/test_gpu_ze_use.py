@@ -231,6 +231,7 @@ def test_refusals_of_the_binding():
             (lambda: ze.ze_vocab_loss(h[:, :0], w[:, :0], ids), zc.ZcError),
             (lambda: ze.ze_join_loss(torch.zeros((2, 4), device="cuda"), ids), ValueError), (lambda: ze.ze_join_loss(torch.zeros((0, 3, 4), device="cuda"), ids), zc.ZcError),
             (lambda: ze.ze_vocab_loss_backward(h, w, ids, f, f[:3]), ValueError), (lambda: ze.ze_vocab_loss_backward(h, w, ids, f, f.double()), TypeError),
+            (lambda: ze.ze_vocab_loss_backward(h, w, ids, f, f, piece=-1), ValueError),
             (lambda: ze.ze_vocab_loss_backward(h, w, ids, f, f, d_dtable=w, want_table=False), ValueError)):
         with pytest.raises(error):
             call()

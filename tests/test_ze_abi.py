@@ -170,3 +170,19 @@ def test_binding_rejects_host_tensors_and_wrong_combinations():
             call()
     with pytest.raises(ValueError):
         ze.ze_embedding_backward(ids, t, 3, accumulate=True)
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_ids_do_not_wrap_around(call):
+    """A table whose rows reach the greatest id: the least of ids would be counted among them."""
+    most = (1 << 63) - 1 - ze.ZE_MAX_ROWS
+    assert call(_form(first=most + 1)) == call(_form(first=(1 << 63) - 1)) == ze.ZC_ERR_ARG
+    assert call(_form(first=most), **{"out" if call is lookup else "dtable" if call is lookup_back else "labels": None}) == zc.ZC_ERR_NULL
+
+
+def test_rows_that_overlap_are_copied():
+    """The products over a piece's rows count on zeros behind the last one, where a row that is longer than the stride still has values."""
+    L = ze.lib()
+    for backward in (False, True):
+        size = (lambda f: L.ze_loss_backward_work_bytes(f, GOOD, GOOD, 0)) if backward else lambda f: L.ze_loss_work_bytes(f, GOOD, GOOD)
+        assert size(_form(rows=65, stride_table=32)) > size(_form(rows=65)) == size(_form(rows=65, stride_table=96))
