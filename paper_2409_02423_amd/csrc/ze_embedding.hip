@@ -3,7 +3,10 @@
 // The gradient is a sum over the tokens that have a row, in the order of the tokens.  They are sorted by row (a stable counting sort, eight bits of the
 // row's number at a time), the sorted list is cut into pieces of the same length, and each wavefront adds up one piece, for 64 vectors of the
 // columns: a row whose tokens lie within a piece is done, parts of rows that go on are kept and joined by a second kernel.  So a token that half of the batch has
-// takes no longer than others, there are no atomics, and the sums' order depends on the ids alone.
+// takes no longer than others, there are no sums by atomics, and their order depends on the ids alone.
+//
+// Memory bounds both on large tensors, the chain of launches the gradient of small ones.  8192 tokens on one of four ranks, 12608 rows of 6144
+// bf16 values: lookup 23.8 us at 4.9 TB/s, of which six sevenths are written; fp32 gradient 11.9 (sort) + 62.6 (sums and zeros, 5.4 TB/s) + 5.8 (joins).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -29,6 +32,9 @@ struct LookupArgs {
 };
 
 constexpr int kLookupSteps = 4;   // vectors of a lane
+
+// A row's lanes ask for all that they have of it before they use any.  Ids come from the same few cache lines for all workgroups of a token, rows that are not this
+// rank's cost their stores alone.
 
 template <int DT, class ID>
 __global__ void __launch_bounds__(kThreads) lookup_kernel(LookupArgs a) {
@@ -168,7 +174,7 @@ __device__ __forceinline__ void name_none(const SortArgs& a, uint32_t thread, ui
 
 // Up to one tile: one workgroup takes all passes in LDS.  The tokens that have a row are brought together first (on one of four ranks they are
 // a quarter), so that the rest costs what they cost.  What bounds it is the chain of steps that wait for one another.  8192 tokens of which a quarter has a
-// row, 14 bits in two passes: SORT_FULL; 512 tokens, 10 bits in two passes: SORT_SMALL.
+// row, 14 bits in two passes: 11.9 us; 512 tokens, 10 bits in two passes: 4.1 us.
 template <class ID, int ITEMS>
 __global__ void __launch_bounds__(kSortThreads) sort_kernel(SortArgs a) {
   __shared__ uint32_t keys[kSortThreads * ITEMS], counts[kCounts], buffer[kWaves];
@@ -394,7 +400,7 @@ __device__ __forceinline__ void keep(float* to, const float (&v)[N]) {
   for (int i = 0; i < N; i += 4) *reinterpret_cast<f4*>(to + i) = f4{v[i], v[i + 1], v[i + 2], v[i + 3]};
 }
 
-// One piece of the sorted list, in 64 vectors of the columns.  A run of tokens with the same row that begins and ends in the piece is stored; the part of one that
+// One piece of the sorted list, in 64 vectors of the columns (wavefronts beside one another take those beside one another, of the same tokens).  A run of tokens with the same row that begins and ends in the piece is stored; the part of one that
 // comes from the piece before is kept as the piece's first, that of one which goes on (and began here) as its second.  What is read of eight tokens is
 // asked for at once: their rows, and with `accumulate` the gradient's rows that are done among them.
 template <int DT, int DO>
@@ -477,7 +483,7 @@ __global__ void __launch_bounds__(kThreads) sum_kernel(SumArgs a) {
   }
 }
 
-// The rows whose tokens do not lie within a piece: the sums that were kept of them, from the piece that they begin in.
+// The rows whose tokens do not lie within a piece (few, where ids are many: the launch is most of the time, 3.3 to 5.8 us): the sums that were kept of them, from the piece that they begin in.
 template <int DT, int DO>
 __device__ __forceinline__ void join_from(const SumArgs& a, uint32_t piece, int vector) {
   constexpr int kN = kVec<DT>, kAhead = 8;
@@ -543,7 +549,8 @@ Plan plan_for(const struct ze_form& f) {
   while (f.rows >> bits) ++bits;   // of keys up to `rows`
   p.passes = (bits + kDigitBits - 1) / kDigitBits;
   p.bits = (bits + p.passes - 1) / p.passes;
-  // Short pieces where there are few of them, so that none waits for a second load; else longer ones, which keep less.
+  // Short pieces where there are few of them, so that none waits for a second load; else longer ones, which keep less.  In turn, sums + joins in us: 512
+  // tokens of 256 fp32 values, pieces of 8 5.3 + 3.3, of 16 7.5 + 3.3; 8192 tokens of 6144 bf16 values, 8 71.4 + 9.6, 16 67.7 + 6.2.
   p.piece = parts(f.tokens, 16) * parts((size_t)p.vectors, 64) <= 2048 ? 8 : f.tokens <= 16384 ? 16 : f.tokens <= 65536 ? 32 : kMostPiece;
   p.pieces = (uint32_t)parts(f.tokens, (size_t)p.piece);
   Places places;
