@@ -71,6 +71,19 @@ def test_large_tiles(tokens, rows, cols, dtype):
         _close(a, b, c)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("tokens, rows, cols", [(4096, 4200, 40), (4100, 4096, 64), (2300, 9000, 130), (4096, 4500, 192), (2048, 5000, 254)])
+def test_large_tiles_of_short_rows(tokens, rows, cols, dtype):
+    """No whole step, one, two with an end, three, and three with one."""
+    hidden, table, labels, dloss = _inputs(tokens, rows, cols, TYPES[dtype], 6, absent=0.4)
+    stats = ze.ze_vocab_loss(hidden, table, labels)
+    _check_stats(stats, hidden, table, labels, 0, 1.0)
+    lse = ze.ze_join_loss(stats, labels)[1]
+    got = ze.ze_vocab_loss_backward(hidden, table, labels, lse, dloss)
+    for a, b, c in zip(got, *ze_ref.vocab_loss_backward(hidden, table, labels, lse, dloss)):
+        _close(a, b, c)
+
+
 @pytest.mark.parametrize("dtype", sorted(TYPES))
 @pytest.mark.parametrize("tokens, rows, cols, piece", [(70, 1000, 136, 256), (70, 1000, 136, 1), (70, 1000, 136, 999), (70, 1000, 136, 1 << 40), (5, 2600, 64, 512),
                                                       (300, 700, 4096, 256)])
