@@ -273,12 +273,16 @@ __device__ __forceinline__ void use_logits(const LogitsArgs& a, int there, f32x4
   const int x_wave = __builtin_amdgcn_readfirstlane(tx * S::BX + wx * (S::BX / S::WX));
   const bool edge = x_wave + S::BX / S::WX > a.rows;
   const int x0 = tx * S::BX + wx * (S::BX / S::WX) + lane / 16 * 4, y0 = ty * S::BY + wy * (S::BY / S::WY) + (lane & 15);
+  int labels[S::NY];   // asked for at once (there are places for whole tiles of rows)
+#pragma unroll
+  for (int j = 0; j < S::NY; ++j) labels[j] = a.label_of[y0 + 16 * j];
+  have_come(labels);
 #pragma unroll
   for (int j = 0; j < S::NY; ++j) {
     rest_of_sums<S>(sum, j);
     const int y = y0 + 16 * j;
     if (y >= there) continue;
-    const int label = a.label_of[y] - a.v0;
+    const int label = labels[j] - a.v0;
     f32x4 l[S::NX];
 #pragma unroll
     for (int i = 0; i < S::NX; ++i) l[i] = a.scale * sum[i][j];
@@ -422,13 +426,24 @@ __device__ __forceinline__ void use_gradient(const GradientArgs& a, int there, f
   const int x_wave = __builtin_amdgcn_readfirstlane(tx * S::BX + wx * (S::BX / S::WX));
   const bool edge = x_wave + S::BX / S::WX > a.rows || (ty + 1) * S::BY > there;
   const int x0 = tx * S::BX + wx * (S::BX / S::WX) + lane / 16 * 4, y0 = ty * S::BY + wy * (S::BY / S::WY) + (lane & 15);
+  int labels[S::NY];   // asked for at once (there are places for whole tiles of rows)
+  float of_lse[S::NY], of_dloss[S::NY];
+#pragma unroll
+  for (int j = 0; j < S::NY; ++j) {
+    labels[j] = a.label_of[y0 + 16 * j];
+    of_lse[j] = a.lse[y0 + 16 * j];
+    of_dloss[j] = a.dloss[y0 + 16 * j];
+  }
+  have_come(labels);
+  have_come(of_lse);
+  have_come(of_dloss);
 #pragma unroll
   for (int j = 0; j < S::NY; ++j) {
     rest_of_sums<S>(sum, j);
     const int y = y0 + 16 * j;
     if (y >= padded) continue;
-    const int label = a.label_of[y] - a.v0;
-    const float lse = a.lse[y], factor = most > 0.0f ? a.dloss[y] / most * kLift<DT> : a.dloss[y];
+    const int label = labels[j] - a.v0;
+    const float lse = of_lse[j], factor = most > 0.0f ? of_dloss[j] / most * kLift<DT> : of_dloss[j];
     char* const row = a.g + (size_t)y * a.g_stride;
     const bool has = any_lane((unsigned)(label - x_wave) < (unsigned)(S::BX / S::WX));   // few parts of rows have a label
 #pragma unroll
@@ -520,12 +535,16 @@ template <int DT, class S>
 __device__ __forceinline__ void use_hidden_gradient(const OutArgs& a, int there, int ny, int split, bool finish, float factor, f32x4 (&sum)[S::NX][S::NY], int tx, int ty) {
   const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, wx = wave % S::WX, wy = wave / S::WX;
   const int x0 = tx * S::BX + wx * (S::BX / S::WX) + lane / 16 * 4, y0 = ty * S::BY + wy * (S::BY / S::WY) + (lane & 15);
+  int tokens[S::NY];   // asked for at once (there are places for whole tiles of rows)
+#pragma unroll
+  for (int j = 0; j < S::NY; ++j) tokens[j] = a.token_of[y0 + 16 * j];
+  have_come(tokens);
 #pragma unroll
   for (int j = 0; j < S::NY; ++j) {
     rest_of_sums<S>(sum, j);
     const int y = y0 + 16 * j;
     if (y >= there) continue;
-    char* const row = finish ? a.out + (size_t)a.token_of[y] * a.out_stride : nullptr;
+    char* const row = finish ? a.out + (size_t)tokens[j] * a.out_stride : nullptr;
     float* const kept = a.kept + ((size_t)split * ny * S::BY + y) * a.kept_stride;
 #pragma unroll
     for (int i = 0; i < S::NX; i += 2) {

@@ -57,6 +57,13 @@ struct Ends {
   const int* places;
 };
 
+// Loads have come.  (Where one may stay unused the compiler waits for it wherever its register is needed next: in the steps of the next tile.)
+template <class T, int N>
+__device__ __forceinline__ void have_come(T (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
+}
+
 constexpr uint32_t kNowhere = 0xFFFFFF00u;   // behind the end of every buffer
 
 // One operand of a tile that is SIZE rows of x (or y) wide, for a workgroup of THREADS lanes.
@@ -91,14 +98,20 @@ struct Operand {
       const size_t skip = listed ? 0 : first * m.stride;
       at = m.at + skip;
       left = (long long)m.bytes - (long long)skip;
+      const int row0 = tid / 8;
+      if (listed) {
+        // (asked for at once: one after the other they took a tenth of a tile's time)
+        int place[kLoads];
 #pragma unroll
-      for (int j = 0; j < kLoads; ++j) {
-        const int row = j * (THREADS / 8) + tid / 8, piece = (tid & 7) ^ swap_along(row);
-        if (listed) {
-          const int place = m.places[first + row];
-          from[j] = place < 0 ? kNowhere : (uint32_t)place * (uint32_t)m.stride + piece * 16;
-        } else {
-          from[j] = row * (uint32_t)m.stride + piece * 16;
+        for (int j = 0; j < kLoads; ++j) place[j] = m.places[first + row0 + j * (THREADS / 8)];
+        have_come(place);
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) from[j] = place[j] < 0 ? kNowhere : (uint32_t)place[j] * (uint32_t)m.stride + ((tid & 7) ^ swap_along(row0 + j * (THREADS / 8))) * 16;
+      } else {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+          const int row = row0 + j * (THREADS / 8);
+          from[j] = row * (uint32_t)m.stride + ((tid & 7) ^ swap_along(row)) * 16;
         }
       }
       const int row = wave_first + (lane & 15);
