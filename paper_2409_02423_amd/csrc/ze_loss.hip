@@ -6,8 +6,8 @@
 // gradient and across it for the matrix's.  Tokens without a label are left out before anything else: the products work on a list of those that have
 // one, so what the others hold is not read at all.
 //
-// The products bound all of it, but for a few tokens, where reading the matrix does.  8192 tokens, 12608 rows of 6144 bf16 values: forward 986 us of
-// product (1287 TFLOP/s; a library's bare product of that size takes 957) and 16 of the rest; backward 1039 + 948 + 875 and 44.  The matrix units are 60 to 73 % busy at
+// The products bound all of it, but for a few tokens, where reading the matrix does.  8192 tokens, 12608 rows of 6144 bf16 values: forward 964 us of
+// product (1317 TFLOP/s; a library's bare product of that size takes 957) and 15 of the rest; backward 1014 + 938 + 860 and 44.  The matrix units are 60 to 73 % busy at
 // the clock that their power leaves.  Four tokens: 34.0 us, 4.6 TB/s.
 #include <hip/hip_runtime.h>
 #include <math.h>
