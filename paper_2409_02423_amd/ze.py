@@ -15,6 +15,7 @@ from .zt import ZC_ERR_ARG, _check, _current, _DTYPES, _empty, _flat, _refuse  #
 
 ZE_I32, ZE_I64 = 0, 1
 ZE_MAX_TOKENS, ZE_MAX_ROWS, ZE_MAX_COLS = 1 << 25, 1 << 28, 65536
+_MOST_FIRST = (1 << 63) - 1 - ZE_MAX_ROWS
 
 EXPORTS = ("ze_embedding", "ze_embedding_work_bytes", "ze_embedding_backward", "ze_loss_work_bytes", "ze_vocab_loss", "ze_join_loss",
            "ze_loss_backward_work_bytes", "ze_vocab_loss_backward")
@@ -61,6 +62,11 @@ class _Call:
     __slots__ = ("device", "dtype", "shape", "table_shape", "tokens_shape", "ids", "form")
 
     def __init__(self, d_ids, what, like, like_what, rows, first, scale):
+        # (what does not fit into the form's fields would be cut to their width, without an error)
+        if not 0 <= first <= _MOST_FIRST:
+            raise ZcError(ZC_ERR_ARG, "first = %d" % first)
+        if not 0 <= rows <= ZE_MAX_ROWS:
+            raise ZcError(zc.ZC_ERR_SIZE, "rows = %d" % rows)
         device = self.device = _current(like, like_what)
         dtype = self.dtype = like.dtype
         code, of = _DTYPES.get(dtype), like.shape
@@ -226,6 +232,7 @@ def ze_vocab_loss_backward(d_hidden, d_table, d_labels, d_lse, d_dloss, first=0,
     dhidden = c.tokens(d_dhidden, "d_dhidden", "dtokens") if want_hidden else None
     dtable = c.table(d_dtable, "d_dtable", "dtable") if want_table else None
     lse, dloss = c.floats(d_lse, "d_lse"), c.floats(d_dloss, "d_dloss")
+    piece = min(piece, ZE_MAX_ROWS)      # (as many rows as there can be; more would be cut to the argument's width)
     L = lib()
     size = L.ze_loss_backward_work_bytes(c.form, hidden, table, piece)
     work, at = c.work(size, stream)

@@ -323,3 +323,14 @@ def test_rows_of_the_matrix_that_overlap(dtype):
         got, want = (ze.ze_vocab_loss_backward(hidden, m, labels, lse, dloss) for m in (table, clean))
         assert torch.equal(got[1], want[1]) and got[0][:, :-1].isfinite().all()
         assert torch.equal(got[0][:, :-1], want[0][:, :-1])
+
+
+def test_pieces_of_more_rows_than_an_argument_holds():
+    """As many as there are: 2^64 + 256 is not 256, nor 2^64 the library's choice."""
+    hidden, table, labels, dloss = _inputs(70, 5000, 64, torch.float32, 8)
+    lse = ze.ze_join_loss(ze.ze_vocab_loss(hidden, table, labels), labels)[1]
+    whole = ze.ze_vocab_loss_backward(hidden, table, labels, lse, dloss, piece=5000)
+    assert not torch.equal(ze.ze_vocab_loss_backward(hidden, table, labels, lse, dloss, piece=256)[0], whole[0])   # (another order of sums)
+    for piece in (ze.ZE_MAX_ROWS, 1 << 64, (1 << 64) + 256):
+        for got, want in zip(ze.ze_vocab_loss_backward(hidden, table, labels, lse, dloss, piece=piece), whole):
+            assert torch.equal(got, want)

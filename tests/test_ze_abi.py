@@ -186,3 +186,21 @@ def test_rows_that_overlap_are_copied():
     for backward in (False, True):
         size = (lambda f: L.ze_loss_backward_work_bytes(f, GOOD, GOOD, 0)) if backward else lambda f: L.ze_loss_work_bytes(f, GOOD, GOOD)
         assert size(_form(rows=65, stride_table=32)) > size(_form(rows=65)) == size(_form(rows=65, stride_table=96))
+
+
+@pytest.mark.parametrize("first", (-1, (1 << 63) - ze.ZE_MAX_ROWS, 1 << 63, 1 << 64, (1 << 64) + 5, -(1 << 64)))
+def test_binding_refuses_a_first_id_that_does_not_fit(first):
+    """Cut to 64 bits, the last three would be 0 or 5: another shard's rows."""
+    t, ids = torch.zeros(4, 8), torch.zeros(4, dtype=torch.int64)
+    for call in (lambda: ze.ze_embedding(ids, t, first=first), lambda: ze.ze_embedding_backward(ids, t, 3, first=first),
+                 lambda: ze.ze_vocab_loss(t, t, ids, first=first), lambda: ze.ze_vocab_loss_backward(t, t, ids, t, t, first=first)):
+        with pytest.raises(zc.ZcError) as refused:
+            call()
+        assert refused.value.code == ze.ZC_ERR_ARG
+
+
+@pytest.mark.parametrize("rows", (-1, ze.ZE_MAX_ROWS + 1, 1 << 64, (1 << 64) + 3))
+def test_binding_refuses_rows_that_do_not_fit(rows):
+    with pytest.raises(zc.ZcError) as refused:
+        ze.ze_embedding_backward(torch.zeros(4, dtype=torch.int64), torch.zeros(4, 8), rows)
+    assert refused.value.code == zc.ZC_ERR_SIZE
