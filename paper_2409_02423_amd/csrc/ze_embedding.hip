@@ -2,8 +2,10 @@
 //
 // The gradient is a sum over the tokens that have a row, in the order of the tokens.  They are sorted by row (a stable counting sort, eight bits of the
 // row's number at a time), the sorted list is cut into pieces of the same length, and each wavefront adds up one piece, for 64 vectors of the
-// columns: a row whose tokens lie within a piece is done, parts of rows that go on are kept and joined by a second kernel.  So a token that half of the batch has
-// takes no longer than others, there are no sums by atomics, and their order depends on the ids alone.
+// columns: a row whose tokens lie within a piece is done, parts of rows that go on are kept and joined by a second kernel, in which a workgroup shares out a
+// row of many parts.  So there are no sums by atomics, their order depends on the ids alone, and a token that the whole batch has (a pad token that is
+// an ordinary row) takes 1.1 to 2.2 times the time of as many tokens of many rows: 8192 tokens of 6144 bf16 values 121 us for 110, 16384 of 256 87 for 56,
+// 16384 of 1024 146 for 66, 65536 of 1024 163 for 91.
 //
 // Memory bounds both on large tensors, the chain of launches the gradient of small ones.  8192 tokens on one of four ranks, 12608 rows of 6144
 // bf16 values: lookup 23.8 us at 4.9 TB/s, of which six sevenths are written; fp32 gradient 11.9 (sort) + 62.6 (sums and zeros, 5.4 TB/s) + 5.8 (joins).
@@ -483,54 +485,110 @@ __global__ void __launch_bounds__(kThreads) sum_kernel(SumArgs a) {
   }
 }
 
-// The rows whose tokens do not lie within a piece (few, where ids are many: the launch is most of the time, 3.3 to 5.8 us): the sums that were kept of them, from the piece that they begin in.
-template <int DT, int DO>
-__device__ __forceinline__ void join_from(const SumArgs& a, uint32_t piece, int vector) {
+// The rows whose tokens do not lie within a piece (few, where ids are many: the launch is most of the time): the sums that were kept of them, from the piece
+// that they begin in.
+constexpr int kJoinThreads = 512, kJoinWaves = kJoinThreads / 64;
+constexpr uint32_t kShortRun = 32;   // pieces behind its first that a wavefront adds up alone
+
+// The last piece of the run that goes on from a piece into the next, or the piece itself where none does, or one that began before.
+__device__ __forceinline__ uint32_t last_of_run(const SumArgs& a, uint32_t piece, uint32_t& key) {
+  const uint32_t from = piece * (uint32_t)a.piece, next = from + (uint32_t)a.piece;
+  if (piece + 1 >= a.pieces) return piece;
+  key = a.keys[next - 1];
+  if (key >= a.rows || a.keys[next] != key) return piece;
+  // a run that fills the piece and comes from the one before it began there
+  if (a.keys[from] == key && from > 0 && a.keys[from - 1] == key) return piece;
+  // The pieces' first keys are sorted: those of the run come before all others.  64 are compared at once, next to one another and then as far apart as
+  // those that are left ask for.
+  uint32_t low = piece, high = a.pieces, step = 1;   // low has the key, high (or the end) has not
+  for (;;) {
+    const uint32_t q = low + ((threadIdx.x & 63) + 1) * step;
+    const uint64_t same = __builtin_amdgcn_ballot_w64(q < high && a.keys[q * (size_t)a.piece] == key);
+    const uint32_t many = ~same ? (uint32_t)__builtin_ctzll(~same) : 64;
+    if (many < 64 && low + (many + 1) * step < high) high = low + (many + 1) * step;
+    low += many * step;
+    if (high - low <= 1) return low;
+    step = (high - low - 1 + 63) / 64;
+  }
+}
+
+// sum += the first sums that were kept of the pieces from..to-1, in their order
+template <int DT>
+__device__ __forceinline__ void add_kept(const SumArgs& a, uint32_t from, uint32_t to, int vector, float (&sum)[kVec<DT>]) {
   constexpr int kN = kVec<DT>, kAhead = 8;
   typedef float f4 __attribute__((ext_vector_type(4)));
-  const uint32_t from = piece * (uint32_t)a.piece, next = from + (uint32_t)a.piece;
-  if (piece + 1 >= a.pieces) return;
-  const uint32_t key = a.keys[next - 1];
-  if (key >= a.rows || a.keys[next] != key) return;
-  // a run that fills the piece and comes from the one before it began there
-  if (a.keys[from] == key && from > 0 && a.keys[from - 1] == key) return;
-  // the run's last piece: 64 of their first keys are compared at once
-  uint32_t last = piece;
-  for (;;) {
-    const uint32_t q = last + 1 + (threadIdx.x & 63);
-    const uint64_t same = __builtin_amdgcn_ballot_w64(q < a.pieces && a.keys[q * (size_t)a.piece] == key);
-    const int many = ~same ? __builtin_ctzll(~same) : 64;
-    last += many;
-    if (many < 64) break;
-  }
-  if (vector >= a.vectors) return;
-  Raw<DO, kN> old;
-  if (a.accumulate) load_old<DT, DO>(a, key, vector, old);
-  float sum[kN];
-  const float* p = kept_at<DT>(a, piece, 1, vector);
-#pragma unroll
-  for (int j = 0; j < kN; ++j) sum[j] = p[j];
-  for (uint32_t q = piece + 1; q <= last; q += kAhead) {
+  for (uint32_t q = from; q < to; q += kAhead) {
     f4 v[kAhead][kN / 4];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)
 #pragma unroll
-      for (int j = 0; j < kN / 4; ++j) v[u][j] = reinterpret_cast<const f4*>(kept_at<DT>(a, q + u <= last ? q + u : last, 0, vector))[j];
+      for (int j = 0; j < kN / 4; ++j) v[u][j] = reinterpret_cast<const f4*>(kept_at<DT>(a, q + u < to ? q + u : to - 1, 0, vector))[j];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)
-      if (q + u <= last) {
+      if (q + u < to) {
 #pragma unroll
         for (int j = 0; j < kN; ++j) sum[j] += v[u][j / 4][j % 4];
       }
   }
-  store_sums<DT, DO>(a, key, vector, sum, old);
 }
 
+// A wavefront for each piece and 64 vectors of the columns; a workgroup has pieces that follow one another.  A run of many pieces (one at most begins among
+// them: kShortRun is more than they are) is shared out among all wavefronts, each of which adds up pieces that follow one another, and their
+// sums are added in that order: what bounds it are loads that wait for one another, eight parts at a time.  All tokens of one row, us a call, with one wavefront for
+// a run and with eight: 16384 tokens of 256 bf16 values 244 and 87, 65536 of 1024 292 and 163.  Sixteen took 82 and 122, and 84.8 for 81.2 where no run is
+// long (8192 tokens of 6144).
 template <int DT, int DO>
-__global__ void __launch_bounds__(kThreads) join_kernel(SumArgs a) {
-  const uint32_t chunks = (a.vectors + 63) / 64, units = a.pieces * chunks;
-  for (uint32_t unit = __builtin_amdgcn_readfirstlane(blockIdx.x * (kThreads / 64) + threadIdx.x / 64); unit < units; unit += gridDim.x * (kThreads / 64))
-    join_from<DT, DO>(a, unit / chunks, (int)(unit % chunks * 64 + (threadIdx.x & 63)));
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(SumArgs a) {
+  constexpr int kN = kVec<DT>;
+  static_assert(kShortRun >= kJoinWaves, "one long run in a workgroup");
+  __shared__ uint32_t lasts[kJoinWaves];   // of a long run that begins in the wavefront's piece, or 0
+  __shared__ float sums[kJoinWaves][kN][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const uint32_t groups = (a.pieces + kJoinWaves - 1) / kJoinWaves, units = groups * ((a.vectors + 63) / 64);
+  for (uint32_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const uint32_t first = unit % groups * kJoinWaves, piece = first + wave;
+    const int vector = (int)(unit / groups * 64) + lane;
+    const bool there = vector < a.vectors;
+    uint32_t key = 0;
+    const uint32_t last = last_of_run(a, piece, key);
+    const bool many = last - piece > kShortRun;
+    if (lane == 0) lasts[wave] = many ? last : 0;
+    Raw<DO, kN> old;
+    float sum[kN];
+    if (last > piece && there) {
+      if (a.accumulate) load_old<DT, DO>(a, key, vector, old);
+      const float* p = kept_at<DT>(a, piece, 1, vector);
+#pragma unroll
+      for (int j = 0; j < kN; ++j) sum[j] = p[j];
+      if (!many) {
+        add_kept<DT>(a, piece + 1, last + 1, vector, sum);
+        store_sums<DT, DO>(a, key, vector, sum, old);
+      }
+    }
+    __syncthreads();
+    const uint32_t mine = lasts[lane % kJoinWaves];
+    const uint64_t with = __builtin_amdgcn_ballot_w64(mine > 0) & ((1u << kJoinWaves) - 1);
+    if (with) {   // (the same in all wavefronts)
+      const int owner = __builtin_ctzll(with);
+      const uint32_t begin = first + owner + 1, count = (uint32_t)__builtin_amdgcn_readlane((int)mine, owner) + 1 - begin;
+      const uint32_t from = begin + (uint32_t)((uint64_t)count * wave / kJoinWaves), to = begin + (uint32_t)((uint64_t)count * (wave + 1) / kJoinWaves);
+      float part[kN];
+#pragma unroll
+      for (int j = 0; j < kN; ++j) part[j] = 0.0f;
+      if (there) add_kept<DT>(a, from, to, vector, part);
+#pragma unroll
+      for (int j = 0; j < kN; ++j) sums[wave][j][lane] = part[j];
+      __syncthreads();
+      if (wave == owner && there) {
+#pragma unroll 4
+        for (int w = 0; w < kJoinWaves; ++w)
+#pragma unroll
+          for (int j = 0; j < kN; ++j) sum[j] += sums[w][j][lane];
+        store_sums<DT, DO>(a, key, vector, sum, old);
+      }
+    }
+    __syncthreads();
+  }
 }
 
 // ---- host ----------------------------------------------------------------------------------
@@ -596,7 +654,8 @@ void launch_sums(const SumArgs& a, size_t rows, hipStream_t s) {
   SumArgs b = a;
   b.sum_groups = (unsigned)(groups < kMostGroups ? groups : kMostGroups);
   hipLaunchKernelGGL((sum_kernel<DT, DO>), dim3((unsigned)(b.sum_groups + (zeros < kMostGroups ? zeros : kMostGroups))), dim3(kThreads), 0, s, b);
-  if (a.pieces > 1) hipLaunchKernelGGL((join_kernel<DT, DO>), dim3(b.sum_groups), dim3(kThreads), 0, s, b);
+  const size_t joins = parts((size_t)a.pieces, kJoinWaves) * parts((size_t)a.vectors, 64);
+  if (a.pieces > 1) hipLaunchKernelGGL((join_kernel<DT, DO>), dim3((unsigned)(joins < kMostGroups ? joins : kMostGroups)), dim3(kJoinThreads), 0, s, b);
 }
 
 }  // namespace
