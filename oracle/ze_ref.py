@@ -143,3 +143,42 @@ def vocab_loss_backward(hidden, table, labels, lse, dloss, first=0, scale=1.0):
     dtable, dtable_off = product(g.t().contiguous(), g_off.t().contiguous(), hd, n)
     dhidden_off[~present] = 0.0
     return (dhidden, dtable), (dhidden_off, dtable_off)
+
+
+def vocab_loss_backward_as_stored(hidden, table, labels, lse, dloss, first=0, exact_logits=False):
+    """vocab_loss_backward at scale 1 with g / max |dloss| (fp16: times 2^15) rounded to the inputs' type, as the header says that it lies in the workspace, so that
+    the bounds hold what is left: roundings of the products, and of g only where it lies so near to the middle between two values of its type that
+    its own error decides.  Rounding keeps order, so g as stored lies between its formula less its error, rounded, and plus its error, rounded.  exact_logits: the
+    caller has chosen inputs whose products and sums fp32 holds exactly, in any order."""
+    dtype = hidden.dtype
+    labels = labels.reshape(-1)
+    n, rows = labels.numel(), table.shape[0]
+    present = labels >= 0
+    h = torch.where(present[:, None], hidden.reshape(n, -1), torch.zeros_like(hidden.reshape(n, -1)))
+    zero = torch.zeros(n, dtype=torch.float64, device=h.device)
+    lse, dloss = (torch.where(present, v.reshape(-1).double(), zero) for v in (lse, dloss))
+    l, off = _logits(h, table, 1.0)
+    if exact_logits:
+        off = torch.zeros_like(off)
+    p = torch.exp(l - lse[:, None])
+    off = p * torch.expm1(off + 4 * U32 * (l.abs() + lse.abs()[:, None]) + 4 * U32)
+    at, here = _local(labels, first, rows)
+    most, lift = dloss.abs().max(), 2.0 ** 15 if dtype == torch.float16 else 1.0
+    unit = (dloss / most * lift)[:, None]
+    off = unit.abs() * (off + 4 * U32 * (p + off))
+    g = unit * p
+    g[here, at[here]] -= unit[here, 0]
+    off[here, at[here]] += 4 * U32 * unit[here, 0].abs()
+    low, high = (g - off).to(dtype).double(), (g + off).to(dtype).double()
+    g, off = (low + high) / 2, (high - low) / 2
+    g[~present], off[~present] = 0.0, 0.0
+    factor = most / lift
+
+    def product(a, a_off, b, k):
+        value = factor * (a @ b)
+        size = factor * ((a.abs() + a_off) @ b.abs())
+        return value, stored(value, factor * (a_off @ b.abs()) + 2 * U32 * _chain(k, dtype) * size + 4 * U32 * value.abs(), dtype)
+
+    dhidden, dhidden_off = product(g, off, table.double(), rows)
+    dtable, dtable_off = product(g.t().contiguous(), off.t().contiguous(), h.double(), n)
+    return (dhidden, dtable), (dhidden_off, dtable_off)

@@ -334,3 +334,66 @@ def test_pieces_of_more_rows_than_an_argument_holds():
     for piece in (ze.ZE_MAX_ROWS, 1 << 64, (1 << 64) + 256):
         for got, want in zip(ze.ze_vocab_loss_backward(hidden, table, labels, lse, dloss, piece=piece), whole):
             assert torch.equal(got, want)
+
+
+def _whole_inputs(tokens, rows, cols, dtype, seed, absent=0.2):
+    """Hidden states of -1 and 1 and a matrix of 0 and two values that are a power of two from 0: logits of a spread of about 1, which fp32 holds exactly."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    sign = lambda *shape: torch.randint(0, 2, shape, generator=g, device="cuda") * 2 - 1
+    hidden = sign(tokens, cols).to(dtype)
+    step = 2.0 ** -((cols - 1).bit_length() // 2)
+    table = (sign(rows, cols) * torch.randint(0, 3, (rows, cols), generator=g, device="cuda").clamp_max(1) * step).to(dtype)
+    labels = torch.randint(0, rows, (tokens,), generator=g, device="cuda")
+    labels[torch.rand(tokens, generator=g, device="cuda") < absent] = -100
+    labels[-1] = rows - 1                                     # the last row of all is one of those that count
+    return hidden, table, labels, (0.2 + torch.rand(tokens, generator=g, device="cuda")) / tokens
+
+
+def _check_whole(hidden, table, labels, dloss, piece=0, **out):
+    stats = ze.ze_vocab_loss(hidden, table, labels)
+    _check_stats(stats, hidden, table, labels, 0, 1.0)
+    lse = ze.ze_join_loss(stats, labels)[1]
+    got = ze.ze_vocab_loss_backward(hidden, table, labels, lse, dloss, piece=piece, **out)
+    for a, b, c in zip(got, *ze_ref.vocab_loss_backward_as_stored(hidden, table, labels, lse, dloss, exact_logits=True)):
+        _close(a, b, c)
+    for a, b in zip(got, ze.ze_vocab_loss_backward(hidden, table, labels, lse, dloss, piece=piece)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("tokens, rows, cols", [(90, 700, 128), (600, 3001, 520), (1030, 5000, 1024), (2048, 8192, 2048), (2047, 6201, 4106), (4100, 4096, 64)])
+def test_gradients_are_off_by_the_rounding_of_g_alone(dtype, tokens, rows, cols):
+    """All shapes of tiles in half precision: with g rounded as it is stored, what is left are roundings of fp32 sums and of the result, so that one step of a product
+    too few would show."""
+    _check_whole(*_whole_inputs(tokens, rows, cols, TYPES[dtype], 3))
+
+
+# A matrix that has to be copied comes in pieces of 64 MiB, forward and backward: of odd width, at an odd place, of rows that overlap
+@pytest.mark.parametrize("tokens, rows, cols, dtype, start", [(130, 50003, 2049, "bf16", 0), (600, 50003, 2049, "f16", 0), (200, 33000, 1026, "f16", 1), (5, 70001, 1023, "bf16", 0)])
+def test_a_copied_matrix_in_pieces(tokens, rows, cols, dtype, start):
+    hidden, close, labels, dloss = _whole_inputs(tokens, rows, cols, TYPES[dtype], 17)
+    table = torch.empty(rows * cols + start, dtype=TYPES[dtype], device="cuda")[start:].view(rows, cols)
+    table.copy_(close)
+    labels[:4] = torch.tensor([0, rows // 2, rows - 2, rows // 3], device="cuda")
+    _check_whole(hidden, table, labels, dloss)
+
+
+def test_a_copied_matrix_of_rows_that_overlap_in_pieces():
+    hidden, _, labels, dloss = _whole_inputs(70, 20001, 1000, torch.float32, 19)
+    flat = torch.randint(-1, 2, (20000 * 500 + 1000,), generator=torch.Generator(device="cuda").manual_seed(20), device="cuda") / 32.0
+    _check_whole(hidden, flat.as_strided((20001, 1000), (500, 1)), labels, dloss)
+
+
+@pytest.mark.parametrize("absent", (0.1, 0.9))
+@pytest.mark.parametrize("tokens, rows, cols, dtype, piece", [
+    (2048, 8300, 2048, "bf16", 4096), (2047, 8200, 2050, "f16", 4096),        # large tiles of the hidden states' gradient: shares of 64 steps, and of two and one
+    (3000, 8300, 1024, "bf16", 4096), (1000, 3000, 4096, "f16", 1024),        # half ones, three steps under way
+    (300, 4200, 2048, "bf16", 2048), (300, 9000, 512, "f16", 1024), (300, 1100, 2048, "f32", 512)])
+def test_pieces_whose_steps_are_shared_out(tokens, rows, cols, dtype, piece, absent):
+    """Sums that several workgroups keep from piece to piece, the last piece with fewer steps than there are workgroups for them."""
+    _check_whole(*_whole_inputs(tokens, rows, cols, TYPES[dtype], 23, absent), piece=piece)
+
+
+def test_a_large_vocabulary_in_the_librarys_pieces():
+    """Two pieces, five shares of each."""
+    _check_whole(*_whole_inputs(4096, 50257, 768, torch.bfloat16, 29))
