@@ -19,7 +19,8 @@
  *     to even, where it is stored, but for what ze_vocab_loss_backward says.  Results do not depend on the
  *     order in which workgroups run.
  *   - A workspace is aligned to 256 bytes; its contents before and after a call do not matter.
- *   - No output overlaps an input or another output, and no two rows of an output overlap.
+ *   - No output overlaps an input or another output, and no two rows of an output overlap.  (One may take the place of another: d_dhidden that of
+ *     d_hidden, at the same address with the same stride.)
  */
 #ifndef ZE_H
 #define ZE_H

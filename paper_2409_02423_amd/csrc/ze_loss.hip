@@ -194,7 +194,8 @@ __global__ void __launch_bounds__(kListThreads) list_kernel(const ID* ids, int t
 // ---- rows where the products can read them -----------------------------------------------
 
 // The rows with a label, packed; and zeros for the gradients of the hidden states of tokens without one.  (One pass over them, 31.5 us for 8192 x 6144 bf16 values, 6.4 TB/s: the
-// matrix's gradient runs over them across k, where a list of places would be one for each row of each step.)
+// matrix's gradient runs over them across k, where a list of places would be one for each row of each step.  After it the hidden states themselves are not read any
+// more, and the rows that are read are not those that get zeros: so the gradients may take their place.)
 template <int DT>
 __global__ void __launch_bounds__(kThreads) pack_hidden_kernel(PackArgs a, size_t from, const int* row_of, size_t tokens, char* dhidden, size_t dhidden_stride) {
   const size_t r = from + blockIdx.x;

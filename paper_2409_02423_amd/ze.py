@@ -219,7 +219,7 @@ def ze_vocab_loss_backward(d_hidden, d_table, d_labels, d_lse, d_dloss, first=0,
                            want_table=True, piece=0):
     """(d_dhidden, d_dtable): the gradients of the hidden states (this rank's part, to be added up over the ranks) and of this rank's rows, from d_lse
     (ze_join_loss) and the gradient of each token's loss.  want_hidden or want_table False: that one is not computed (and None).
-    piece: rows of the table whose probabilities lie in the workspace at a time, 0 for the library's choice."""
+    piece: rows of the table whose probabilities lie in the workspace at a time, 0 for the library's choice.  d_dhidden may be d_hidden."""
     c, hidden, table = _loss_call(d_hidden, d_table, d_labels, first, scale)
     if (d_dhidden is not None and not want_hidden) or (d_dtable is not None and not want_table):
         raise ValueError("an output that is not wanted")

@@ -397,3 +397,20 @@ def test_pieces_whose_steps_are_shared_out(tokens, rows, cols, dtype, piece, abs
 def test_a_large_vocabulary_in_the_librarys_pieces():
     """Two pieces, five shares of each."""
     _check_whole(*_whole_inputs(4096, 50257, 768, torch.bfloat16, 29))
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("tokens, rows, cols, piece", [(70, 300, 65, 0), (500, 2000, 256, 512), (2100, 4200, 1024, 0), (40, 0, 64, 0)])
+def test_gradients_in_the_hidden_states_place(dtype, tokens, rows, cols, piece):
+    """Where many tokens have no label: their rows become zeros while the others' are read, which lie between them."""
+    hidden, table, labels, dloss = _inputs(tokens, rows, cols, TYPES[dtype], 43, absent=0.5)
+    hidden[labels < 0] = float("nan")
+    lse = ze.ze_join_loss(ze.ze_vocab_loss(hidden, table, labels), labels)[1]
+    want = ze.ze_vocab_loss_backward(hidden, table, labels, lse, dloss, piece=piece)
+    wide = torch.full((tokens, cols + 7), 7.0, dtype=TYPES[dtype], device="cuda")
+    for place in (hidden.clone(), wide[:, 3:3 + cols].copy_(hidden)):
+        got = ze.ze_vocab_loss_backward(place, table, labels, lse, dloss, d_dhidden=place, piece=piece)
+        assert got[0] is place and torch.equal(place, want[0]) and torch.equal(got[1], want[1])
+        assert (place[labels < 0] == 0).all()
+    wide[:, 3:3 + cols] = 7.0
+    assert (wide == 7.0).all()
