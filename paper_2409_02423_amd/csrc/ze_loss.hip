@@ -678,20 +678,17 @@ int shape_for(int dtype, size_t nx, size_t ny) {
   return best;
 }
 
-#define ZE_BY_SHAPE(SHAPE, DT, LAUNCH)              \
+#define ZE_BY_SHAPE_AND(HALF, SHAPE, DT, LAUNCH)    \
   do {                                              \
     if ((SHAPE) == kMedium) LAUNCH(DT, Medium);     \
     else if ((SHAPE) == kSmall) LAUNCH(DT, Small);  \
     else if constexpr (DT != kF32) {                \
-      if ((SHAPE) == kHalf) LAUNCH(DT, Half);       \
+      if ((SHAPE) == kHalf) LAUNCH(DT, HALF);       \
       else LAUNCH(DT, Large);                       \
     }                                               \
   } while (0)
-#define ZE_BY_SHAPE_OF_HIDDEN(SHAPE, DT, LAUNCH)    \
-  do {                                              \
-    if ((SHAPE) != kHalf) ZE_BY_SHAPE(SHAPE, DT, LAUNCH); \
-    else if constexpr (DT != kF32) LAUNCH(DT, Deep); \
-  } while (0)
+#define ZE_BY_SHAPE(SHAPE, DT, LAUNCH) ZE_BY_SHAPE_AND(Half, SHAPE, DT, LAUNCH)
+#define ZE_BY_SHAPE_OF_HIDDEN(SHAPE, DT, LAUNCH) ZE_BY_SHAPE_AND(Deep, SHAPE, DT, LAUNCH)
 #define ZE_BY_SHAPE_OF_LOGITS(SHAPE, DT, LAUNCH)    \
   do {                                              \
     if ((SHAPE) == kThin) LAUNCH(DT, Thin);         \

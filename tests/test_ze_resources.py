@@ -74,3 +74,11 @@ def test_large_products_keep_their_sums_in_place(assembly):
             assert "v_accvgpr" not in body[body.rindex("v_mfma", 0, at):at], name
         seen += 1
     assert seen >= 14
+
+
+def test_half_tiles_of_the_hidden_gradient_have_three_steps_under_way(assembly):
+    """Kernels of that gradient with two, which the other products' half tiles have, would have no caller."""
+    stages = {}
+    for kind, n in re.findall(r"\.amdhsa_kernel \S*\d([a-z_]+_kernel)ILi\dENS_5ShapeILi256ELi128ELi2ELi2ELi(\d)E", assembly["ze_loss.hip"]):
+        stages.setdefault(kind, set()).add(n)
+    assert stages == {"logits_kernel": {"2"}, "gradient_kernel": {"2"}, "table_gradient_kernel": {"2"}, "hidden_gradient_kernel": {"3"}, "hidden_finish_kernel": {"3"}}
