@@ -771,10 +771,22 @@ Plan plan_with(const struct ze_form& f, bool backward, size_t piece, bool pack_h
     p.g = places.take(p.padded * padded * p.e);
     const size_t steps = padded * p.e / kStepBytes;
     p.hidden_shape = shape_for(f.dtype, f.cols, f.tokens);
-    // Where a tile's steps are shared out, few tiles are as good as many.  Large ones then keep twice the sums that half ones do, and take two thirds of
-    // the time for a product (2047 tokens, half with a label, 32003 x 2048 fp16 values: 118 us and 12 of joining; half ones 151 + 8, medium 168 + 8).
+    // Where a tile's steps are shared out, few tiles are as good as many.  Large ones then keep twice the sums that half ones do, which pays once there are
+    // many steps for each compute unit.  Backward calls without the matrix's gradient, bf16, large / half tiles in us, with all tokens labelled and
+    // with half of them:
+    //
+    //     tokens x rows x cols     steps of all large tiles / compute units
+    //     1024 x 2000 x 2048         4          54.7 / 48.5      47.3 / 41.2
+    //     1024 x 8000 x 2048        16          93.1 / 88.4      79.3 / 72.1
+    //     1024 x 16000 x 2048       31         140.0 / 138.7    108.5 / 104.2
+    //     1024 x 32003 x 2048       63         234.9 / 242.1    139.2 / 139.7
+    //     512 x 32003 x 4096        63         234.7 / 257.6    191.9 / 185.9
+    //     2047 x 32003 x 2048      125         438.5 / 470.3    240.4 / 243.8
+    //
+    // Below 32 half ones were as fast or faster in all of 120 calls, up to 1.16 times; from 125 on large ones in all of 10.
+    constexpr size_t kManySteps = 48;
     if (f.dtype != ZC_F32 && f.tokens > (size_t)kSizes[kSmall].y && p.hidden_shape != kLarge && tiles(kHalf, f.cols, f.tokens) * (steps / 8) >= kComputeUnits)
-      p.hidden_shape = tiles(kLarge, f.cols, f.tokens) * steps >= 16 * kComputeUnits ? kLarge : kHalf;
+      p.hidden_shape = tiles(kLarge, f.cols, f.tokens) * steps >= kManySteps * kComputeUnits ? kLarge : kHalf;
     const Size& size = kSizes[p.hidden_shape];
     p.sharers = size.at_once * kComputeUnits;   // as many as run at once
     p.most_splits = (int)(steps < 16 ? 1 : steps / 8);

@@ -361,7 +361,7 @@ def _check_whole(hidden, table, labels, dloss, piece=0, **out):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-@pytest.mark.parametrize("tokens, rows, cols", [(90, 700, 128), (600, 3001, 520), (1030, 5000, 1024), (2048, 8192, 2048), (2047, 6201, 4106), (4100, 4096, 64)])
+@pytest.mark.parametrize("tokens, rows, cols", [(90, 700, 128), (600, 3001, 520), (1030, 5000, 1024), (2048, 8192, 2048), (2047, 6201, 4106), (1024, 32003, 2048), (4100, 4096, 64)])
 def test_gradients_are_off_by_the_rounding_of_g_alone(dtype, tokens, rows, cols):
     """All shapes of tiles in half precision: with g rounded as it is stored, what is left are roundings of fp32 sums and of the result, so that one step of a product
     too few would show."""
@@ -386,8 +386,9 @@ def test_a_copied_matrix_of_rows_that_overlap_in_pieces():
 
 @pytest.mark.parametrize("absent", (0.1, 0.9))
 @pytest.mark.parametrize("tokens, rows, cols, dtype, piece", [
-    (2048, 8300, 2048, "bf16", 4096), (2047, 8200, 2050, "f16", 4096),        # large tiles of the hidden states' gradient: shares of 64 steps, and of two and one
-    (3000, 8300, 1024, "bf16", 4096), (1000, 3000, 4096, "f16", 1024),        # half ones, three steps under way
+    (2048, 16500, 4096, "bf16", 8192), (1021, 33000, 4098, "f16", 16384),     # large tiles of the hidden states' gradient: the last piece has two steps, and four
+    (2048, 8300, 2048, "bf16", 4096), (2047, 8200, 2050, "f16", 4096),        # half ones, three steps under way
+    (3000, 8300, 1024, "bf16", 4096), (1000, 3000, 4096, "f16", 1024),
     (300, 4200, 2048, "bf16", 2048), (300, 9000, 512, "f16", 1024), (300, 1100, 2048, "f32", 512)])
 def test_pieces_whose_steps_are_shared_out(tokens, rows, cols, dtype, piece, absent):
     """Sums that several workgroups keep from piece to piece, the last piece with fewer steps than there are workgroups for them."""
