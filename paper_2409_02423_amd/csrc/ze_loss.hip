@@ -4,11 +4,11 @@
 // logit and the sum of exponentials of its part of a row, a second kernel joins them.  Backward, for a piece of the vocabulary at a time: the same product again,
 // whose tiles become g = dloss (softmax - onehot) in the workspace, and two products that read it, along the vocabulary for the hidden states'
 // gradient and across it for the matrix's.  Tokens without a label are left out before anything else: the products work on a list of those that have
-// one, so what the others hold is not read at all.
+// one, so what the others hold has no part in any result.
 //
 // The products bound all of it, but for a few tokens, where reading the matrix does.  8192 tokens, 12608 rows of 6144 bf16 values: forward 964 us of
-// product (1317 TFLOP/s; a library's bare product of that size takes 957) and 15 of the rest; backward 1014 + 938 + 860 and 44.  The matrix units are 60 to 73 % busy at
-// the clock that their power leaves.  Four tokens: 34.0 us, 4.6 TB/s.
+// product (1317 TFLOP/s; a library's bare product of that size takes 957) and 15 of the rest; backward 1014 + 938 + 860 and 44 (3 to 5 % more on other cards).  The matrix
+// units are 60 to 73 % busy at the clock that their power leaves.  Four tokens: 34.0 us, 4.6 TB/s.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -752,7 +752,8 @@ Plan plan_with(const struct ze_form& f, bool backward, size_t piece, bool pack_h
   }
   p.shape = shape_for(f.dtype, p.piece, f.tokens);
   if (!backward && f.tokens <= Thin::BY) p.shape = kThin;
-  // (The ends are added first also where a copy has them behind the rest: the sums do not depend on where the tensors lie.)
+  // (The ends are added first also where a copy has them behind the rest: the sums do not depend on where the tensors lie, as long as a copied table
+  // comes in the pieces that it would be taken in where it lies.  Of more than kMostPacked bytes it may come in more, whose tiles may have another shape.)
   p.steps = (int)(f.cols * p.e / kStepBytes);
   p.ends = f.cols * p.e % kStepBytes != 0;
   Places places;

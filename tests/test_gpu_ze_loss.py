@@ -415,3 +415,20 @@ def test_gradients_in_the_hidden_states_place(dtype, tokens, rows, cols, piece):
         assert (place[labels < 0] == 0).all()
     wide[:, 3:3 + cols] = 7.0
     assert (wide == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("tokens, rows, cols", [(9, 700, 130), (500, 3000, 1026), (1700, 2049, 1030), (2047, 6201, 4106)])
+def test_a_matrix_of_one_piece_gives_the_same_wherever_it_lies(dtype, tokens, rows, cols):
+    """Read where it lies, or copied from an odd place: up to 64 MiB the same bits, of the statistics and of both gradients."""
+    hidden, table, labels, dloss = _inputs(tokens, rows, cols, TYPES[dtype], 47)
+    apart = []
+    for t in (hidden, table):
+        apart.append(torch.empty(t.numel() + 1, dtype=t.dtype, device="cuda")[1:].view(t.shape).copy_(t))
+    stats = ze.ze_vocab_loss(hidden, table, labels)
+    lse = ze.ze_join_loss(stats, labels)[1]
+    want = ze.ze_vocab_loss_backward(hidden, table, labels, lse, dloss)
+    for h, w in ((hidden, apart[1]), (apart[0], table), tuple(apart)):
+        assert torch.equal(ze.ze_vocab_loss(h, w, labels), stats)
+        for a, b in zip(ze.ze_vocab_loss_backward(h, w, labels, lse, dloss), want):
+            assert torch.equal(a, b)
